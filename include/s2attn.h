@@ -142,6 +142,91 @@ typedef struct {
   int64_t page_stride, tok_stride; /* elements, multiples of 8; tok_stride >= head_dim       */
 } s2_paged_decode_args;
 
+/* A paged cache in one of three formats, and its block table (section 4.1's cache, as in
+ * s2_paged_decode_args: a page holds the block_size tokens of one logical block of one (sequence,
+ * head), K and V pools use the same page numbers, negative = not resident).
+ * S2_KV_BF16: rows of head_dim bf16 values, strides in elements, no scales.
+ * S2_KV_MXFP8: rows of head_dim bytes, e4m3 codes.  S2_KV_MXFP4: rows of head_dim / 2 bytes, e2m1
+ * codes, the even feature in the low half.  Strides in bytes.  Both have one scale to 32 features of a
+ * row, a power of two 2^e held as the byte e + 127 ([page, token, head_dim / 32] bytes): a row reads as
+ * code * 2^e, which bf16 holds exactly, so that attention over such a cache is attention over
+ * the bf16 cache that s2_kv_read_paged gives.  Byte 255 reads as NaN whatever the codes are; bytes below 17,
+ * which s2_kv_append_paged does not write, read as any value. */
+enum { S2_KV_BF16 = 0, S2_KV_MXFP8 = 1, S2_KV_MXFP4 = 2 };
+typedef struct {
+  void* k_pages;              /* DEVICE, element (page,t,d) at page*sp + t*st + d            */
+  void* v_pages;              /* DEVICE, same strides                                        */
+  void* k_scales;             /* DEVICE bytes, 4-byte aligned; NULL for S2_KV_BF16           */
+  void* v_scales;             /* DEVICE bytes, same strides                                  */
+  const int32_t* block_table; /* DEVICE int32 [nseq, heads, max_blocks]                      */
+  int32_t format, nseq, heads, head_dim; /* head_dim 64 or 128                               */
+  int32_t block_size;         /* 16, 32, 64 or 128                                           */
+  int32_t max_blocks;         /* row length of block_table                                   */
+  int32_t num_pages;          /* pages in each pool                                          */
+  int64_t page_stride, tok_stride; /* multiples of 16 bytes; a page's rows (block_size * tok_stride)
+                                      lie within 2^30 bytes                                  */
+  int64_t scale_page_stride, scale_tok_stride; /* bytes, multiples of head_dim / 32; tok >= head_dim / 32 */
+} s2_paged_cache;
+
+/* New rows for the cache: row r of head h at base + r*stride_row + h*stride_head + d (elements, multiples of 8). */
+typedef struct {
+  const void* k;          /* DEVICE bf16, may be NULL when num_rows is 0                      */
+  const void* v;          /* DEVICE bf16, same strides                                        */
+  const int32_t* cu_new;  /* DEVICE int32 [nseq + 1], ascending: sequence b's new tokens are items
+                             cu_new[b] .. cu_new[b+1]-1                                       */
+  const int32_t* start;   /* DEVICE int32 [nseq]: position of the sequence's first new token  */
+  const int32_t* rows;    /* DEVICE int32 [cu_new[nseq]] or NULL: the row that an item takes
+                             (NULL: item i is row i)                                          */
+  int32_t* skipped;       /* DEVICE int32[1] or NULL: the call ADDS the number of (item, head)
+                             pairs it left out; the caller zeroes it                          */
+  int32_t num_rows;       /* rows of k and v: an item whose row is not one of them is left out */
+  int32_t num_items;      /* entries of rows (without it not looked at): no item beyond them   */
+  int32_t max_new;        /* no sequence has more new tokens (>= 0; what is beyond is not looked at) */
+  int64_t stride_row, stride_head;
+} s2_kv_append_args;
+
+/* Where rows read from the cache go: item i of head h at base + i*stride_row + h*stride_head + d. */
+typedef struct {
+  void* k;                /* DEVICE bf16, out, may be NULL when num_rows is 0                 */
+  void* v;                /* DEVICE bf16, out, same strides                                   */
+  const int32_t* cu_rows; /* DEVICE int32 [nseq + 1], ascending: sequence b's tokens go to rows
+                             cu_rows[b] .. cu_rows[b+1]-1                                     */
+  const int32_t* start;   /* DEVICE int32 [nseq]: position of the first of them               */
+  int32_t num_rows;       /* rows of k and v                                                  */
+  int32_t max_rows;       /* no sequence reads more tokens (>= 0; what is beyond is not looked at) */
+  int64_t stride_row, stride_head;
+} s2_kv_read_args;
+
+/* One decode step over such a cache. */
+typedef struct {
+  const void* q;           /* DEVICE bf16 [nseq, heads, head_dim], element (b,h,d) at
+                              b*q_stride_seq + h*q_stride_head + d; o has the same strides    */
+  const int32_t* seq_lens; /* DEVICE int32 [nseq], each in [1, max_blocks*block_size]         */
+  void* o;                 /* DEVICE bf16, out                                                */
+  float* lse;              /* DEVICE fp32 [nseq, heads], out (may be NULL)                    */
+  int32_t* missing;        /* as in s2_paged_decode_args                                      */
+  int32_t num_splits;      /* KV splits per (sequence, head); 0 = library chooses             */
+  int64_t q_stride_seq, q_stride_head; /* elements, multiples of 8                            */
+} s2_cache_decode_args;
+
+/* A tree of drafted tokens to each sequence, its nodes beyond the seq_lens[b] tokens in the cache.  Element (b,h,i,d) of
+ * q and o at b*q_stride_seq + h*q_stride_head + i*q_stride_node + d, of k and v at the kv_* strides. */
+typedef struct {
+  const void* q;           /* DEVICE bf16                                                     */
+  const void* k;           /* DEVICE bf16: keys and values of the nodes (not in the cache)    */
+  const void* v;           /* DEVICE bf16                                                     */
+  const int32_t* parents;  /* DEVICE int32 [nseq, nodes]: an earlier node of the sequence, or -1: the
+                              last cached token.  Anything else: there is no such node        */
+  const int32_t* seq_lens; /* DEVICE int32 [nseq], each in [0, max_blocks*block_size]         */
+  void* o;                 /* DEVICE bf16, out                                                */
+  float* lse;              /* DEVICE fp32 [nseq, heads, nodes], out (may be NULL)             */
+  int32_t* missing;        /* as in s2_paged_decode_args; a block that several rows keep counts once */
+  int32_t nodes;           /* 1 .. 64                                                         */
+  int32_t num_splits;      /* KV splits per (sequence, head); 0 = library chooses             */
+  int64_t q_stride_seq, q_stride_head, q_stride_node;    /* elements, multiples of 8          */
+  int64_t kv_stride_seq, kv_stride_head, kv_stride_node; /* elements, multiples of 8          */
+} s2_tree_args;
+
 /* ---- layout (section 4.2 mask -> compressed lists, section 3.2) ------------------------- */
 
 /* Builds the per-head lists of kept KV blocks from the closed form of the mask, on the host,
@@ -364,6 +449,46 @@ int s2_attn_decode_paged_layout(const s2_layout* layout, const s2_paged_decode_a
                                 void* workspace, size_t workspace_bytes, void* stream);
 int s2_layout_resident_blocks(const s2_layout* layout, int32_t head, int32_t length,
                               int32_t* blocks, int32_t capacity, int32_t* count);
+
+/* ---- a paged cache in bf16, 8 or 4 bits (section 4.1) --------------------------------------- */
+
+/* Writes new rows into the pages of their (sequence, head, block): item i of sequence b is the token at
+ * position start[b] + i.  Quantising (S2_KV_MXFP8, S2_KV_MXFP4): of each 32 features with largest magnitude a, the scale is
+ * 2^e with the smallest e >= -110 for which a * 2^-e < 464 (e4m3) or 7 (e2m1), and a code is the nearest to x * 2^-e, ties to
+ * even; features that are not all finite and below 2^127 are written as scale byte 255, codes 0.  The result depends on
+ * a row's values alone.  An item is left out for a head whose table does not hold its block (an evicted one), and
+ * for all heads where its position is not in [0, max_blocks*block_size) or its row not in [0, num_rows); nothing but the rows of
+ * the items written is touched.  Two items that name one position of one page leave either, but items may take the same row.
+ * Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
+int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void* stream);
+
+/* Rows of the cache as bf16, what their codes stand for: sequence b's row i is the token at position start[b] + i.
+ * A row whose block is not resident, or whose position is outside [0, max_blocks*block_size), comes out as zeros.  Rows that belong to no
+ * sequence are left as they were.  Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
+int s2_kv_read_paged(const s2_paged_cache* c, const s2_kv_read_args* a, void* stream);
+
+/* s2_attn_decode_paged / s2_attn_decode_paged_layout over a cache of any format (over S2_KV_BF16, with q and o contiguous, it is that
+ * call).  The mask's block size and heads are the cache's.  Workspace as for s2_attn_decode with max_len = max_blocks * block_size.
+ * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
+int s2_attn_decode_paged_cache(const s2_layout_params* p, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
+                               void* workspace, size_t workspace_bytes, void* stream);
+int s2_attn_decode_paged_cache_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
+                                      void* workspace, size_t workspace_bytes, void* stream);
+
+/* Attention of a tree of drafted tokens over the cache: node i, with depth(i) nodes above it, is the token at position
+ * L + depth(i), L = seq_lens[b].  It attends, of the L cached tokens and of itself and the nodes above it, those whose
+ * block row (L + depth(i)) div S of the mask keeps: a chain of nodes gives what as many decode steps give.
+ * A node whose parent does not exist, or whose position is max_blocks*block_size or beyond, does not exist: its o is 0 and
+ * its lse -inf, and its q, k, v are not looked at.  What a node does not attend stays out of its result whatever it
+ * holds.  Kept blocks that are not resident contribute nothing and are counted, as in s2_attn_decode_paged.
+ * workspace: s2_attn_tree_workspace_bytes(..., max_blocks * block_size, num_splits) bytes, DEVICE, 256-byte aligned, contents
+ * undefined on entry and exit.  With a layout, it covers the cache.
+ * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
+int s2_attn_tree_paged(const s2_layout_params* p, const s2_paged_cache* c, const s2_tree_args* a, float scale,
+                       void* workspace, size_t workspace_bytes, void* stream);
+int s2_attn_tree_paged_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_tree_args* a, float scale,
+                              void* workspace, size_t workspace_bytes, void* stream);
+size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, int32_t head_dim, int32_t max_len, int32_t num_splits);
 
 /* ---- ceiling probes (measurement only) ------------------------------------------------------ */
 

@@ -510,3 +510,110 @@ def paged_decode_row_mask(q, k_pages, v_pages, table_row, length, Mh, block_size
             k[j * block_size:(j + 1) * block_size] = 0.0
             v[j * block_size:(j + 1) * block_size] = 0.0
     return decode_row_mask(q, k, v, L, Mh, block_size, scale)
+
+
+# ---------------------------------------------------------------------------------------------
+# A cache in 8 or 4 bits, and a tree of drafted tokens over a cache (section 4.1's cache, one step with several queries)
+# ---------------------------------------------------------------------------------------------
+def mx_code_values(fmt):
+    """The number that each code stands for at scale 1: fmt "mxfp8" (e4m3, 256 codes) or "mxfp4" (e2m1, 16 codes), written out bit by bit."""
+    exp_bits, man_bits, bias = (4, 3, 7) if fmt == "mxfp8" else (2, 1, 1)
+    out = []
+    for code in range(1 << (1 + exp_bits + man_bits)):
+        man = code & ((1 << man_bits) - 1)
+        exp = (code >> man_bits) & ((1 << exp_bits) - 1)
+        sign = -1.0 if code >> (man_bits + exp_bits) else 1.0
+        if fmt == "mxfp8" and exp == 15 and man == 7:
+            out.append(np.nan)
+        elif exp == 0:
+            out.append(sign * man / 2 ** man_bits * 2.0 ** (1 - bias))
+        else:
+            out.append(sign * (1 + man / 2 ** man_bits) * 2.0 ** (exp - bias))
+    return np.array(out)
+
+
+def mx_quantise(x, fmt):
+    """Rows x [..., D] -> (codes [..., D], scale bytes [..., D / 32]), by search.
+
+    Of each 32 features with largest magnitude a: the smallest e >= -110 with a 2^-e below the
+    bound at which codes end (464, 7); then of all codes the nearest to x 2^-e, the even one of two as near.
+    Not finite, or 2^127 and beyond: byte 255, codes 0.
+    """
+    x = np.asarray(x, dtype=np.float64)
+    b = x.reshape(x.shape[:-1] + (x.shape[-1] // 32, 32))
+    limit = 464.0 if fmt == "mxfp8" else 7.0
+    values = mx_code_values(fmt)
+    half = len(values) // 2
+    positive = values[:half][~np.isnan(values[:half])]  # ascending, their index is the code
+    blocks = b.reshape(-1, 32)
+    codes = np.zeros(blocks.shape, dtype=np.uint8)
+    byte = np.full(len(blocks), 255, dtype=np.uint8)
+    with np.errstate(invalid="ignore"):
+        top = np.abs(blocks).max(axis=1)
+        there = top < 2.0 ** 127
+    for e in range(-110, 128):  # (those that have no exponent yet)
+        do = there & (byte == 255) & (np.where(there, top, 0) * 2.0 ** -e < limit)
+        byte[do] = e + 127
+        for lo in range(0, int(do.sum()), 4096):
+            i = np.nonzero(do)[0][lo:lo + 4096]
+            off = np.abs(np.abs(blocks[i] * 2.0 ** -e)[..., None] - positive)
+            least = off.min(axis=-1)
+            first = off.argmin(axis=-1)  # of two as near the lower one: it, or the one after it if that is even
+            tie = (first + 1 < len(positive)) & (off[np.arange(len(i))[:, None], np.arange(32), np.minimum(first + 1, len(positive) - 1)] == least)
+            codes[i] = np.where(tie & (first % 2 == 1), first + 1, first) + np.where(np.signbit(blocks[i]), half, 0)
+    return codes.reshape(x.shape), byte.reshape(b.shape[:-1])
+
+
+def mx_values(codes, byte, fmt):
+    """What codes and scale bytes stand for."""
+    v = mx_code_values(fmt)[np.asarray(codes)]
+    v = v.reshape(v.shape[:-1] + (v.shape[-1] // 32, 32))
+    scale = np.exp2(np.asarray(byte, dtype=np.float64) - 127)
+    v = np.where(np.asarray(byte)[..., None] == 255, np.nan, v * scale[..., None])
+    return v.reshape(np.asarray(codes).shape)
+
+
+def tree_chains(parents):
+    """For every node the nodes from the root down to it, or None for one that does not exist (its parent is neither an
+    earlier node nor -1, or does not exist)."""
+    chains = []
+    for i, p in enumerate(parents):
+        if p == -1:
+            chains.append([i])
+        elif 0 <= p < i and chains[p] is not None:
+            chains.append(chains[p] + [i])
+        else:
+            chains.append(None)
+    return chains
+
+
+def attend(q, k, v, scale):
+    """Softmax attention of one query over the rows of k and v: (o, lse, sum_j p_j |v_j|), zeros and -inf over none."""
+    if len(k) == 0:
+        return np.zeros(v.shape[-1]), -np.inf, np.zeros(v.shape[-1])
+    s = (_f64(k) @ _f64(q)) * scale
+    m = s.max()
+    p = np.exp(s - m)
+    return p @ _f64(v) / p.sum(), m + np.log(p.sum()), p @ np.abs(_f64(v)) / p.sum()
+
+
+def tree_attention(q, k_cache, v_cache, k_draft, v_draft, parents, length, keeps, block_size, scale, max_len, resident=None):
+    """One head's tree step: q, k_draft, v_draft [T, D], k_cache, v_cache [>= length, D].
+
+    keeps(row, col): whether block row `row` of the mask keeps block `col`.  Node i is the token at position length + depth; it attends the
+    cached tokens and the nodes from the root down to it whose block its row keeps: by definition what decoding the chain token by
+    token gives.  resident(col): whether the cache holds the block (nothing of one that it does not).
+    Returns (o [T, D], lse [T], sum_j p_j |v_j| [T, D]).
+    """
+    T, D = q.shape
+    o, lse, weight = np.zeros((T, D)), np.full(T, -np.inf), np.zeros((T, D))
+    for i, chain in enumerate(tree_chains(parents)):
+        if chain is None or length + len(chain) - 1 >= max_len:
+            continue
+        row = (length + len(chain) - 1) // block_size
+        cached = [t for t in range(length) if keeps(row, t // block_size) and (resident is None or resident(t // block_size))]
+        nodes = [j for d, j in enumerate(chain) if keeps(row, (length + d) // block_size)]
+        k = np.concatenate([_f64(k_cache)[cached], _f64(k_draft)[nodes]])
+        v = np.concatenate([_f64(v_cache)[cached], _f64(v_draft)[nodes]])
+        o[i], lse[i], weight[i] = attend(q[i], k, v, scale)
+    return o, lse, weight

@@ -83,12 +83,44 @@ class PagedDecodeArgs(C.Structure):
                 ("page_stride", C.c_int64), ("tok_stride", C.c_int64)]
 
 
+class PagedCacheStruct(C.Structure):
+    _fields_ = [("k_pages", C.c_void_p), ("v_pages", C.c_void_p), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p),
+                ("block_table", C.c_void_p), ("format", C.c_int32), ("nseq", C.c_int32), ("heads", C.c_int32), ("head_dim", C.c_int32),
+                ("block_size", C.c_int32), ("max_blocks", C.c_int32), ("num_pages", C.c_int32),
+                ("page_stride", C.c_int64), ("tok_stride", C.c_int64), ("scale_page_stride", C.c_int64), ("scale_tok_stride", C.c_int64)]
+
+
+class KvAppendArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cu_new", C.c_void_p), ("start", C.c_void_p), ("rows", C.c_void_p),
+                ("skipped", C.c_void_p), ("num_rows", C.c_int32), ("num_items", C.c_int32), ("max_new", C.c_int32),
+                ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class KvReadArgs(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("cu_rows", C.c_void_p), ("start", C.c_void_p), ("num_rows", C.c_int32),
+                ("max_rows", C.c_int32), ("stride_row", C.c_int64), ("stride_head", C.c_int64)]
+
+
+class CacheDecodeArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("seq_lens", C.c_void_p), ("o", C.c_void_p), ("lse", C.c_void_p), ("missing", C.c_void_p),
+                ("num_splits", C.c_int32), ("q_stride_seq", C.c_int64), ("q_stride_head", C.c_int64)]
+
+
+class TreeArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("parents", C.c_void_p), ("seq_lens", C.c_void_p), ("o", C.c_void_p),
+                ("lse", C.c_void_p), ("missing", C.c_void_p), ("nodes", C.c_int32), ("num_splits", C.c_int32),
+                ("q_stride_seq", C.c_int64), ("q_stride_head", C.c_int64), ("q_stride_node", C.c_int64),
+                ("kv_stride_seq", C.c_int64), ("kv_stride_head", C.c_int64), ("kv_stride_node", C.c_int64)]
+
+
 EXPORTS = (
     "s2_layout_build", "s2_layout_from_csr", "s2_layout_destroy", "s2_layout_get", "s2_layout_get_tiles", "s2_layout_get_ds_units", "s2_attn_fwd", "s2_attn_fwd_rows", "s2_attn_fwd_varlen", "s2_attn_bwd_varlen",
     "s2_attn_bwd_varlen_workspace_bytes", "s2_attn_bwd",
     "s2_attn_bwd_workspace_bytes", "s2_attn_bwd_layout_workspace_bytes", "s2_attn_bwd_stages", "s2_dense_causal_fwd", "s2_dense_causal_bwd", "s2_dense_causal_bwd_workspace_bytes", "s2_attn_decode",
     "s2_attn_decode_workspace_bytes", "s2_attn_decode_default_splits", "s2_attn_decode_static", "s2_attn_decode_paged",
     "s2_kv_resident_blocks", "s2_attn_decode_layout", "s2_attn_decode_paged_layout",
+    "s2_kv_append_paged", "s2_kv_read_paged", "s2_attn_decode_paged_cache", "s2_attn_decode_paged_cache_layout", "s2_attn_tree_paged",
+    "s2_attn_tree_paged_layout", "s2_attn_tree_workspace_bytes",
     "s2_layout_resident_blocks", "s2_probe_scratch_bytes", "s2_probe_mfma", "s2_probe_read", "s2_probe_atomic_add", "s2_status_string",
     "s2_last_hip_error", "s2_version",
 )
@@ -97,6 +129,9 @@ EXPORTS = (
 _MARSHALLED = ("s2_attn_fwd", "s2_attn_fwd_rows", "s2_attn_fwd_varlen", "s2_attn_bwd_stages", "s2_attn_bwd_varlen", "s2_dense_causal_fwd",
                "s2_dense_causal_bwd", "s2_attn_decode", "s2_attn_decode_static", "s2_attn_decode_layout", "s2_attn_decode_paged",
                "s2_attn_decode_paged_layout")
+# the same for those over a cache of any format (bind_cache())
+_CACHE_CALLS = ("s2_kv_append_paged", "s2_kv_read_paged", "s2_attn_decode_paged_cache", "s2_attn_decode_paged_cache_layout", "s2_attn_tree_paged",
+                "s2_attn_tree_paged_layout")
 
 _lib = None
 _calls = None
@@ -111,9 +146,10 @@ def _marshal():
             from . import _marshal as calls
         except ImportError as e:
             raise ImportError("_marshal.so is not built: run `python -m paper_2407_17678_amd.build`") from e
-        if getattr(calls, "entry_points", None) != _MARSHALLED:
+        if getattr(calls, "entry_points", None) != _MARSHALLED or getattr(calls, "cache_entry_points", None) != _CACHE_CALLS:
             raise ImportError("_marshal.so is built from other sources: run `python -m paper_2407_17678_amd.build`")
         calls.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in _MARSHALLED))
+        calls.bind_cache(*(C.cast(getattr(L, name), C.c_void_p).value for name in _CACHE_CALLS))
         _calls = calls
     return _calls
 
@@ -169,6 +205,13 @@ def lib():
                                               C.c_void_p, C.c_size_t, C.c_void_p]
     L.s2_layout_resident_blocks.argtypes = [C.c_void_p, C.c_int32, C.c_int32,
                                             C.POINTER(C.c_int32), C.c_int32, C.POINTER(C.c_int32)]
+    L.s2_kv_append_paged.argtypes = [C.POINTER(PagedCacheStruct), C.POINTER(KvAppendArgs), C.c_void_p]
+    L.s2_kv_read_paged.argtypes = [C.POINTER(PagedCacheStruct), C.POINTER(KvReadArgs), C.c_void_p]
+    for pattern, suffix in ((C.POINTER(LayoutParams), ""), (C.c_void_p, "_layout")):
+        for name, args in (("s2_attn_decode_paged_cache", CacheDecodeArgs), ("s2_attn_tree_paged", TreeArgs)):
+            getattr(L, name + suffix).argtypes = [pattern, C.POINTER(PagedCacheStruct), C.POINTER(args), C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+    L.s2_attn_tree_workspace_bytes.argtypes = [C.c_int32] * 6
+    L.s2_attn_tree_workspace_bytes.restype = C.c_size_t
     L.s2_probe_scratch_bytes.restype = C.c_size_t
     L.s2_probe_mfma.argtypes = [C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.POINTER(C.c_double)]
     L.s2_probe_read.argtypes = [C.c_void_p, C.c_size_t, C.c_void_p, C.c_void_p]
@@ -418,6 +461,63 @@ def s2_attn_decode_paged_layout(layout, q, k_pages, v_pages, block_table, seq_le
     """s2_attn_decode_paged following the rows of a Layout (any pattern) instead of the closed form."""
     _check(_marshal().decode_paged_layout(layout.handle, q, k_pages, v_pages, block_table, seq_lens, o, lse, scale, workspace, missing,
                                           num_splits, _stream(stream)), "s2_attn_decode_paged_layout")
+
+
+KV_BF16, KV_MXFP8, KV_MXFP4 = 0, 1, 2
+
+
+class PagedCache:
+    """A paged cache as the calls below take it: an s2_paged_cache, and the tensors it points into."""
+    __slots__ = ("raw", "tensors")
+
+    def __init__(self, raw, tensors):
+        self.raw, self.tensors = raw, tensors
+
+
+def paged_cache(fmt, block_size, k_pages, v_pages, block_table, k_scales=None, v_scales=None):
+    """k_pages, v_pages: [num_pages, block_size, D] bf16 (KV_BF16) or one-byte elements (KV_MXFP8), or [.., D / 2] one-byte elements (KV_MXFP4);
+    block_table: int32 [nseq, heads, max_blocks]; k_scales, v_scales: one-byte elements [num_pages, block_size, D / 32], None for KV_BF16."""
+    return PagedCache(_marshal().paged_cache(fmt, block_size, k_pages, v_pages, block_table, k_scales, v_scales),
+                      (k_pages, v_pages, block_table, k_scales, v_scales))
+
+
+def s2_kv_append_paged(cache, k, v, cu_new, start, max_new, rows=None, skipped=None, stream=None):
+    """k, v: bf16 [rows, heads, D]; cu_new: device int32 [nseq + 1]; start: [nseq]; rows: int32, the row each item takes (None: its own)."""
+    _check(_marshal().kv_append(cache.raw, k, v, cu_new, start, max_new, rows, skipped, _stream(stream)), "s2_kv_append_paged")
+
+
+def s2_kv_read_paged(cache, k, v, cu_rows, start, max_rows, stream=None):
+    """k, v: bf16 [heads, rows, D], written; cu_rows: device int32 [nseq + 1]; start: [nseq]."""
+    _check(_marshal().kv_read(cache.raw, k, v, cu_rows, start, max_rows, _stream(stream)), "s2_kv_read_paged")
+
+
+def s2_attn_decode_paged_cache(params, cache, q, seq_lens, o, lse, scale, workspace, missing=None, num_splits=0, stream=None):
+    """s2_attn_decode_paged over a cache of any format; q, o: bf16 [nseq, heads, D] of the same strides."""
+    _check(_marshal().decode_cache(_params_ptr(params), cache.raw, q, seq_lens, o, lse, scale, workspace, missing, num_splits, _stream(stream)),
+           "s2_attn_decode_paged_cache")
+
+
+def s2_attn_decode_paged_cache_layout(layout, cache, q, seq_lens, o, lse, scale, workspace, missing=None, num_splits=0, stream=None):
+    """s2_attn_decode_paged_cache following the rows of a Layout (any pattern) instead of the closed form."""
+    _check(_marshal().decode_cache_layout(layout.handle, cache.raw, q, seq_lens, o, lse, scale, workspace, missing, num_splits, _stream(stream)),
+           "s2_attn_decode_paged_cache_layout")
+
+
+def s2_attn_tree_workspace_bytes(nseq, heads, nodes, head_dim, max_len, num_splits=0):
+    return lib().s2_attn_tree_workspace_bytes(nseq, heads, nodes, head_dim, max_len, num_splits)
+
+
+def s2_attn_tree_paged(params, cache, q, k_draft, v_draft, parents, seq_lens, o, lse, scale, workspace, missing=None, num_splits=0, stream=None):
+    """q, o and k_draft, v_draft: bf16 [nseq, heads, nodes, D], each two of the same strides; parents: int32 [nseq, nodes]; lse: [nseq, heads, nodes]."""
+    _check(_marshal().tree(_params_ptr(params), cache.raw, q, k_draft, v_draft, parents, seq_lens, o, lse, scale, workspace, missing, num_splits,
+                           _stream(stream)), "s2_attn_tree_paged")
+
+
+def s2_attn_tree_paged_layout(layout, cache, q, k_draft, v_draft, parents, seq_lens, o, lse, scale, workspace, missing=None, num_splits=0,
+                              stream=None):
+    """s2_attn_tree_paged following the rows of a Layout (any pattern) instead of the closed form."""
+    _check(_marshal().tree_layout(layout.handle, cache.raw, q, k_draft, v_draft, parents, seq_lens, o, lse, scale, workspace, missing, num_splits,
+                                  _stream(stream)), "s2_attn_tree_paged_layout")
 
 
 def s2_kv_resident_blocks(params, head, length):

@@ -658,7 +658,8 @@ int choose_splits(const s2_layout_params* lp, const s2_layout* layout, int nseq,
   return n;
 }
 
-void set_pattern(s2::DecodeParams& p, const s2_layout_params* lp, const s2_layout* layout) {
+extern "C++" template <class PARAMS>
+void set_pattern(PARAMS& p, const s2_layout_params* lp, const s2_layout* layout) {
   p.block_size = lp->block_size;
   p.local_blocks = lp->local_blocks;
   p.stride = lp->stride;
@@ -770,7 +771,239 @@ int decode_paged(const s2_layout_params* lp, const s2_layout* layout, const s2_p
   return hip_ok(s2::launch_decode(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
+// A paged cache of any format, with strides in bytes.
+int check_cache(const s2_paged_cache* c, s2::CacheRef& r) {
+  if (!c->k_pages || !c->v_pages || !c->block_table) return S2_ERR_NULL;
+  if (c->format != S2_KV_BF16 && c->format != S2_KV_MXFP8 && c->format != S2_KV_MXFP4) return S2_ERR_BAD_PARAM;
+  if (!good_block_size(c->block_size)) return S2_ERR_BAD_PARAM;
+  if (c->format != S2_KV_BF16 && (!c->k_scales || !c->v_scales)) return S2_ERR_NULL;
+  if (c->nseq < 1 || c->heads < 1 || c->max_blocks < 1 || c->num_pages < 1) return S2_ERR_SHAPE;
+  if (c->head_dim != 64 && c->head_dim != 128) return S2_ERR_SHAPE;
+  if ((int64_t)c->nseq * c->heads > std::numeric_limits<int32_t>::max() / 64) return S2_ERR_SHAPE;
+  // (positions of a tree's nodes go up to 64 beyond the last)
+  if ((int64_t)c->max_blocks * c->block_size > std::numeric_limits<int32_t>::max() - 64) return S2_ERR_SHAPE;
+  const int64_t element = c->format == S2_KV_BF16 ? 2 : 1;
+  const int64_t row = c->format == S2_KV_BF16 ? 2 * c->head_dim : c->format == S2_KV_MXFP8 ? c->head_dim : c->head_dim / 2;
+  if (!aligned16(c->k_pages) || !aligned16(c->v_pages) || (reinterpret_cast<uintptr_t>(c->block_table) & 3u) != 0) return S2_ERR_ALIGN;
+  if (c->page_stride < 0 || c->page_stride % (16 / element) != 0 || c->tok_stride < 0 || c->tok_stride % (16 / element) != 0) return S2_ERR_ALIGN;
+  if (c->tok_stride * element < row) return S2_ERR_ALIGN;
+  // the kernels address a page's rows with 32-bit byte offsets
+  constexpr int64_t kPage = (int64_t)1 << 30;
+  if (c->tok_stride > kPage / element / c->block_size || c->page_stride > ((int64_t)1 << 56)) return S2_ERR_SHAPE;
+  r = s2::CacheRef{};
+  if (c->format != S2_KV_BF16) {
+    const int64_t scales = c->head_dim / 32;
+    if ((reinterpret_cast<uintptr_t>(c->k_scales) & 3u) != 0 || (reinterpret_cast<uintptr_t>(c->v_scales) & 3u) != 0) return S2_ERR_ALIGN;
+    if (c->scale_page_stride < 0 || c->scale_page_stride % scales != 0 || c->scale_tok_stride < scales || c->scale_tok_stride % scales != 0)
+      return S2_ERR_ALIGN;
+    if (c->scale_tok_stride > kPage / c->block_size || c->scale_page_stride > ((int64_t)1 << 56)) return S2_ERR_SHAPE;
+    r.ks = static_cast<uint8_t*>(c->k_scales);
+    r.vs = static_cast<uint8_t*>(c->v_scales);
+    r.scale_page = c->scale_page_stride;
+    r.scale_tok = (int)c->scale_tok_stride;
+  }
+  r.k = static_cast<uint8_t*>(c->k_pages);
+  r.v = static_cast<uint8_t*>(c->v_pages);
+  r.table = c->block_table;
+  r.page = c->page_stride * element;
+  r.tok = (int)(c->tok_stride * element);
+  r.format = c->format;
+  r.heads = c->heads;
+  r.head_dim = c->head_dim;
+  r.max_blocks = c->max_blocks;
+  r.num_pages = c->num_pages;
+  r.block_shift = 31 - __builtin_clz((unsigned)c->block_size);
+  return S2_OK;
+}
+
+// What s2_kv_append_paged and s2_kv_read_paged have in common, and the launch.
+int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, const void* v, void* stream) {
+  if (!p.cu || !p.start) return S2_ERR_NULL;
+  if (p.num_rows < 0 || p.max_rows < 0) return S2_ERR_SHAPE;
+  if (p.num_rows > 0 && (!k || !v)) return S2_ERR_NULL;
+  if (!aligned16(k) || !aligned16(v) || (reinterpret_cast<uintptr_t>(p.cu) & 3u) != 0 || (reinterpret_cast<uintptr_t>(p.start) & 3u) != 0)
+    return S2_ERR_ALIGN;
+  if (p.stride_row < 0 || (p.stride_row & 7) != 0 || p.stride_head < 0 || (p.stride_head & 7) != 0) return S2_ERR_ALIGN;
+  if (p.stride_row > (int64_t)1 << 40 || p.stride_head > (int64_t)1 << 40) return S2_ERR_SHAPE;
+  if (p.max_rows == 0) return S2_OK;
+  const int64_t grid = s2::kv_rows_tiles(p, c->nseq);
+  if (grid > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  return hip_ok(s2::launch_kv_rows(p, (int)grid, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+// The splits of a call over a cache when the caller leaves them to the library: about two workgroups to a compute unit, and a
+// unit of 64 tokens at least to each of a workgroup's wavefronts.
+int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, int nseq, int heads, int max_len) {
+  const int S = lp->block_size;
+  const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / S, nullptr, 0);
+  const int64_t units = (blocks * S + 63) / 64, pairs = (int64_t)nseq * heads;
+  const int64_t want = std::min<int64_t>((512 + pairs - 1) / pairs, units / 4);
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, s2_attn_decode_default_splits(nseq, heads, max_len)));
+}
+
+int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, s2::CacheAttnParams& p, float scale,
+                 int num_splits, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!p.q || !p.seq_lens || !p.o) return S2_ERR_NULL;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return S2_ERR_BAD_PARAM;
+  int st = check_cache(c, p.c);
+  if (st != S2_OK) return st;
+  if (lp->block_size != c->block_size) return S2_ERR_SHAPE;
+  const int max_len = c->max_blocks * c->block_size;
+  st = check_pattern(lp, layout, c->heads, max_len);
+  if (st != S2_OK) return st;
+  if (num_splits < 0 || num_splits > 64) return S2_ERR_BAD_PARAM;
+  for (int64_t s : {p.q_ss, p.q_sh, p.q_sn, p.kv_ss, p.kv_sh, p.kv_sn}) {
+    if (s < 0 || (s & 7) != 0) return S2_ERR_ALIGN;
+    if (s > (int64_t)1 << 40) return S2_ERR_SHAPE;
+  }
+  if (!aligned16(p.q) || !aligned16(p.k_draft) || !aligned16(p.v_draft) || !aligned16(p.o) || (reinterpret_cast<uintptr_t>(p.seq_lens) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(p.parents) & 3u) != 0 || (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0 ||
+      (reinterpret_cast<uintptr_t>(p.missing) & 3u) != 0)
+    return S2_ERR_ALIGN;
+  const int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, c->nseq, c->heads, max_len);
+  if ((int64_t)c->nseq * c->heads * splits > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  const size_t need = s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, splits);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < need) return S2_ERR_WORKSPACE;
+  p.part_acc = static_cast<float*>(workspace);
+  p.part_ml = p.part_acc + (size_t)c->nseq * c->heads * p.nodes * splits * c->head_dim;
+  p.nseq = c->nseq;
+  p.heads = c->heads;
+  p.max_len = max_len;
+  p.num_splits = splits;
+  p.scale = scale;
+  p.scale_log2e = scale * 1.4426950408889634f;
+  set_pattern(p, lp, layout);
+  return hip_ok(s2::launch_cache_attn(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+int decode_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
+                 void* workspace, size_t workspace_bytes, void* stream) {
+  if (c->format == S2_KV_BF16 && (c->heads == 1 || a->q_stride_head == c->head_dim) &&
+      (c->nseq == 1 || a->q_stride_seq == (int64_t)c->heads * c->head_dim)) {
+    if (c->block_size != lp->block_size) return S2_ERR_SHAPE;
+    s2_paged_decode_args d{};
+    d.q = a->q;
+    d.k_pages = c->k_pages;
+    d.v_pages = c->v_pages;
+    d.block_table = c->block_table;
+    d.seq_lens = a->seq_lens;
+    d.o = a->o;
+    d.lse = a->lse;
+    d.missing = a->missing;
+    d.nseq = c->nseq;
+    d.heads = c->heads;
+    d.head_dim = c->head_dim;
+    d.max_blocks = c->max_blocks;
+    d.num_pages = c->num_pages;
+    d.num_splits = a->num_splits;
+    d.page_stride = c->page_stride;
+    d.tok_stride = c->tok_stride;
+    return decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+  }
+  s2::CacheAttnParams p{};
+  p.q = static_cast<const uint16_t*>(a->q);
+  p.seq_lens = a->seq_lens;
+  p.o = static_cast<uint16_t*>(a->o);
+  p.lse = a->lse;
+  p.missing = a->missing;
+  p.nodes = 1;
+  p.q_ss = a->q_stride_seq;
+  p.q_sh = a->q_stride_head;
+  return attend_cache(lp, layout, c, p, scale, a->num_splits, workspace, workspace_bytes, stream);
+}
+
+int tree_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, const s2_tree_args* a, float scale,
+               void* workspace, size_t workspace_bytes, void* stream) {
+  if (!a->k || !a->v || !a->parents) return S2_ERR_NULL;
+  if (a->nodes < 1 || a->nodes > 64) return S2_ERR_SHAPE;
+  s2::CacheAttnParams p{};
+  p.q = static_cast<const uint16_t*>(a->q);
+  p.k_draft = static_cast<const uint16_t*>(a->k);
+  p.v_draft = static_cast<const uint16_t*>(a->v);
+  p.parents = a->parents;
+  p.seq_lens = a->seq_lens;
+  p.o = static_cast<uint16_t*>(a->o);
+  p.lse = a->lse;
+  p.missing = a->missing;
+  p.nodes = a->nodes;
+  p.q_ss = a->q_stride_seq;
+  p.q_sh = a->q_stride_head;
+  p.q_sn = a->q_stride_node;
+  p.kv_ss = a->kv_stride_seq;
+  p.kv_sh = a->kv_stride_head;
+  p.kv_sn = a->kv_stride_node;
+  return attend_cache(lp, layout, c, p, scale, a->num_splits, workspace, workspace_bytes, stream);
+}
+
 }  // namespace
+
+int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void* stream) {
+  if (!c || !a) return S2_ERR_NULL;
+  s2::KvRowsParams p{};
+  const int st = check_cache(c, p.c);
+  if (st != S2_OK) return st;
+  if ((reinterpret_cast<uintptr_t>(a->rows) & 3u) != 0 || (reinterpret_cast<uintptr_t>(a->skipped) & 3u) != 0) return S2_ERR_ALIGN;
+  if (a->rows && a->num_items < 0) return S2_ERR_SHAPE;
+  p.k = static_cast<const uint16_t*>(a->k);
+  p.v = static_cast<const uint16_t*>(a->v);
+  p.cu = a->cu_new;
+  p.start = a->start;
+  p.rows = a->rows;
+  p.skipped = a->skipped;
+  p.num_rows = a->num_rows;
+  p.num_items = a->num_items;
+  p.max_rows = a->max_new;
+  p.stride_row = a->stride_row;
+  p.stride_head = a->stride_head;
+  return cache_rows(p, c, a->k, a->v, stream);
+}
+
+int s2_kv_read_paged(const s2_paged_cache* c, const s2_kv_read_args* a, void* stream) {
+  if (!c || !a) return S2_ERR_NULL;
+  s2::KvRowsParams p{};
+  const int st = check_cache(c, p.c);
+  if (st != S2_OK) return st;
+  p.k_out = static_cast<uint16_t*>(a->k);
+  p.v_out = static_cast<uint16_t*>(a->v);
+  p.cu = a->cu_rows;
+  p.start = a->start;
+  p.num_rows = a->num_rows;
+  p.max_rows = a->num_rows > 0 ? a->max_rows : std::min(a->max_rows, 0);  // (without rows there is no output to tell the two launches apart by)
+  p.stride_row = a->stride_row;
+  p.stride_head = a->stride_head;
+  return cache_rows(p, c, a->k, a->v, stream);
+}
+
+int s2_attn_decode_paged_cache(const s2_layout_params* lp, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
+                               void* workspace, size_t workspace_bytes, void* stream) {
+  if (!lp || !c || !a) return S2_ERR_NULL;
+  return decode_cache(lp, nullptr, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+int s2_attn_decode_paged_cache_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
+                                      void* workspace, size_t workspace_bytes, void* stream) {
+  if (!layout || !c || !a) return S2_ERR_NULL;
+  return decode_cache(&layout->p, layout, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+int s2_attn_tree_paged(const s2_layout_params* lp, const s2_paged_cache* c, const s2_tree_args* a, float scale, void* workspace,
+                       size_t workspace_bytes, void* stream) {
+  if (!lp || !c || !a) return S2_ERR_NULL;
+  return tree_cache(lp, nullptr, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+int s2_attn_tree_paged_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_tree_args* a, float scale, void* workspace,
+                              size_t workspace_bytes, void* stream) {
+  if (!layout || !c || !a) return S2_ERR_NULL;
+  return tree_cache(&layout->p, layout, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, int32_t head_dim, int32_t max_len, int32_t num_splits) {
+  if (nseq < 1 || heads < 1 || nodes < 1 || head_dim < 1) return 0;
+  if (num_splits <= 0) num_splits = s2_attn_decode_default_splits(nseq, heads, max_len);
+  const size_t items = (size_t)nseq * heads * nodes * num_splits;
+  return ((items * (head_dim + 2) * sizeof(float) + 255) / 256) * 256;
+}
 
 int s2_attn_decode(const s2_layout_params* lp, const s2_decode_args* a, float scale, void* workspace,
                    size_t workspace_bytes, void* stream) {

@@ -28,6 +28,7 @@
 #include "config.h"
 #include "device_util.h"
 #include "kernels.h"
+#include "row_blocks.h"
 #include "sched_util.h"
 
 namespace s2 {
@@ -38,50 +39,6 @@ constexpr float kNegInf = -__builtin_inff();
 
 // From this token stride (in elements) on, the offsets of a unit's 64 rows do not fit into the 31 bits of a buffer's size.
 constexpr int64_t kFarRows = (int64_t)1 << 24;
-
-// Kept blocks of block row i, in ascending order, as (stripe run, local run), or as a list.
-struct RowBlocks {
-  int first_stripe, n_stripe, stride, local_lo, count;
-  const int32_t* cols;  // caller-supplied pattern: the row's list; nullptr = closed form
-  __device__ int block(int n) const {
-    const int striped = first_stripe + n * stride, local = local_lo + (n - n_stripe);
-    if (cols) return load_const<int32_t>(cols + n);
-    return n < n_stripe ? striped : local;
-  }
-};
-
-__device__ inline RowBlocks row_blocks(const DecodeParams& p, int head, int i) {
-  RowBlocks r;
-  r.stride = p.stride;
-  r.first_stripe = 0;
-  r.n_stripe = 0;
-  r.cols = nullptr;
-  r.local_lo = 0;
-  if (p.row_ptr) {
-    const int32_t lo = load_const<int32_t>(p.row_ptr + (int64_t)head * p.num_blocks + i);
-    r.cols = p.col_idx + lo;
-    r.count = load_const<int32_t>(p.row_ptr + (int64_t)head * p.num_blocks + i + 1) - lo;
-    return r;
-  }
-  if (p.dense) {
-    r.local_lo = 0;
-    r.count = i + 1;
-    return r;
-  }
-  r.local_lo = max(0, i - p.local_blocks + 1);
-  if (p.stride > 0) {
-    const int o = p.head_index_base + head - (p.head_index_base + head) / p.by_stride * p.stride;
-    const int lo = p.window_blocks > 0 ? max(0, i - p.window_blocks + 1) : 0;
-    int first = o;
-    if (lo > o) first = o + (lo - o + p.stride - 1) / p.by_stride * p.stride;
-    if (first < r.local_lo) {
-      r.first_stripe = first;
-      r.n_stripe = (r.local_lo - 1 - first) / p.by_stride + 1;
-    }
-  }
-  r.count = r.n_stripe + (i - r.local_lo + 1);
-  return r;
-}
 
 // GATHER: the instantiation for 16-token blocks, where a unit of work is four consecutive kept blocks
 // of the row's list side by side, so that every load still fetches rows the query attends (a 16-token

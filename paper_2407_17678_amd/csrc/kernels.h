@@ -123,6 +123,61 @@ struct DecodeParams {
   FastDiv by_heads, by_splits, by_stride;  // set by launch_decode
 };
 
+// A paged cache of any format (s2_paged_cache): strides in bytes.
+struct CacheRef {
+  uint8_t* k;
+  uint8_t* v;
+  uint8_t* ks;
+  uint8_t* vs;
+  const int32_t* table;
+  int64_t page, scale_page;
+  int tok, scale_tok;
+  int format, heads, head_dim, max_blocks, num_pages, block_shift;
+};
+
+// Rows written into a cache (k_out == nullptr) or read from it.
+struct KvRowsParams {
+  CacheRef c;
+  const uint16_t* k;
+  const uint16_t* v;
+  uint16_t* k_out;
+  uint16_t* v_out;
+  const int32_t* cu;     // [nseq + 1]
+  const int32_t* start;  // [nseq]
+  const int32_t* rows;   // rows that the items take, nullptr = their own
+  int32_t* skipped;
+  int num_rows, num_items, max_rows;
+  int64_t stride_row, stride_head;
+  // set by kv_rows_tiles: a workgroup takes tile_rows rows of tile_heads heads
+  int tile_rows, tile_heads, row_tiles, by_heads_groups;
+  FastDiv div_groups, div_tiles;
+};
+
+// Attention over such a cache: a decode step (parents == nullptr) or a tree of drafted tokens to a sequence.
+struct CacheAttnParams {
+  CacheRef c;
+  const uint16_t* q;
+  const uint16_t* k_draft;
+  const uint16_t* v_draft;
+  const int32_t* parents;  // [nseq, nodes]
+  const int32_t* seq_lens;
+  uint16_t* o;
+  float* lse;       // [nseq, heads, nodes]
+  float* part_acc;  // [nseq * heads * nodes][split][head_dim]
+  float* part_ml;   // [nseq * heads * nodes][split][2]  (max, sum)
+  int32_t* missing;
+  int nseq, heads, nodes, max_len, num_splits;
+  int64_t q_ss, q_sh, q_sn;
+  int64_t kv_ss, kv_sh, kv_sn;
+  float scale, scale_log2e;
+  // the pattern, as in DecodeParams
+  int block_size, local_blocks, stride, window_blocks, dense, head_index_base;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  int num_blocks;
+  FastDiv by_heads, by_splits, by_stride;  // set by launch_cache_attn
+};
+
 // Each returns the hipError_t of the launch (hipGetLastError after the launch).
 hipError_t launch_fwd(const AttnParams& p, bool dense, hipStream_t stream);
 // The launch of it for mask blocks of 16 and 32 tokens (row_map set).
@@ -149,5 +204,9 @@ constexpr int decode_wide_groups(int block_size, int head_dim) {
   return block_size == 16 && head_dim == 64 ? 2 * kDecodeWideGroups : kDecodeWideGroups;
 }
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
+// The workgroups of a launch over rows of a cache (sets the tile fields), and the launch.
+int64_t kv_rows_tiles(KvRowsParams& p, int nseq);
+hipError_t launch_kv_rows(const KvRowsParams& p, int grid, hipStream_t stream);
+hipError_t launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);
 
 }  // namespace s2

@@ -1,0 +1,178 @@
+// Rows written into a paged cache, quantised on the way, and read back (section 4.1's cache in bf16, 8 or 4 bits).
+//
+// One power of two to 32 features of a row: with a the largest magnitude, 2^e is the smallest for which a * 2^-e rounds into the code's
+// range (below 464 in e4m3, 7 in e2m1).  bf16 magnitudes order as their bit patterns do, so a is an integer maximum over
+// four lanes of eight features, and e the exponent field of a + (what carries a mantissa of 1.8125 or 1.75 into the next exponent).
+// Scaling by a power of two is exact: the one rounding is that of the conversion instruction, and what is read back is exact in bf16.
+//
+// Both move bytes and nothing else; D/8 lanes take a row, 16 bytes of bf16 each.
+#include <hip/hip_runtime.h>
+
+#include "kernels.h"
+#include "kv_cache.h"
+
+namespace s2 {
+
+namespace {
+
+// Where the kv_rows grid's workgroup begins: rows [row, row + p.tile_rows) of the sequence's new ones, for p.tile_heads heads from `head`.
+struct Slot {
+  int b, row, head;
+};
+__device__ __forceinline__ Slot slot_of(const KvRowsParams& p, int wg) {
+  Slot s;
+  const int groups = p.by_heads_groups;  // workgroups side by side take heads of the same rows
+  const int t = wg / p.div_groups;
+  s.head = (wg - t * groups) * p.tile_heads;
+  s.b = t / p.div_tiles;
+  s.row = (t - s.b * p.row_tiles) * p.tile_rows;
+  return s;
+}
+
+template <int D, int FMT>
+__global__ __launch_bounds__(256) void kv_append_kernel(const KvRowsParams p) {
+  constexpr int LPR = D / 8, RPI = 256 / LPR;  // lanes to a row, rows to a pass of the workgroup
+  const Slot s = slot_of(p, blockIdx.x);
+  const int tid = threadIdx.x, c = tid % LPR, first = tid / LPR;
+  const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
+  const int start = load_const<int32_t>(p.start + s.b);
+  int left_out = 0;
+  for (int i = first; i < p.tile_rows * p.tile_heads; i += RPI) {
+    const int head = s.head + i / p.tile_rows, item = s.row + i % p.tile_rows;
+    if (item >= n || head >= p.c.heads) continue;
+    const int64_t pos = (int64_t)start + item;
+    int row = lo + item;
+    if (p.rows) row = row >= 0 && row < p.num_items ? p.rows[row] : -1;
+    const int64_t blk = pos >> p.c.block_shift;
+    int page = -1;
+    if (pos >= 0 && blk < p.c.max_blocks && row >= 0 && row < p.num_rows) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
+    if (page < 0 || page >= p.c.num_pages) {
+      left_out += c == 0;
+      continue;
+    }
+    const int in_page = (int)(pos & ((1 << p.c.block_shift) - 1));
+    const int64_t from = row * p.stride_row + head * p.stride_head + 8 * c;
+    const int64_t to = page * p.c.page + (int64_t)in_page * p.c.tok;
+    const int64_t scale_to = page * p.c.scale_page + (int64_t)in_page * p.c.scale_tok;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const u32x4 x = *reinterpret_cast<const u32x4*>((kv ? p.v : p.k) + from);
+      uint8_t* const pool = (kv ? p.c.v : p.c.k) + to;
+      if constexpr (FMT == S2_KV_BF16) {
+        *reinterpret_cast<u32x4*>(pool + 16 * c) = x;
+      } else {
+        uint32_t a = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) a = max(a, max(x[e] & 0x7fffu, (x[e] >> 16) & 0x7fffu));
+        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xf, 0xf, true));  // (quads of lanes: 1032, 2301)
+        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xf, 0xf, true));
+        constexpr int kCarry = FMT == S2_KV_MXFP8 ? 24 : 32, kTop = FMT == S2_KV_MXFP8 ? 8 : 2;
+        const bool held = a < 0x7f00u;
+        const uint32_t byte = held ? (uint32_t)max((int)((a + kCarry) >> 7) - kTop, 17) : 255u;
+        const float scale = scale_of(held ? byte : 127u);
+        if constexpr (FMT == S2_KV_MXFP8) {
+          u32x2 w;
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            s16x2_ r = {0, 0};
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e]), scale, false);
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e + 1]), scale, true);
+            w[e] = held ? __builtin_bit_cast(uint32_t, r) : 0u;
+          }
+          *reinterpret_cast<u32x2*>(pool + 8 * c) = w;
+        } else {
+          uint32_t w = 0;
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[0]), scale, 0);
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[1]), scale, 1);
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[2]), scale, 2);
+          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[3]), scale, 3);
+          *reinterpret_cast<uint32_t*>(pool + 4 * c) = held ? w : 0u;
+        }
+        if (c % 4 == 0) (kv ? p.c.vs : p.c.ks)[scale_to + c / 4] = (uint8_t)byte;
+      }
+    }
+  }
+  if (p.skipped && left_out > 0) atomicAdd(p.skipped, left_out);
+}
+
+template <int D, int FMT>
+__global__ __launch_bounds__(256) void kv_read_kernel(const KvRowsParams p) {
+  constexpr int LPR = D / 8, RPI = 256 / LPR;
+  const Slot s = slot_of(p, blockIdx.x);
+  const int tid = threadIdx.x, c = tid % LPR, first = tid / LPR;
+  const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
+  const int start = load_const<int32_t>(p.start + s.b);
+  for (int i = first; i < p.tile_rows * p.tile_heads; i += RPI) {
+    const int head = s.head + i / p.tile_rows, item = s.row + i % p.tile_rows;
+    if (item >= n || head >= p.c.heads) continue;
+    const int row = lo + item;
+    if (row < 0 || row >= p.num_rows) continue;
+    const int64_t pos = (int64_t)start + item, blk = pos >> p.c.block_shift;
+    int page = -1;
+    if (pos >= 0 && blk < p.c.max_blocks) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
+    const bool held = page >= 0 && page < p.c.num_pages;
+    const int in_page = (int)(pos & ((1 << p.c.block_shift) - 1));
+    const int64_t from = page * p.c.page + (int64_t)in_page * p.c.tok;
+    const int64_t scale_from = page * p.c.scale_page + (int64_t)in_page * p.c.scale_tok + c / 4;
+    const int64_t to = row * p.stride_row + head * p.stride_head + 8 * c;
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      const uint8_t* const pool = (kv ? p.c.v : p.c.k) + from;
+      u32x4 x = {};
+      if (held) {
+        if constexpr (FMT == S2_KV_BF16) {
+          x = *reinterpret_cast<const u32x4*>(pool + 16 * c);
+        } else {
+          const float scale = scale_of((kv ? p.c.vs : p.c.ks)[scale_from]);
+          if constexpr (FMT == S2_KV_MXFP8) {
+            const u32x2 w = *reinterpret_cast<const u32x2*>(pool + 8 * c);
+            uint32_t lo2[2], hi2[2];
+            values8(w[0], scale, lo2);
+            values8(w[1], scale, hi2);
+            x = u32x4{lo2[0], lo2[1], hi2[0], hi2[1]};
+          } else {
+            x = values4(*reinterpret_cast<const uint32_t*>(pool + 4 * c), scale);
+          }
+        }
+      }
+      *reinterpret_cast<u32x4*>((kv ? p.v_out : p.k_out) + to) = x;
+    }
+  }
+}
+
+template <int D, int FMT>
+hipError_t launch_rows(const KvRowsParams& p, int grid, hipStream_t stream) {
+  if (p.k_out)
+    hipLaunchKernelGGL((kv_read_kernel<D, FMT>), dim3(grid), dim3(256), 0, stream, p);
+  else
+    hipLaunchKernelGGL((kv_append_kernel<D, FMT>), dim3(grid), dim3(256), 0, stream, p);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_format(const KvRowsParams& p, int grid, hipStream_t stream) {
+  switch (p.c.format) {
+    case S2_KV_BF16: return launch_rows<D, S2_KV_BF16>(p, grid, stream);
+    case S2_KV_MXFP8: return launch_rows<D, S2_KV_MXFP8>(p, grid, stream);
+    default: return launch_rows<D, S2_KV_MXFP4>(p, grid, stream);
+  }
+}
+
+}  // namespace
+
+int64_t kv_rows_tiles(KvRowsParams& p, int nseq) {
+  p.tile_rows = 1;
+  while (p.tile_rows < 16 && p.tile_rows < p.max_rows) p.tile_rows *= 2;
+  p.tile_heads = 16 / p.tile_rows;
+  p.row_tiles = (int)(((int64_t)p.max_rows + p.tile_rows - 1) / p.tile_rows);
+  p.by_heads_groups = (p.c.heads + p.tile_heads - 1) / p.tile_heads;
+  p.div_groups = fast_div(p.by_heads_groups);
+  p.div_tiles = fast_div(p.row_tiles);
+  return (int64_t)nseq * p.row_tiles * p.by_heads_groups;
+}
+
+hipError_t launch_kv_rows(const KvRowsParams& p, int grid, hipStream_t stream) {
+  return p.c.head_dim == 128 ? launch_format<128>(p, grid, stream) : launch_format<64>(p, grid, stream);
+}
+
+}  // namespace s2

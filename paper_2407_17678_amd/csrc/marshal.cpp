@@ -32,6 +32,21 @@ union {
 } api;
 constexpr Py_ssize_t kEntryPoints = sizeof(Api) / sizeof(void*);
 
+// The entry points of the cache in several formats, in the order bind_cache() is given their addresses (_CACHE_CALLS in binding.py).
+#define S2_CACHE_ENTRY_POINTS(X) \
+  X(s2_kv_append_paged, append) X(s2_kv_read_paged, read) X(s2_attn_decode_paged_cache, decode) X(s2_attn_decode_paged_cache_layout, decode_layout) \
+  X(s2_attn_tree_paged, tree) X(s2_attn_tree_paged_layout, tree_layout)
+struct CacheApi {
+#define X(entry, name) decltype(&entry) name;
+  S2_CACHE_ENTRY_POINTS(X)
+#undef X
+};
+union {
+  CacheApi f;
+  void* at[sizeof(CacheApi) / sizeof(void*)];
+} cache_api;
+constexpr Py_ssize_t kCacheEntryPoints = sizeof(CacheApi) / sizeof(void*);
+
 struct Names {
   PyObject *data_ptr, *stride, *shape, *is_contiguous, *numel, *element_size, *value;
 } names;
@@ -370,25 +385,244 @@ PyObject* paged(PyObject* const* a, Py_ssize_t n) {
 PyObject* decode_paged(PyObject*, PyObject* const* a, Py_ssize_t n) { return paged<false>(a, n); }
 PyObject* decode_paged_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return paged<true>(a, n); }
 
-PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) {
-  if (!count_is(n, kEntryPoints)) return nullptr;
-  void* at[kEntryPoints];
-  for (Py_ssize_t i = 0; i < n; ++i) {
-    at[i] = PyLong_AsVoidPtr(a[i]);
-    if (!at[i]) {
+// ------------------------------------------------------------------------------------ a cache of any format
+
+// a tensor of n sizes whose elements are `bytes` long
+bool sizes_and_element(PyObject* t, int n, int64_t bytes, int64_t* out) {
+  if (!sizes_of(t, n, out)) return false;
+  const Ref e(PyObject_CallMethodNoArgs(t, names.element_size));
+  int64_t have;
+  if (!e.o || !as_i64(e.o, have)) return false;
+  return have == bytes || fail_assert();
+}
+// int32 values side by side, `count` of them; None if it may be
+bool ints_of(PyObject* t, int64_t count, const int32_t*& at) {
+  const Ref n(PyObject_CallMethodNoArgs(t, names.numel)), e(n.o ? PyObject_CallMethodNoArgs(t, names.element_size) : nullptr);
+  int64_t have, size;
+  if (!e.o || !as_i64(n.o, have) || !as_i64(e.o, size)) return false;
+  if (size != 4 || (count >= 0 && have != count)) return fail_assert();
+  return contiguous(t) && data_of(t, at);
+}
+bool counter_of(PyObject* t, int32_t*& at) {
+  at = nullptr;
+  const int32_t* one;
+  if (t == Py_None) return true;
+  if (!ints_of(t, 1, one)) return false;
+  at = const_cast<int32_t*>(one);
+  return true;
+}
+
+// format, block_size, k_pages, v_pages, block_table, k_scales, v_scales -> the bytes of an s2_paged_cache
+PyObject* paged_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  s2_paged_cache c{};
+  if (!count_is(n, 7) || !as_i32(a[0], c.format) || !as_i32(a[1], c.block_size)) return nullptr;
+  const bool scaled = c.format != S2_KV_BF16;
+  int64_t k[3], v[3], table[3];
+  if (!sizes_and_element(a[2], 3, scaled ? 1 : 2, k) || !sizes_and_element(a[3], 3, scaled ? 1 : 2, v) || !sizes_and_element(a[4], 3, 4, table)) return nullptr;
+  const Ref ks(strides_of(a[2])), vs(ks.o ? strides_of(a[3]) : nullptr);
+  if (!vs.o || !same(ks.o, vs.o) || !unit_stride(ks.o, 2) || !contiguous(a[4])) return nullptr;
+  const int64_t D = c.format == S2_KV_MXFP4 ? 2 * k[2] : k[2];
+  if (k[0] != v[0] || k[1] != v[1] || k[2] != v[2] || k[1] != c.block_size || k[0] > INT32_MAX || table[0] > INT32_MAX || table[1] > INT32_MAX ||
+      table[2] > INT32_MAX || D > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!stride_at(ks.o, 0, c.page_stride) || !stride_at(ks.o, 1, c.tok_stride)) return nullptr;
+  if (scaled) {
+    int64_t sk[3], sv[3];
+    if (!sizes_and_element(a[5], 3, 1, sk) || !sizes_and_element(a[6], 3, 1, sv)) return nullptr;
+    const Ref sks(strides_of(a[5])), svs(sks.o ? strides_of(a[6]) : nullptr);
+    if (!svs.o || !same(sks.o, svs.o) || !unit_stride(sks.o, 2)) return nullptr;
+    for (int i = 0; i < 3; ++i)
+      if (sk[i] != sv[i] || sk[i] != (i < 2 ? k[i] : D / 32)) {
+        fail_assert();
+        return nullptr;
+      }
+    if (!data_of(a[5], c.k_scales) || !data_of(a[6], c.v_scales) || !stride_at(sks.o, 0, c.scale_page_stride) || !stride_at(sks.o, 1, c.scale_tok_stride))
+      return nullptr;
+  } else if (a[5] != Py_None || a[6] != Py_None) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!data_of(a[2], c.k_pages) || !data_of(a[3], c.v_pages) || !data_of(a[4], c.block_table)) return nullptr;
+  c.nseq = (int32_t)table[0];
+  c.heads = (int32_t)table[1];
+  c.head_dim = (int32_t)D;
+  c.max_blocks = (int32_t)table[2];
+  c.num_pages = (int32_t)k[0];
+  return PyBytes_FromStringAndSize(reinterpret_cast<const char*>(&c), sizeof c);
+}
+bool cache_of(PyObject* o, s2_paged_cache& c) {
+  if (!PyBytes_Check(o) || PyBytes_GET_SIZE(o) != (Py_ssize_t)sizeof c) {
+    PyErr_SetString(PyExc_TypeError, "expected a paged cache");
+    return false;
+  }
+  __builtin_memcpy(&c, PyBytes_AS_STRING(o), sizeof c);
+  return true;
+}
+
+// two bf16 tensors of the same strides, of `n` sizes, the last of them features side by side; their sizes and the strides of the first two
+bool pair_of(PyObject* a, PyObject* b, int n, int64_t* size, int64_t* stride) {
+  int64_t other[4];
+  if (!sizes_and_element(a, n, 2, size) || !sizes_and_element(b, n, 2, other)) return false;
+  for (int i = 0; i < n; ++i)
+    if (size[i] != other[i]) return fail_assert();
+  const Ref as(strides_of(a)), bs(as.o ? strides_of(b) : nullptr);
+  if (!bs.o || !same(as.o, bs.o) || !unit_stride(as.o, n - 1)) return false;
+  for (int i = 0; i < n - 1; ++i)
+    if (!stride_at(as.o, i, stride[i])) return false;
+  return true;
+}
+
+PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k v cu_new start, max_new, rows, skipped, stream
+  s2_paged_cache c;
+  s2_kv_append_args d{};
+  void* stream;
+  int64_t size[3], stride[2];
+  if (!count_is(n, 9) || !cache_of(a[0], c) || !pair_of(a[1], a[2], 3, size, stride)) return nullptr;
+  if (size[1] != c.heads || size[2] != c.head_dim || size[0] > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_new) || !ints_of(a[4], c.nseq, d.start) || !as_i32(a[5], d.max_new) || !counter_of(a[7], d.skipped)) return nullptr;
+  if (a[6] != Py_None) {
+    const Ref count(PyObject_CallMethodNoArgs(a[6], names.numel));
+    int64_t items;
+    if (!count.o || !as_i64(count.o, items) || !ints_of(a[6], -1, d.rows)) return nullptr;
+    // (no rows at all: an empty tensor has no address, and is not "as they come")
+    if (items == 0 || items > INT32_MAX) {
+      fail_assert();
+      return nullptr;
+    }
+    d.num_items = (int32_t)items;
+  }
+  if (!data_of(a[1], d.k) || !data_of(a[2], d.v) || !as_address(a[8], stream)) return nullptr;
+  d.num_rows = (int32_t)size[0];
+  d.stride_row = stride[0];
+  d.stride_head = stride[1];
+  return status_of([&] { return cache_api.f.append(&c, &d, stream); });
+}
+
+PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k v (head, row, feature) cu_rows start, max_rows, stream
+  s2_paged_cache c;
+  s2_kv_read_args d{};
+  void* stream;
+  int64_t size[3], stride[2];
+  if (!count_is(n, 7) || !cache_of(a[0], c) || !pair_of(a[1], a[2], 3, size, stride)) return nullptr;
+  if (size[0] != c.heads || size[2] != c.head_dim || size[1] > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_rows) || !ints_of(a[4], c.nseq, d.start) || !as_i32(a[5], d.max_rows) || !data_of(a[1], d.k) ||
+      !data_of(a[2], d.v) || !as_address(a[6], stream))
+    return nullptr;
+  d.num_rows = (int32_t)size[1];
+  d.stride_head = stride[0];
+  d.stride_row = stride[1];
+  return status_of([&] { return cache_api.f.read(&c, &d, stream); });
+}
+
+// fp32 [nseq, heads, ...] side by side, `count` of them, or None
+bool lse_of(PyObject* t, int64_t count, float*& at) {
+  at = nullptr;
+  if (t == Py_None) return true;
+  const int32_t* words;
+  if (!ints_of(t, count, words)) return false;
+  at = reinterpret_cast<float*>(const_cast<int32_t*>(words));
+  return true;
+}
+
+// params or layout, cache, q seq_lens o lse, scale, workspace, missing, num_splits, stream
+template <bool LAYOUT>
+PyObject* over_cache(PyObject* const* a, Py_ssize_t n) {
+  s2_paged_cache c;
+  s2_cache_decode_args d{};
+  float scale;
+  void *pattern, *stream, *ws;
+  size_t bytes;
+  int64_t size[3], stride[2];
+  if (!count_is(n, 11) || !cache_of(a[1], c) || !pair_of(a[2], a[4], 3, size, stride)) return nullptr;
+  if (size[0] != c.nseq || size[1] != c.heads || size[2] != c.head_dim) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!ints_of(a[3], c.nseq, d.seq_lens) || !lse_of(a[5], (int64_t)c.nseq * c.heads, d.lse) || !counter_of(a[8], d.missing) || !data_of(a[2], d.q) ||
+      !data_of(a[4], d.o) || !as_i32(a[9], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[6], scale) || !workspace_of(a[7], ws, bytes) ||
+      !as_address(a[10], stream))
+    return nullptr;
+  d.q_stride_seq = stride[0];
+  d.q_stride_head = stride[1];
+  return status_of([&] {
+    if constexpr (LAYOUT)
+      return cache_api.f.decode_layout(static_cast<s2_layout*>(pattern), &c, &d, scale, ws, bytes, stream);
+    else
+      return cache_api.f.decode(static_cast<s2_layout_params*>(pattern), &c, &d, scale, ws, bytes, stream);
+  });
+}
+PyObject* decode_cache(PyObject*, PyObject* const* a, Py_ssize_t n) { return over_cache<false>(a, n); }
+PyObject* decode_cache_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return over_cache<true>(a, n); }
+
+// params or layout, cache, q k v parents seq_lens o lse, scale, workspace, missing, num_splits, stream
+template <bool LAYOUT>
+PyObject* drafts(PyObject* const* a, Py_ssize_t n) {
+  s2_paged_cache c;
+  s2_tree_args d{};
+  float scale;
+  void *pattern, *stream, *ws;
+  size_t bytes;
+  int64_t size[4], stride[3], kv_size[4], kv_stride[3];
+  if (!count_is(n, 14) || !cache_of(a[1], c) || !pair_of(a[2], a[7], 4, size, stride) || !pair_of(a[3], a[4], 4, kv_size, kv_stride)) return nullptr;
+  for (int i = 0; i < 4; ++i)
+    if (size[i] != kv_size[i]) {
+      fail_assert();
+      return nullptr;
+    }
+  if (size[0] != c.nseq || size[1] != c.heads || size[3] != c.head_dim || size[2] > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!ints_of(a[5], c.nseq * size[2], d.parents) || !ints_of(a[6], c.nseq, d.seq_lens) ||
+      !lse_of(a[8], (int64_t)c.nseq * c.heads * size[2], d.lse) || !counter_of(a[11], d.missing) || !data_of(a[2], d.q) || !data_of(a[3], d.k) ||
+      !data_of(a[4], d.v) || !data_of(a[7], d.o) || !as_i32(a[12], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[9], scale) ||
+      !workspace_of(a[10], ws, bytes) || !as_address(a[13], stream))
+    return nullptr;
+  d.nodes = (int32_t)size[2];
+  d.q_stride_seq = stride[0];
+  d.q_stride_head = stride[1];
+  d.q_stride_node = stride[2];
+  d.kv_stride_seq = kv_stride[0];
+  d.kv_stride_head = kv_stride[1];
+  d.kv_stride_node = kv_stride[2];
+  return status_of([&] {
+    if constexpr (LAYOUT)
+      return cache_api.f.tree_layout(static_cast<s2_layout*>(pattern), &c, &d, scale, ws, bytes, stream);
+    else
+      return cache_api.f.tree(static_cast<s2_layout_params*>(pattern), &c, &d, scale, ws, bytes, stream);
+  });
+}
+PyObject* tree(PyObject*, PyObject* const* a, Py_ssize_t n) { return drafts<false>(a, n); }
+PyObject* tree_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return drafts<true>(a, n); }
+
+PyObject* bind_to(void** to, Py_ssize_t count, PyObject* const* a, Py_ssize_t n) {
+  if (!count_is(n, count)) return nullptr;
+  for (Py_ssize_t i = 0; i < n; ++i)
+    if (!PyLong_AsVoidPtr(a[i])) {
       if (!PyErr_Occurred()) PyErr_SetString(PyExc_ValueError, "no address");
       return nullptr;
     }
-  }
-  for (Py_ssize_t i = 0; i < n; ++i) api.at[i] = at[i];
+  for (Py_ssize_t i = 0; i < n; ++i) to[i] = PyLong_AsVoidPtr(a[i]);
   Py_RETURN_NONE;
 }
+PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) { return bind_to(api.at, kEntryPoints, a, n); }
+PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t n) { return bind_to(cache_api.at, kCacheEntryPoints, a, n); }
 
 #define S2_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {S2_METHOD(bind),          S2_METHOD(fwd),          S2_METHOD(fwd_rows),      S2_METHOD(fwd_varlen),
                          S2_METHOD(bwd_stages),    S2_METHOD(bwd_varlen),   S2_METHOD(dense_fwd),     S2_METHOD(dense_bwd),
                          S2_METHOD(decode),        S2_METHOD(decode_static), S2_METHOD(decode_layout), S2_METHOD(decode_paged),
-                         S2_METHOD(decode_paged_layout), {nullptr, nullptr, 0, nullptr}};
+                         S2_METHOD(decode_paged_layout), S2_METHOD(bind_cache), S2_METHOD(paged_cache), S2_METHOD(kv_append),
+                         S2_METHOD(kv_read),       S2_METHOD(decode_cache), S2_METHOD(decode_cache_layout), S2_METHOD(tree),
+                         S2_METHOD(tree_layout),   {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -406,15 +640,23 @@ PyMODINIT_FUNC PyInit__marshal(void) {
   if (!m.o) return nullptr;
 #define X(entry, name) #entry,
   const char* const entries[] = {S2_ENTRY_POINTS(X)};
+  const char* const cache_entries[] = {S2_CACHE_ENTRY_POINTS(X)};
 #undef X
-  const Ref order(PyTuple_New(kEntryPoints));
-  if (!order.o) return nullptr;
-  for (Py_ssize_t i = 0; i < kEntryPoints; ++i) {
-    PyObject* const name = PyUnicode_FromString(entries[i]);
-    if (!name) return nullptr;
-    PyTuple_SET_ITEM(order.o, i, name);
+  const struct {
+    const char* attribute;
+    const char* const* entry;
+    Py_ssize_t count;
+  } orders[] = {{"entry_points", entries, kEntryPoints}, {"cache_entry_points", cache_entries, kCacheEntryPoints}};
+  for (const auto& of : orders) {
+    const Ref order(PyTuple_New(of.count));
+    if (!order.o) return nullptr;
+    for (Py_ssize_t i = 0; i < of.count; ++i) {
+      PyObject* const name = PyUnicode_FromString(of.entry[i]);
+      if (!name) return nullptr;
+      PyTuple_SET_ITEM(order.o, i, name);
+    }
+    if (PyObject_SetAttrString(m.o, of.attribute, order.o)) return nullptr;
   }
-  if (PyObject_SetAttrString(m.o, "entry_points", order.o)) return nullptr;
   Py_INCREF(m.o);
   return m.o;
 }
