@@ -29,20 +29,27 @@ namespace {
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kMaxRows = 5;  // block rows that 64 positions can lie in, blocks of 16 tokens
 
-// Wavefronts to a SIMD that the registers are for: accumulators, queries, K and V of a unit on their way, scores.
-constexpr int waves_for(int D, int dwords, int NQ) { return NQ * (D / 4 + D / 8 + 16) + 8 * dwords + 48 <= 256 ? 2 : 1; }
+// Wavefronts to a SIMD: two while accumulators, scores, queries and a unit of K and of V on their way fit 256 registers.
+constexpr int waves_for(int D, int NQ) { return NQ == 1 || (NQ == 2 && D == 64) ? 2 : 1; }
 
-template <int D, int FMT, int NQ>
-__global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) void cache_attn_kernel(const CacheAttnParams p) {
+// SMALL: blocks of 16 or 32 tokens, so that a unit of 64 is gathered from four or two of the list's blocks; else it is a piece of one block.
+template <int D, int FMT, int NQ, bool SMALL>
+__global__ __launch_bounds__(256, waves_for(D, NQ)) void cache_attn_kernel(const CacheAttnParams p) {
   using Rows = CacheRows<D, FMT>;
   using Tile = ChunkTile<D>;
   constexpr int W = 4, KK = D / 32, FT = D / 16, Q = 16 * NQ;
   constexpr int RS = D + 4;  // floats to a row where wavefronts are summed
+  // With 64 queries their operands are read from LDS, one by one for a whole unit's K; with fewer they stay in registers.
+  constexpr bool kQueriesInLds = NQ == 4;
+  constexpr int kGroup = kQueriesInLds ? 4 : 1;  // pieces of K that are operands at the same time
   static_assert(16 * RS * 4 <= 32 * Tile::RB, "a tile of sums fits where V was");
 
   __shared__ __align__(16) uint16_t sh_v[W][32 * Tile::kStride];
-  __shared__ float sh_p[W][16][Q];  // probabilities of 16 tokens, where V is taken token by token
+  __shared__ u32x4 sh_q[kQueriesInLds ? NQ * KK * 64 : 1];
   __shared__ float sh_m[W][Q], sh_l[W][Q];
+  // Infinities and NaN of V that were taken out of the products (values(), below): bits of [query tile][feature tile][lane], a byte to a feature.
+  __shared__ uint32_t sh_odd[NQ * FT * 64];
+  __shared__ uint32_t sh_any_odd;
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -92,15 +99,21 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
     rel_q[n] = __shfl(rel, 16 * n + c, 64);
     there_q[n] = nodes_there >> (16 * n + c) & 1;
   }
-  bf16x8 qf[NQ][KK];
-  auto load_queries = [&](auto feature) {
+  for (int i = tid; i < NQ * FT * 64; i += 64 * W) sh_odd[i] = 0;
+  if (tid == 0) sh_any_odd = 0;
+  bf16x8 qf[kQueriesInLds ? 1 : NQ][KK];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
+  for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-        qf[n][kk] = there_q[n] ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + (16 * n + c) * p.q_sn + feature(kk)) : bf16x8{};
-  };
-  load_queries([&](int kk) { return Rows::feature(kk, g); });
+    for (int kk = 0; kk < KK; ++kk) {
+      if (kQueriesInLds && (n * KK + kk) % W != wave) continue;
+      const bf16x8 x = there_q[n] ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + (16 * n + c) * p.q_sn + Rows::feature(kk, g)) : bf16x8{};
+      if constexpr (kQueriesInLds)
+        sh_q[(n * KK + kk) * 64 + lane] = __builtin_bit_cast(u32x4, x);
+      else
+        qf[n][kk] = x;
+    }
+  __syncthreads();
 
   f32x4 acc[NQ][FT];
   float m_run[NQ], l_run[NQ];
@@ -116,14 +129,20 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
   const uint32_t v_write = lds_addr(my_v) + c * Tile::RB, v_read = lds_addr(my_v) + Tile::tr_lane(lane);
 
   f32x4 s[NQ][4];
-  // Scores of 16 tokens.
-  auto score = [&](int t, const u32x4 (&k)[KK]) __attribute__((always_inline)) {
+  // Scores of the pieces t0 .. t0 + kGroup - 1.
+  auto score = [&](int t0, const u32x4 (&k)[kGroup][KK]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      s[n][t] = f32x4{};
+    for (int n = 0; n < NQ; ++n)
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s[n][t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[n][kk], s[n][t]);
-    }
+      for (int kk = 0; kk < KK; ++kk) {
+        bf16x8 q;
+        if constexpr (kQueriesInLds)
+          q = __builtin_bit_cast(bf16x8, sh_q[(n * KK + kk) * 64 + lane]);
+        else
+          q = qf[n][kk];
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) s[n][t0 + i] = mfma16(__builtin_bit_cast(bf16x8, k[i][kk]), q, kk ? s[n][t0 + i] : f32x4{});
+      }
   };
   // Scores (masked ones -inf) to probabilities; the accumulators go along with the maximum.
   auto softmax = [&]() __attribute__((always_inline)) {
@@ -137,7 +156,13 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
       mx = max_halves(max_rows(mx));
       const float m_new = fmaxf(m_run[n], mx);
       const float mc = m_new == kNegInf ? 0.f : m_new * cl;
-      const float alpha = fast_exp2(m_run[n] * cl - mc);  // (-inf before the first token: 0)
+      if (__any(m_new > m_run[n])) {
+        const float alpha = fast_exp2(m_run[n] * cl - mc);  // (-inf before the first token: 0)
+        l_run[n] *= alpha;
+        m_run[n] = m_new;
+#pragma unroll
+        for (int ft = 0; ft < FT; ++ft) acc[n][ft] *= alpha;
+      }
       float sum = 0.f;
 #pragma unroll
       for (int t = 0; t < 4; ++t)
@@ -146,55 +171,55 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
           s[n][t][e] = fast_exp2(__builtin_fmaf(s[n][t][e], cl, -mc));
           sum += s[n][t][e];
         }
-      l_run[n] = l_run[n] * alpha + sum;
-      m_run[n] = m_new;
-#pragma unroll
-      for (int ft = 0; ft < FT; ++ft) acc[n][ft] *= alpha;
+      l_run[n] += sum;
     }
   };
-  // 32 tokens' V (two pieces) into LDS, and their products.  seen(n, t, e): whether the column's query attends token 4 * g + e of piece t; asked only
-  // where `mixed`: then a token that some query does not attend may hold anything, and 0 times that need not be 0.
-  auto values = [&](int half, const u32x4 (&v0)[KK], const u32x4 (&v1)[KK], auto feature, bool mixed, auto seen) __attribute__((always_inline)) {
-    uint32_t odd = 0;
+  auto write_v = [&](int piece, const u32x4 (&v)[KK]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int kk = 0; kk < KK; ++kk) {
-      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 2 * feature(kk)) = v0[kk];
-      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * Tile::RB + 2 * feature(kk)) = v1[kk];
-      if (mixed) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          odd |= (v0[kk][e] & 0x7f80u) == 0x7f80u || (v0[kk][e] & 0x7f800000u) == 0x7f800000u || (v1[kk][e] & 0x7f80u) == 0x7f80u ||
-                 (v1[kk][e] & 0x7f800000u) == 0x7f800000u;
-      }
-    }
+    for (int kk = 0; kk < KK; ++kk)
+      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * piece * Tile::RB + 2 * Rows::feature(kk, g)) = v[kk];
+  };
+  // 32 tokens' V (two pieces) into LDS, and their products.  odd: there are infinities or NaN among them (asked only where some query does not attend some
+  // token: that may hold anything, and 0 times it need not be 0).  They are then taken out, and which of them a query attends is found by products of ones
+  // and zeros and kept until the end.
+  auto values = [&](int half, const u32x4 (&v)[2][KK], bool odd, const uint64_t (&seen)[NQ]) __attribute__((always_inline)) {
+    write_v(0, v[0]);
+    write_v(1, v[1]);
     wait_lds();
-    if (mixed && __any(odd)) {
-      for (int t = 0; t < 2; ++t) {
+    if (odd) {
+      uint32_t* const words = reinterpret_cast<uint32_t*>(my_v);
+#pragma unroll 1
+      for (int kind = 0; kind < 3; ++kind) {  // infinity, minus infinity, NaN
+        auto ones = [&](uint32_t x) { return (kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u) ? 0x3f80u : 0u; };
+#pragma unroll 1
+        for (int ft = 0; ft < FT; ++ft) {
+          u32x4 vf = lds_read_tr2(v_read + 32 * ft, v_read + 32 * ft, 0, 16 * Tile::RB);
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e) {
-            // (as the product takes it; -1: not attended)
-            const float x = (float)(__bf16)(t ? s[n][2 * half + 1][e] : s[n][2 * half][e]);
-            sh_p[wave][4 * g + e][16 * n + c] = seen(n, 2 * half + t, e) ? x : -1.f;
-          }
-        wait_lds();
-        for (int j = 0; j < 16; ++j)
+          for (int e = 0; e < 4; ++e) vf[e] = ones(vf[e] & 0xffffu) | ones(vf[e] >> 16) << 16;
 #pragma unroll
           for (int n = 0; n < NQ; ++n) {
-            const float x = sh_p[wave][j][16 * n + c];
+            const uint32_t mine = (uint32_t)(seen[n] >> (32 * half)) >> (4 * g);  // tokens 4 g .. and 16 + 4 g ..
+            u32x4 w;
 #pragma unroll
-            for (int ft = 0; ft < FT; ++ft)
+            for (int e = 0; e < 4; ++e) w[e] = ((mine >> (16 * (e / 2) + 2 * (e % 2))) & 1) * 0x3f80u + ((mine >> (16 * (e / 2) + 2 * (e % 2) + 1)) & 1) * 0x3f800000u;
+            const f32x4 count = mfma16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, w), f32x4{});
+            uint32_t found = 0;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const uint16_t bits = my_v[(16 * t + j) * Tile::kStride + 16 * ft + 4 * g + e];
-                const float v = __builtin_bit_cast(float, (uint32_t)bits << 16);
-                acc[n][ft][e] = x < 0.f ? acc[n][ft][e] : __builtin_fmaf(x, v, acc[n][ft][e]);
-              }
+            for (int e = 0; e < 4; ++e) found |= (count[e] > 0.f ? 1u : 0u) << (8 * e + kind);
+            if (found) {
+              atomicOr(&sh_odd[(n * FT + ft) * 64 + lane], found);
+              sh_any_odd = 1;
+            }
           }
-        wait_lds();
+        }
       }
-      return;
+      wait_lds();
+#pragma unroll 1
+      for (int i = lane; i < 32 * Tile::RB / 4; i += 64) {
+        const uint32_t x = words[i];
+        words[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+      }
+      wait_lds();
     }
     bf16x8 pf[NQ];
 #pragma unroll
@@ -216,18 +241,28 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
   int n_missing = 0;
   const int all_rows = (1 << n_rows) - 1;
 
-  // Four pieces of 16 tokens of the list's blocks.
+  // 64 tokens: of one block, or (SMALL) four pieces of 16 of the list's blocks; or the drafted ones.
+  constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB;
   struct Unit {
-    int page[4], skip[4], rows[4], bits[4];
+    int page[NB], skip[NB], rows[NB], bits[NB];
+    bool drafts;
   };
-  int r_now = -1, u_now = 0, u_end = 0;
+  int r_now = -1, u_now = -W, u_end = 0;
   RowBlocks rb{};
+  bool drafts_left = tree && split == p.num_splits - 1 && wave == W - 1 && nodes_there;
   // The wavefront's next unit with a token to read.
-  auto next_unit = [&](Unit& w) {
+  auto next_unit = [&](Unit& w) __attribute__((always_inline)) {
+    w.drafts = false;
     for (;;) {
       u_now += W;
       while (u_now >= u_end) {
-        if (++r_now >= n_rows) return false;
+        if (r_now + 1 >= n_rows) {
+          if (!drafts_left) return false;
+          drafts_left = false;
+          w.drafts = true;
+          return true;
+        }
+        ++r_now;
         rb = row_blocks(p, h, row0 + r_now);
         const int units = ((rb.count << sh) + 63) >> 6;
         const int even = units / p.by_splits, rest = units - even * p.num_splits;
@@ -236,12 +271,13 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
       }
       int any = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
+      for (int i = 0; i < NB; ++i) {
         const int l = 64 * u_now + 16 * i, n = l >> sh, skip = l & (S - 1);
-        const bool inside = n < rb.count;
+        const bool inside = !SMALL || n < rb.count;
         const int blk = rb.block(inside ? n : 0);
-        int rows = inside ? min(max(L - (blk * S + skip), 0), 16) : 0, bits = 1 << r_now;
+        int rows = inside ? min(max(L - (blk * S + skip), 0), kTokens) : 0, bits = 1 << r_now;
         if (n_rows > 1 && rows > 0) {
+#pragma unroll 1
           for (int r = 0; r < n_rows; ++r) {
             if (r == r_now || !row_keeps(p, row_blocks(p, h, row0 + r), h, row0 + r, blk, n)) continue;
             if (r < r_now) rows = 0;  // (read in that row's turn)
@@ -266,102 +302,156 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
     }
   };
 
-  typename Rows::Part kr[4], vr[4];
-  auto load = [&](const Unit& w, const uint8_t* pool, const uint8_t* scales, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
+  // What a node's row i keeps of the nodes above it and itself, for the query of my column.
+  auto drafts_seen = [&](uint64_t (&seen)[NQ]) __attribute__((always_inline)) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const uint8_t* const at = pool + w.page[i] * p.c.page + w.skip[i] * p.c.tok;
-      const uint8_t* const scale_at = Rows::kScaled ? scales + w.page[i] * p.c.scale_page + w.skip[i] * p.c.scale_tok : nullptr;
-      Rows::load(x[i], at, scale_at, w.rows[i], p.c.tok, p.c.scale_tok, c, g);
+    for (int n = 0; n < NQ; ++n) {
+      const uint32_t lo = __shfl((uint32_t)above, 16 * n + c, 64), hi = __shfl((uint32_t)(above >> 32), 16 * n + c, 64);
+      seen[n] = (uint64_t)hi << 32 | lo;
+    }
+    if (n_rows == 1) return;
+#pragma unroll 1
+    for (int r = 0; r < n_rows; ++r) {
+      const RowBlocks row = row_blocks(p, h, row0 + r);
+      uint64_t kept = 0;
+#pragma unroll 1
+      for (int a = 0; a <= r; ++a)
+        if (row_keeps(p, row, h, row0 + r, row0 + a, row.count - 1)) kept |= __ballot(there && rel == a);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+        if (rel_q[n] == r) seen[n] &= kept;
     }
   };
-  auto compute = [&](const Unit& w) __attribute__((always_inline)) {
-    bool mixed = false;
+  // (a node that is not there may hold anything: nobody attends it, and it is not fetched)
+  auto draft_rows = [&](int t, const uint16_t* of, auto& x) __attribute__((always_inline)) {
+    const bool here = nodes_there >> (16 * t + c) & 1;
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      u32x4 k[KK];
-      Rows::operands(kr[t], g, k);
-      score(t, k);
-      mixed |= w.rows[t] > 0 && w.bits[t] != all_rows;
-      if (w.rows[t] < 16 || w.bits[t] != all_rows) {
+    for (int kk = 0; kk < KK; ++kk) {
+      const u32x4 row = here ? *reinterpret_cast<const u32x4*>(of + b * p.kv_ss + h * p.kv_sh + (16 * t + c) * p.kv_sn + Rows::feature(kk, g)) : u32x4{};
+      if constexpr (Rows::kScaled) {
+        x[kk] = row;
+      } else {
 #pragma unroll
-        for (int n = 0; n < NQ; ++n)
-#pragma unroll
-          for (int e = 0; e < 4; ++e)
-            if (4 * g + e >= w.rows[t] || !(w.bits[t] >> rel_q[n] & 1)) s[n][t][e] = kNegInf;
+        for (int e = 0; e < 4; ++e) x[4 * kk + e] = row[e];
       }
     }
+  };
+
+  typename Rows::Part kr[4], vr[4];
+  auto load = [&](const Unit& w, const uint8_t* pool, const uint8_t* scales, const uint16_t* drafted, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
+    if (w.drafts) {
+      if constexpr (!Rows::kScaled) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) draft_rows(t, drafted, x[t].x);
+      }
+      return;  // (else fetched where they are used)
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+      const uint8_t* const at = pool + w.page[i] * p.c.page + w.skip[i] * p.c.tok;
+      const uint8_t* const scale_at = Rows::kScaled ? scales + w.page[i] * p.c.scale_page + w.skip[i] * p.c.scale_tok : nullptr;
+#pragma unroll
+      for (int t = 0; t < 4 / NB; ++t) Rows::load(x[i + t], at, scale_at, w.rows[i], p.c.tok, p.c.scale_tok, 16 * t + c, g);
+    }
+  };
+  // Tokens that the query of my column attends, where they are not all of the unit.
+  uint64_t seen[NQ];
+  bool some, mixed;  // not all queries attend all tokens; some query does not attend a token that is there
+  auto scores = [&](const Unit& w) __attribute__((always_inline)) {
+#pragma unroll
+    for (int t0 = 0; t0 < 4; t0 += kGroup) {
+      u32x4 k[kGroup][KK];
+      if (Rows::kScaled && w.drafts) {
+        if constexpr (Rows::kScaled) {
+#pragma unroll
+          for (int i = 0; i < kGroup; ++i) draft_rows(t0 + i, p.k_draft, k[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < kGroup; ++i) Rows::operands(kr[t0 + i], g, k[i]);
+      }
+      score(t0, k);
+    }
+    some = mixed = w.drafts;
+    if (w.drafts) {
+      drafts_seen(seen);
+    } else {
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        some |= w.rows[i] < kTokens || w.bits[i] != all_rows;
+        mixed |= w.rows[i] > 0 && w.bits[i] != all_rows;
+      }
+      if (some) {
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) {
+          seen[n] = 0;
+#pragma unroll
+          for (int i = 0; i < NB; ++i)
+            if (w.bits[i] >> rel_q[n] & 1) seen[n] |= (w.rows[i] >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << w.rows[i]) - 1) << (16 * i);
+        }
+      }
+    }
+    if (some) {
+#pragma unroll
+      for (int n = 0; n < NQ; ++n)
+#pragma unroll
+        for (int t = 0; t < 4; ++t) {
+          const uint32_t mine = (uint32_t)(seen[n] >> (32 * (t / 2))) >> (16 * (t % 2) + 4 * g);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) s[n][t][e] = mine >> e & 1 ? s[n][t][e] : kNegInf;
+        }
+    }
+  };
+  auto sums = [&](const Unit& w) __attribute__((always_inline)) {
     softmax();
 #pragma unroll
     for (int half = 0; half < 2; ++half) {
-      u32x4 v0[KK], v1[KK];
-      Rows::operands(vr[2 * half], g, v0);
-      Rows::operands(vr[2 * half + 1], g, v1);
-      values(half, v0, v1, [&](int kk) { return Rows::feature(kk, g); }, mixed,
-             [&](int n, int t, int e) { return 4 * g + e < w.rows[t] && (w.bits[t] >> rel_q[n] & 1); });
+      u32x4 v[2][KK];
+      if (Rows::kScaled && w.drafts) {
+        if constexpr (Rows::kScaled) {
+#pragma unroll
+          for (int i = 0; i < 2; ++i) draft_rows(2 * half + i, p.v_draft, v[i]);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) Rows::operands(vr[2 * half + i], g, v[i]);
+      }
+      bool odd = false;
+      if (mixed) {
+        uint32_t top = 0;  // (an exponent field of ones carries into its value's sign)
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+#pragma unroll
+          for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) top |= (v[i][kk][e] & 0x7fff7fffu) + 0x00800080u;
+        odd = __any((top & 0x80008000u) != 0);
+      }
+      values(half, v, odd, seen);
     }
   };
   {
     Unit w;
-    u_now = -W;
-    while (next_unit(w)) {
-      load(w, p.c.k, p.c.ks, kr);
-      load(w, p.c.v, p.c.vs, vr);
-      compute(w);
+    if (next_unit(w)) {
+      load(w, p.c.k, p.c.ks, p.k_draft, kr);
+      load(w, p.c.v, p.c.vs, p.v_draft, vr);
+      for (;;) {
+        Unit next;
+        const bool more = next_unit(next);
+        // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
+        scores(w);
+        __builtin_amdgcn_sched_barrier(0);
+        if (more) load(next, p.c.k, p.c.ks, p.k_draft, kr);
+        __builtin_amdgcn_sched_barrier(0);
+        sums(w);
+        __builtin_amdgcn_sched_barrier(0);
+        if (!more) break;
+        load(next, p.c.v, p.c.vs, p.v_draft, vr);
+        w = next;
+      }
     }
   }
   if (p.missing && lane == 0 && n_missing > 0) atomicAdd(p.missing, n_missing);
-
-  // ---- the drafted ones: one unit, taken by one wavefront of the last split
-  if (tree && split == p.num_splits - 1 && wave == W - 1 && nodes_there) {
-    uint64_t in_row[kMaxRows];
-#pragma unroll
-    for (int r = 0; r < kMaxRows; ++r) in_row[r] = __ballot(there && rel == r);
-    uint64_t sees[NQ];
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      const uint32_t lo = __shfl((uint32_t)above, 16 * n + c, 64), hi = __shfl((uint32_t)(above >> 32), 16 * n + c, 64);
-      sees[n] = (uint64_t)hi << 32 | lo;
-    }
-    for (int r = 0; r < n_rows; ++r) {
-      const RowBlocks row = row_blocks(p, h, row0 + r);
-      uint64_t kept = 0;
-#pragma unroll
-      for (int a = 0; a < kMaxRows; ++a)
-        if (a <= r && row_keeps(p, row, h, row0 + r, row0 + a, row.count - 1)) kept |= in_row[a];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-        if (rel_q[n] == r) sees[n] &= kept;
-    }
-    const uint16_t* const from = p.k_draft + b * p.kv_ss + h * p.kv_sh;
-    const int64_t to_v = p.v_draft - p.k_draft;
-    auto fetch = [&](int t, int64_t off, u32x4 (&x)[KK]) __attribute__((always_inline)) {
-      const bool here = nodes_there >> (16 * t + c) & 1;  // (nobody attends a node that is not there, and it may hold anything)
-#pragma unroll
-      for (int kk = 0; kk < KK; ++kk)
-        x[kk] = here ? *reinterpret_cast<const u32x4*>(from + off + (16 * t + c) * p.kv_sn + Rows::feature(kk, g)) : u32x4{};
-    };
-#pragma unroll
-    for (int t = 0; t < 4; ++t) {
-      u32x4 k[KK];
-      fetch(t, 0, k);
-      score(t, k);
-#pragma unroll
-      for (int n = 0; n < NQ; ++n)
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (!(sees[n] >> (16 * t + 4 * g + e) & 1)) s[n][t][e] = kNegInf;
-    }
-    softmax();
-#pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      u32x4 v0[KK], v1[KK];
-      fetch(2 * half, to_v, v0);
-      fetch(2 * half + 1, to_v, v1);
-      values(half, v0, v1, [&](int kk) { return Rows::feature(kk, g); }, true,
-             [&](int n, int t, int e) { return (sees[n] >> (16 * t + 4 * g + e) & 1) != 0; });
-    }
-  }
 
   // ---- the wavefronts' sums, 16 queries at a time through where V was
 #pragma unroll
@@ -380,6 +470,17 @@ __global__ __launch_bounds__(256, waves_for(D, CacheRows<D, FMT>::kDwords, NQ)) 
     for (int w = 0; w < W; ++w) m = fmaxf(m, sh_m[w][16 * n + c]);
     // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
     const float weight = sh_l[wave][16 * n + c] == 0.f ? 0.f : fast_exp2((m_run[n] - m) * cl);
+    if (sh_any_odd) {
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) {
+        const uint32_t found = wave == 0 ? sh_odd[(n * FT + ft) * 64 + lane] : 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const uint32_t x = found >> (8 * e) & 7;
+          if (x) acc[n][ft][e] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
+        }
+      }
+    }
     float* const mine = reinterpret_cast<float*>(my_v) + c * RS + 4 * g;
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft)
@@ -452,15 +553,23 @@ __global__ __launch_bounds__(256) void cache_attn_merge_kernel(const CacheAttnPa
   if (d == 0 && p.lse) p.lse[row] = l == 0.f ? kNegInf : m * p.scale + __logf(l);
 }
 
-template <int D, int FMT>
-hipError_t launch_nodes(const CacheAttnParams& p, hipStream_t stream) {
+template <int D, int FMT, bool SMALL>
+void launch_split(const CacheAttnParams& p, hipStream_t stream) {
   const dim3 grid(p.nseq * p.heads * p.num_splits), block(256);
   if (p.nodes <= 16)
-    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 1>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 1, SMALL>), grid, block, 0, stream, p);
   else if (p.nodes <= 32)
-    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 2>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 2, SMALL>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 4>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, 4, SMALL>), grid, block, 0, stream, p);
+}
+
+template <int D, int FMT>
+hipError_t launch_nodes(const CacheAttnParams& p, hipStream_t stream) {
+  if (p.block_size < 64)
+    launch_split<D, FMT, true>(p, stream);
+  else
+    launch_split<D, FMT, false>(p, stream);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.num_splits == 1) return e;
   const int64_t rows = (int64_t)p.nseq * p.heads * p.nodes, per = 256 / (D / 8);
