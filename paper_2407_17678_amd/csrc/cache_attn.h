@@ -1,0 +1,267 @@
+// Internal: what the two kernels of attention over a paged cache (cache_attn_kernel.hip, cache_attn_shared_kernel.hip) have in common: the nodes of
+// a tree, the walk over the blocks that their rows keep, masks, and what is done about values of V that are not numbers.
+#pragma once
+#include <hip/hip_runtime.h>
+
+#include "kernels.h"
+#include "kv_cache.h"
+#include "row_blocks.h"
+#include "sched_util.h"
+
+namespace s2 {
+
+constexpr float kNegInf = -__builtin_inff();
+constexpr int kMaxNodeRows = 5;  // block rows that 64 positions can lie in, blocks of 16 tokens
+
+// Node `lane` of a sequence's tree (without a tree one query, the last cached token's).
+struct Nodes {
+  uint64_t above;    // it and the nodes above it, bits
+  bool there;
+  int rel;           // its block row, counted from row0
+  int row0, n_rows;  // block rows of the nodes that are there
+  uint64_t all;      // the nodes that are there
+};
+__device__ __forceinline__ Nodes nodes_of(const CacheAttnParams& p, int b, int L, int lane) {
+  Nodes x;
+  const int sh = p.c.block_shift;
+  int depth = 0;
+  x.above = 1;
+  x.there = lane == 0;
+  if (p.parents) {
+    int up = lane < p.nodes ? p.parents[(int64_t)b * p.nodes + lane] : -2;
+    if (up < -1 || up >= lane) up = -2;
+    x.above = (uint64_t)1 << lane;
+#pragma unroll
+    for (int i = 0; i < 6; ++i) {  // (the chain above a node doubles each time)
+      const int from = max(up, 0);
+      const uint32_t lo = __shfl((uint32_t)x.above, from, 64), hi = __shfl((uint32_t)(x.above >> 32), from, 64);
+      const int next = __shfl(up, from, 64);
+      if (up >= 0) {
+        x.above |= (uint64_t)hi << 32 | lo;
+        up = next;
+      }
+    }
+    depth = __popcll(x.above) - 1;
+    x.there = up == -1 && L + depth < p.max_len;
+  }
+  x.row0 = (p.parents ? L : L - 1) >> sh;
+  x.rel = x.there && p.parents ? ((L + depth) >> sh) - x.row0 : 0;
+  x.all = __ballot(x.there);
+  x.n_rows = x.all ? 1 : 0;
+#pragma unroll
+  for (int r = 1; r < kMaxNodeRows; ++r) x.n_rows += __ballot(x.rel >= r) != 0;
+  return x;
+}
+
+// 64 tokens: of one block, or (SMALL: blocks of 16 or 32) four pieces of 16 of the list's blocks; or the drafted ones.
+template <bool SMALL>
+struct Unit {
+  static constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB;
+  int page[NB], skip[NB], rows[NB], bits[NB];  // (bits: which block rows keep it)
+  bool drafts;
+};
+
+// The units of a split, block row by block row: each block in the turn of the first row that keeps it.
+template <bool SMALL>
+struct Walk {
+  const CacheAttnParams& p;
+  const int32_t* table;
+  int h, L, row0, n_rows, split, first, step;  // unit `first` of the split, and every step-th
+  bool drafts_left;
+  int n_missing = 0;
+  int r_now = -1, u_now = 0, u_end = 0;
+  RowBlocks rb{};
+
+  __device__ __forceinline__ Walk(const CacheAttnParams& p_, int b, int h_, int L_, const Nodes& x, int split_, int first_, int step_, bool drafts)
+      : p(p_), table(p_.c.table + ((int64_t)b * p_.heads + h_) * p_.c.max_blocks), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_),
+        first(first_), step(step_), drafts_left(drafts), u_now(-step_) {}
+
+  // The next unit with a token to read.
+  __device__ __forceinline__ bool next(Unit<SMALL>& w) {
+    constexpr int NB = Unit<SMALL>::NB, kTokens = Unit<SMALL>::kTokens;
+    const int S = p.block_size, sh = p.c.block_shift;
+    w.drafts = false;
+    for (;;) {
+      u_now += step;
+      while (u_now >= u_end) {
+        if (r_now + 1 >= n_rows) {
+          if (!drafts_left) return false;
+          drafts_left = false;
+          w.drafts = true;
+          return true;
+        }
+        ++r_now;
+        rb = row_blocks(p, h, row0 + r_now);
+        const int units = ((rb.count << sh) + 63) >> 6;
+        const int even = units / p.by_splits, rest = units - even * p.num_splits;
+        u_now = even * split + rest * split / p.by_splits + first;
+        u_end = even * (split + 1) + rest * (split + 1) / p.by_splits;
+      }
+      int any = 0;
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int l = 64 * u_now + 16 * i, n = l >> sh, skip = l & (S - 1);
+        const bool inside = !SMALL || n < rb.count;
+        const int blk = rb.block(inside ? n : 0);
+        int rows = inside ? min(max(L - (blk * S + skip), 0), kTokens) : 0, bits = 1 << r_now;
+        if (n_rows > 1 && rows > 0) {
+#pragma unroll 1
+          for (int r = 0; r < n_rows; ++r) {
+            if (r == r_now || !row_keeps(p, row_blocks(p, h, row0 + r), h, row0 + r, blk, n)) continue;
+            if (r < r_now) rows = 0;  // (read in that row's turn)
+            bits |= 1 << r;
+          }
+        }
+        int page = 0;
+        if (rows > 0) {
+          page = load_const<int32_t>(table + blk);
+          if (page < 0 || page >= p.c.num_pages) {
+            n_missing += skip == 0;
+            rows = 0;
+          }
+        }
+        w.page[i] = page;
+        w.skip[i] = skip;
+        w.rows[i] = rows;
+        w.bits[i] = bits;
+        any |= rows;
+      }
+      if (any) return true;
+    }
+  }
+};
+
+// Tokens of a unit that a query in block row `rel` attends, bits; all of them are attended by all queries unless `some`; some query does not attend a
+// token that is there if `mixed`.
+template <bool SMALL>
+__device__ __forceinline__ void unit_masks(const Unit<SMALL>& w, int all_rows, bool& some, bool& mixed) {
+  some = mixed = w.drafts;
+  if (w.drafts) return;
+#pragma unroll
+  for (int i = 0; i < Unit<SMALL>::NB; ++i) {
+    some |= w.rows[i] < Unit<SMALL>::kTokens || w.bits[i] != all_rows;
+    mixed |= w.rows[i] > 0 && w.bits[i] != all_rows;
+  }
+}
+template <bool SMALL>
+__device__ __forceinline__ uint64_t unit_seen(const Unit<SMALL>& w, int rel) {
+  uint64_t seen = 0;
+#pragma unroll
+  for (int i = 0; i < Unit<SMALL>::NB; ++i)
+    if (w.bits[i] >> rel & 1) seen |= (w.rows[i] >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << w.rows[i]) - 1) << (16 * i);
+  return seen;
+}
+// Drafted nodes that the query of node `node` attends: it and those above it, in blocks that its row keeps.
+__device__ __forceinline__ uint64_t drafts_seen(const CacheAttnParams& p, const Nodes& x, int h, int node, int rel) {
+  const uint32_t lo = __shfl((uint32_t)x.above, node, 64), hi = __shfl((uint32_t)(x.above >> 32), node, 64);
+  uint64_t seen = (uint64_t)hi << 32 | lo;
+  if (x.n_rows == 1) return seen;
+#pragma unroll 1
+  for (int r = 0; r < x.n_rows; ++r) {
+    const RowBlocks row = row_blocks(p, h, x.row0 + r);
+    uint64_t kept = 0;
+#pragma unroll 1
+    for (int a = 0; a <= r; ++a)
+      if (row_keeps(p, row, h, x.row0 + r, x.row0 + a, row.count - 1)) kept |= __ballot(x.there && x.rel == a);
+    if (rel == r) seen &= kept;
+  }
+  return seen;
+}
+// A score tile of 16 tokens (the piece of index t) without those that are not attended.
+__device__ __forceinline__ void mask_scores(f32x4& s, uint64_t seen, int t, int g) {
+  const uint32_t mine = (uint32_t)(seen >> (32 * (t / 2))) >> (16 * (t % 2) + 4 * g);
+#pragma unroll
+  for (int e = 0; e < 4; ++e) s[e] = mine >> e & 1 ? s[e] : kNegInf;
+}
+
+// What a query does not attend stays out of its result whatever it holds; but its probability of 0 times an infinity or NaN in V is none.  Where
+// some query does not attend some token of a unit and V holds such values, they are taken out of V, and which of them a query attends is found by
+// products of ones and zeros and kept until the end, when they decide the result.
+//
+// any_odd: whether one of these bf16 pairs is not finite (an exponent field of ones carries into its value's sign)
+template <int KK>
+__device__ __forceinline__ uint32_t odd_bits(const u32x4 (&v)[KK]) {
+  uint32_t top = 0;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) top |= (v[kk][e] & 0x7fff7fffu) + 0x00800080u;
+  return top & 0x80008000u;
+}
+// For a tile of 16 queries and 32 tokens of V in LDS (transposed reads at v_read; seen: bits of the 32): ors into found[feature tile * 64 + lane] a byte to
+// each of the lane's four features: 1 infinity, 2 minus infinity, 4 NaN.
+template <int D>
+__device__ __forceinline__ void count_odd(uint32_t v_read, uint32_t seen, uint32_t* found, uint32_t* any, int lane) {
+  const uint32_t mine = seen >> (4 * (lane >> 4));  // tokens 4 g .. and 16 + 4 g ..
+  u32x4 w;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) w[e] = ((mine >> (16 * (e / 2) + 2 * (e % 2))) & 1) * 0x3f80u + ((mine >> (16 * (e / 2) + 2 * (e % 2) + 1)) & 1) * 0x3f800000u;
+#pragma unroll 1
+  for (int i = 0; i < 3 * (D / 16); ++i) {
+    const int ft = i / 3, kind = i % 3;
+    auto ones = [&](uint32_t x) { return (kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u) ? 0x3f80u : 0u; };
+    u32x4 vf = lds_read_tr2(v_read + 32 * ft, v_read + 32 * ft, 0, 16 * ChunkTile<D>::RB);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) vf[e] = ones(vf[e] & 0xffffu) | ones(vf[e] >> 16) << 16;
+    const f32x4 count = mfma16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, w), f32x4{});
+    uint32_t x = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) x |= (count[e] > 0.f ? 1u : 0u) << (8 * e + kind);
+    if (x) {
+      atomicOr(&found[ft * 64 + lane], x);
+      *any = 1;
+    }
+  }
+}
+// Words of V without what is not finite.
+__device__ __forceinline__ void clean_words(uint32_t* words, int n, int lane) {
+#pragma unroll 1
+  for (int i = lane; i < n; i += 64) {
+    const uint32_t x = words[i];
+    words[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+  }
+}
+// The results that found bytes stand for, in place of the sums.
+__device__ __forceinline__ void put_odd(f32x4& acc, uint32_t found) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t x = found >> (8 * e) & 7;
+    if (x) acc[e] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
+  }
+}
+
+// Rows 16 t .. 16 t + 15 of drafted K or V, a lane's quarter of row c; a node that is not there may hold anything, nobody attends it, and it is
+// not fetched.
+template <class ROWS, int KK>
+__device__ __forceinline__ void draft_rows(const CacheAttnParams& p, const uint16_t* of, uint64_t nodes, int b, int h, int t, int c, int g, u32x4 (&x)[KK]) {
+  const bool here = nodes >> (16 * t + c) & 1;
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    x[kk] = here ? *reinterpret_cast<const u32x4*>(of + b * p.kv_ss + h * p.kv_sh + (16 * t + c) * p.kv_sn + ROWS::feature(kk, g)) : u32x4{};
+}
+
+// A query's result, or its part of a split: eight features from d.
+template <int D>
+__device__ __forceinline__ void put_result(const CacheAttnParams& p, int b, int h, int node, int split, int d, const float (&o)[8], float m, float l) {
+  const int64_t row = ((int64_t)b * p.heads + h) * p.nodes + node;
+  if (p.num_splits == 1) {
+    bf16x8 out;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) out[e] = (__bf16)(l == 0.f ? 0.f : o[e] / l);
+    *reinterpret_cast<bf16x8*>(p.o + b * p.q_ss + h * p.q_sh + node * p.q_sn + d) = out;
+    if (d == 0 && p.lse) p.lse[row] = l == 0.f ? kNegInf : m * p.scale + __logf(l);
+  } else {
+    f32x4* const to = reinterpret_cast<f32x4*>(p.part_acc + (row * p.num_splits + split) * D + d);
+    to[0] = f32x4{o[0], o[1], o[2], o[3]};
+    to[1] = f32x4{o[4], o[5], o[6], o[7]};
+    if (d == 0) {
+      p.part_ml[(row * p.num_splits + split) * 2] = m;
+      p.part_ml[(row * p.num_splits + split) * 2 + 1] = l;
+    }
+  }
+}
+
+// The launch for more than 16 nodes (all but the merge of splits).
+hipError_t launch_cache_attn_shared(const CacheAttnParams& p, hipStream_t stream);
+
+}  // namespace s2

@@ -1,0 +1,266 @@
+// Attention over a paged cache for more than 16 queries to a sequence (see cache_attn_kernel.hip for the mathematics and the operands' layouts).
+//
+// A tile of 16 queries needs 32 accumulators a lane (D = 128), so that one wavefront holds two tiles at most without spilling; and a wavefront to each
+// tile with K and V of its own would fetch and dequantise the cache once per tile.  So the four wavefronts of a workgroup share a unit of 64 tokens: each
+// fetches a piece of 16 of them, brings it to bf16 once and writes its K and V rows into LDS (ChunkTile: row reads and transpose reads of these
+// fragments without bank conflicts); then each takes one tile of queries (QT = 4), or one of two tiles and half of the tokens (QT = 2), against the
+// whole tile.  A unit costs 32 KB of LDS writes and 64 or 128 KB of reads (D = 128): 0.35 or 0.6 us of a compute unit, next to 1.35 us for its bytes to come
+// from HBM in bf16, 0.70 in 8 bits and 0.36 in 4.  The next unit's bytes are on their way while this one is worked on; two barriers a unit, whose waits
+// other workgroups of the compute unit fill.
+#include <hip/hip_runtime.h>
+
+#include "cache_attn.h"
+#include "config.h"
+
+namespace s2 {
+
+namespace {
+
+template <int D, int FMT, int QT, bool SMALL>
+__global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAttnParams p) {
+  using Rows = CacheRows<D, FMT>;
+  using Tile = ChunkTile<D>;
+  constexpr int W = 4, KK = D / 32, FT = D / 16;
+  constexpr int KH = W / QT;          // wavefronts that share a tile of queries, each with its part of the tokens
+  constexpr int NP = 4 / KH;          // pieces of 16 tokens to a wavefront
+  constexpr int RS = D + 4;           // floats to a row where results are turned
+  static_assert(W * 16 * RS * 4 <= 2 * Tile::kBytes, "the wavefronts' sums fit where K and V were");
+
+  __shared__ __align__(16) uint16_t sh_kv[2][Tile::kElems];
+  __shared__ float sh_m[W][16], sh_l[W][16];
+  __shared__ uint32_t sh_odd[QT * FT * 64];  // (count_odd)
+  __shared__ uint32_t sh_any_odd, sh_unit_odd[2];
+
+  const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int qt = wave % QT, kh = wave / QT;
+  const int item = blockIdx.x;
+  const int bh = item / p.by_splits, split = item - bh * p.num_splits;
+  const int b = bh / p.by_heads, h = bh - b * p.heads;
+  const float cl = p.scale_log2e;
+
+  int L = load_const<int32_t>(p.seq_lens + b);
+  L = min(max(L, 0), p.max_len);
+  const Nodes nodes = nodes_of(p, b, L, lane);
+  // the query of my column
+  const int node = 16 * qt + c;
+  const int rel_q = __shfl(nodes.rel, node, 64);
+  const bool there_q = nodes.all >> node & 1;
+  bf16x8 qf[KK];  // (features as K lies in LDS: 32 kk + 8 g ..)
+#pragma unroll
+  for (int kk = 0; kk < KK; ++kk)
+    qf[kk] = there_q ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + node * p.q_sn + 32 * kk + 8 * g) : bf16x8{};
+
+  for (int i = tid; i < QT * FT * 64; i += 64 * W) sh_odd[i] = 0;
+  if (tid == 0) sh_any_odd = sh_unit_odd[0] = sh_unit_odd[1] = 0;
+
+  f32x4 acc[FT];
+  float m_run = kNegInf, l_run = 0.f;
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) acc[ft] = f32x4{};
+
+  const uint32_t at_k = lds_addr(sh_kv[0]), at_v = lds_addr(sh_kv[1]);
+  const uint32_t write = (16 * wave + c) * Tile::RB;
+  const uint32_t k_read = at_k + Tile::row_lane(lane), v_read = at_v + Tile::tr_lane(lane);
+  const int all_rows = (1 << nodes.n_rows) - 1;
+  Walk<SMALL> walk(p, b, h, L, nodes, split, 0, 1, split == p.num_splits - 1 && nodes.all);
+
+  typename Rows::Part kr, vr;
+  // My piece of a unit.
+  auto load = [&](const Unit<SMALL>& w, const uint8_t* pool, const uint8_t* scales, const uint16_t* drafted, typename Rows::Part& x) __attribute__((always_inline)) {
+    if (w.drafts) {
+      if constexpr (!Rows::kScaled) {
+        u32x4 rows[KK];
+        draft_rows<Rows>(p, drafted, nodes.all, b, h, wave, c, g, rows);
+        Rows::take(x, rows);
+      }
+      return;  // (else fetched where they are used)
+    }
+    int page = w.page[0], skip = w.skip[0], rows = w.rows[0];
+    if (SMALL) {
+      page = skip = rows = 0;
+#pragma unroll
+      for (int i = 0; i < Unit<SMALL>::NB; ++i) {  // (by masks: an index would have the unit in memory)
+        const int me = -(int)(wave == i);
+        page |= w.page[i] & me;
+        skip |= w.skip[i] & me;
+        rows |= w.rows[i] & me;
+      }
+    }
+    const uint8_t* const at = pool + page * p.c.page + skip * p.c.tok;
+    const uint8_t* const scale_at = Rows::kScaled ? scales + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
+    Rows::load(x, at, scale_at, rows, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, g);
+  };
+  auto put = [&](const Unit<SMALL>& w, const typename Rows::Part& x, const uint16_t* drafted, uint32_t to) __attribute__((always_inline)) {
+    u32x4 rows[KK];
+    if (Rows::kScaled && w.drafts)
+      draft_rows<Rows>(p, drafted, nodes.all, b, h, wave, c, g, rows);
+    else
+      Rows::operands(x, g, rows);
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk) *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + write + 2 * Rows::feature(kk, g)) = rows[kk];
+    return odd_bits(rows);
+  };
+  // (what it has asked of the LDS is done before a wavefront is past it; loads from memory stay on their way)
+  auto barrier = [&]() __attribute__((always_inline)) {
+    wait_lds();
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+  };
+
+  Unit<SMALL> w;
+  bool more = walk.next(w);
+  if (more) {
+    load(w, p.c.k, p.c.ks, p.k_draft, kr);
+    load(w, p.c.v, p.c.vs, p.v_draft, vr);
+  }
+  for (int turn = 0; more; turn ^= 1) {
+    Unit<SMALL> next;
+    more = walk.next(next);
+    bool some, mixed;
+    unit_masks(w, all_rows, some, mixed);
+    barrier();  // nobody reads the unit before any more
+    (void)put(w, kr, p.k_draft, at_k);
+    const uint32_t odd = put(w, vr, p.v_draft, at_v);
+    if (mixed && odd) sh_unit_odd[turn] = 1;
+    if (tid == 0) sh_unit_odd[turn ^ 1] = 0;
+    if (more) {
+      load(next, p.c.k, p.c.ks, p.k_draft, kr);
+      load(next, p.c.v, p.c.vs, p.v_draft, vr);
+    }
+    barrier();
+
+    f32x4 s[NP];
+#pragma unroll
+    for (int t = 0; t < NP; ++t)
+#pragma unroll
+      for (int kk = 0; kk < KK; ++kk) {
+        const bf16x8 k = __builtin_bit_cast(bf16x8, lds_read16(k_read + 16 * NP * kh * Tile::RB, Tile::row_off(t, kk)));
+        s[t] = mfma16(k, qf[kk], kk ? s[t] : f32x4{});
+      }
+    uint64_t seen = 0;
+    if (some) {
+      seen = w.drafts ? drafts_seen(p, nodes, h, node, rel_q) : unit_seen(w, rel_q);
+      seen >>= 16 * NP * kh;
+#pragma unroll
+      for (int t = 0; t < NP; ++t) mask_scores(s[t], seen, t, g);
+    }
+    float mx = kNegInf;
+#pragma unroll
+    for (int t = 0; t < NP; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
+    mx = max_halves(max_rows(mx));
+    const float m_new = fmaxf(m_run, mx);
+    const float mc = m_new == kNegInf ? 0.f : m_new * cl;
+    if (__any(m_new > m_run)) {
+      const float alpha = fast_exp2(m_run * cl - mc);  // (-inf before the first token: 0)
+      l_run *= alpha;
+      m_run = m_new;
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) acc[ft] *= alpha;
+    }
+#pragma unroll
+    for (int t = 0; t < NP; ++t)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        s[t][e] = fast_exp2(__builtin_fmaf(s[t][e], cl, -mc));
+        l_run += s[t][e];
+      }
+    if (mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
+#pragma unroll 1
+      for (int u = 0; u < NP / 2; ++u)
+        count_odd<D>(v_read + (16 * NP * kh + 32 * u) * Tile::RB, (uint32_t)(seen >> (32 * u)), sh_odd + qt * FT * 64, &sh_any_odd, lane);
+      barrier();
+      clean_words(reinterpret_cast<uint32_t*>(sh_kv[1]) + 16 * wave * Tile::RB / 4, 16 * Tile::RB / 4, lane);
+      barrier();
+    }
+#pragma unroll
+    for (int u = 0; u < NP / 2; ++u) {
+      const f32x4 lo = s[2 * u], hi = s[2 * u + 1];
+      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack2(lo[0], lo[1]), pack2(lo[2], lo[3]), pack2(hi[0], hi[1]), pack2(hi[2], hi[3])});
+      const uint32_t from = v_read + 16 * NP * kh * Tile::RB;
+#pragma unroll
+      for (int ft = 0; ft < FT; ++ft) {
+        const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(from, from, Tile::tr_off(u, ft), Tile::tr_off(u, ft) + 16 * Tile::RB));
+        acc[ft] = mfma16(vf, pf, acc[ft]);
+      }
+    }
+    w = next;
+  }
+  if (p.missing && tid == 0 && walk.n_missing > 0) atomicAdd(p.missing, walk.n_missing);
+
+  // results from query-on-lane to rows, through where K and V were
+  l_run = sum_groups(l_run);
+  if (g == 0) {
+    sh_m[wave][c] = there_q ? m_run : kNegInf;
+    sh_l[wave][c] = there_q ? l_run : 0.f;
+  }
+  __syncthreads();
+  float m = kNegInf;
+#pragma unroll
+  for (int i = 0; i < KH; ++i) m = fmaxf(m, sh_m[qt + QT * i][c]);
+  // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
+  const float weight = sh_l[wave][c] == 0.f ? 0.f : KH == 1 ? 1.f : fast_exp2((m_run - m) * cl);
+  if (sh_any_odd && kh == 0) {
+#pragma unroll
+    for (int ft = 0; ft < FT; ++ft) put_odd(acc[ft], sh_odd[(qt * FT + ft) * 64 + lane]);
+  }
+  float* const sums = reinterpret_cast<float*>(sh_kv[0]);
+  float* const mine = sums + (16 * wave + c) * RS + 4 * g;
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] * weight : f32x4{};
+  __syncthreads();
+  constexpr int TPR = D / 8;  // threads to a query, eight features each
+  for (int i = tid / TPR; i < 16 * QT && i < p.nodes; i += 64 * W / TPR) {
+    const int d = 8 * (tid % TPR), tile = i / 16, q = i % 16;
+    float mt = kNegInf, l = 0.f, o[8];
+#pragma unroll
+    for (int k = 0; k < KH; ++k) mt = fmaxf(mt, sh_m[tile + QT * k][q]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int k = 0; k < KH; ++k) {
+      const int of = tile + QT * k;
+      if (sh_l[of][q] != 0.f) l += KH == 1 ? sh_l[of][q] : sh_l[of][q] * fast_exp2((sh_m[of][q] - mt) * cl);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += sums[(16 * of + q) * RS + d + e];
+    }
+    put_result<D>(p, b, h, i, split, d, o, mt, l);
+  }
+}
+
+template <int D, int FMT, int QT>
+void launch_blocks(const CacheAttnParams& p, hipStream_t stream) {
+  const dim3 grid(p.nseq * p.heads * p.num_splits), block(256);
+  if (p.block_size < 64)
+    hipLaunchKernelGGL((cache_attn_shared_kernel<D, FMT, QT, true>), grid, block, 0, stream, p);
+  else
+    hipLaunchKernelGGL((cache_attn_shared_kernel<D, FMT, QT, false>), grid, block, 0, stream, p);
+}
+
+template <int D, int FMT>
+hipError_t launch_tiles(const CacheAttnParams& p, hipStream_t stream) {
+  if (p.nodes <= 32)
+    launch_blocks<D, FMT, 2>(p, stream);
+  else
+    launch_blocks<D, FMT, 4>(p, stream);
+  return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_dim(const CacheAttnParams& p, hipStream_t stream) {
+  switch (p.c.format) {
+    case S2_KV_BF16: return launch_tiles<D, S2_KV_BF16>(p, stream);
+    case S2_KV_MXFP8: return launch_tiles<D, S2_KV_MXFP8>(p, stream);
+    default: return launch_tiles<D, S2_KV_MXFP4>(p, stream);
+  }
+}
+
+}  // namespace
+
+hipError_t launch_cache_attn_shared(const CacheAttnParams& p, hipStream_t stream) {
+  return p.c.head_dim == 128 ? launch_dim<128>(p, stream) : launch_dim<64>(p, stream);
+}
+
+}  // namespace s2

@@ -83,6 +83,15 @@ struct CacheRows {
     }
   }
 
+  // bf16 rows that are operands already
+  __device__ static __forceinline__ void take(Part& p, const u32x4 (&rows)[kFrags]) {
+    static_assert(!kScaled, "");
+#pragma unroll
+    for (int kk = 0; kk < kFrags; ++kk)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) p.x[4 * kk + e] = rows[kk][e];
+  }
+
   // its operands
   __device__ static __forceinline__ void operands(const Part& p, int g, u32x4 (&out)[kFrags]) {
     if constexpr (FMT == S2_KV_BF16) {
