@@ -97,31 +97,35 @@ struct Walk {
         u_now = even * split + rest * split / p.by_splits + first;
         u_end = even * (split + 1) + rest * (split + 1) / p.by_splits;
       }
+      // (all lookups of a unit together: one after the other each is a trip to the L2 that the wavefront waits for)
+      int blk[NB], page[NB], skip[NB], in_list[NB];
+#pragma unroll
+      for (int i = 0; i < NB; ++i) {
+        const int l = 64 * u_now + 16 * i;
+        in_list[i] = l >> sh;
+        skip[i] = l & (S - 1);
+        blk[i] = rb.block(SMALL ? min(in_list[i], rb.count - 1) : in_list[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < NB; ++i) page[i] = load_const<int32_t>(table + blk[i]);
       int any = 0;
 #pragma unroll
       for (int i = 0; i < NB; ++i) {
-        const int l = 64 * u_now + 16 * i, n = l >> sh, skip = l & (S - 1);
-        const bool inside = !SMALL || n < rb.count;
-        const int blk = rb.block(inside ? n : 0);
-        int rows = inside ? min(max(L - (blk * S + skip), 0), kTokens) : 0, bits = 1 << r_now;
+        int rows = min(max(L - (blk[i] * S + skip[i]), 0), kTokens), bits = 1 << r_now;
+        if (SMALL && in_list[i] >= rb.count) rows = 0;
         if (n_rows > 1 && rows > 0) {
 #pragma unroll 1
           for (int r = 0; r < n_rows; ++r) {
-            if (r == r_now || !row_keeps(p, row_blocks(p, h, row0 + r), h, row0 + r, blk, n)) continue;
+            if (r == r_now || !row_keeps(p, row_blocks(p, h, row0 + r), h, row0 + r, blk[i], in_list[i])) continue;
             if (r < r_now) rows = 0;  // (read in that row's turn)
             bits |= 1 << r;
           }
         }
-        int page = 0;
-        if (rows > 0) {
-          page = load_const<int32_t>(table + blk);
-          if (page < 0 || page >= p.c.num_pages) {
-            n_missing += skip == 0;
-            rows = 0;
-          }
-        }
-        w.page[i] = page;
-        w.skip[i] = skip;
+        const bool held = page[i] >= 0 && page[i] < p.c.num_pages;
+        n_missing += rows > 0 && !held && skip[i] == 0;
+        rows = held ? rows : 0;
+        w.page[i] = held ? page[i] : 0;
+        w.skip[i] = skip[i];
         w.rows[i] = rows;
         w.bits[i] = bits;
         any |= rows;

@@ -228,35 +228,60 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
   put_result<D>(p, b, h, i, split, d, o, mt, l);
 }
 
-// Merges the splits: D/8 lanes to a row of the result.
+// Merges the splits, a wavefront to a row of the result: lane i holds the weight of split i, groups of D/4 lanes add up the splits of their own, four
+// of them requested at a time together with the (max, sum) pairs.
 template <int D>
 __global__ __launch_bounds__(256) void cache_attn_merge_kernel(const CacheAttnParams p) {
-  constexpr int TPR = D / 8;
-  const int64_t row = (int64_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  const int d = 8 * (threadIdx.x % TPR);
+  constexpr int LPR = D / 4, NG = 64 / LPR, NP = 4;
+  const int lane = threadIdx.x & 63, g = lane / LPR, c = lane % LPR, n = p.num_splits;
+  const int64_t row = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (row >= (int64_t)p.nseq * p.heads * p.nodes) return;
-  const float* const ml = p.part_ml + row * p.num_splits * 2;
-  const float* const part = p.part_acc + row * p.num_splits * D + d;
-  float m = kNegInf;
-  for (int i = 0; i < p.num_splits; ++i) m = fmaxf(m, ml[2 * i]);
-  float l = 0.f, o[8];
+  const float* const ml = p.part_ml + row * n * 2;
+  const f32x4* const part = reinterpret_cast<const f32x4*>(p.part_acc) + row * n * LPR + c;
+  f32x4 x[NP];
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = 0.f;
-  for (int i = 0; i < p.num_splits; ++i) {
-    if (ml[2 * i + 1] == 0.f) continue;  // no token
-    const float weight = fast_exp2((ml[2 * i] - m) * p.scale_log2e);
-    l += ml[2 * i + 1] * weight;
+  for (int i = 0; i < NP; ++i) x[i] = part[(int64_t)min(g + NG * i, n - 1) * LPR];
+  const float ms = lane < n ? ml[2 * lane] : kNegInf, ls = lane < n ? ml[2 * lane + 1] : 0.f;
+  float m = ms;
+  m = fmaxf(m, of_neighbour<1>(m));
+  m = fmaxf(m, of_neighbour<2>(m));
+  m = fmaxf(m, of_neighbour<4>(m));
+  m = max_halves(max_rows(fmaxf(m, of_neighbour<8>(m))));
+  const float weight = ls == 0.f ? 0.f : fast_exp2((ms - m) * p.scale_log2e);  // (no sum: no token)
+  float l = ls * weight;
+  l += of_neighbour<1>(l);
+  l += of_neighbour<2>(l);
+  l += of_neighbour<4>(l);
+  l += of_neighbour<8>(l);
+  l = sum_halves(sum_rows(l));
+  f32x4 a = f32x4{};
+  for (int s0 = 0;;) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] += part[(int64_t)i * D + e] * weight;
+    for (int i = 0; i < NP; ++i) {
+      const int s = s0 + g + NG * i;
+      const float of = __shfl(weight, s & 63, 64);
+      if (s < n) a += x[i] * of;
+    }
+    s0 += NG * NP;
+    if (s0 >= n) break;
+#pragma unroll
+    for (int i = 0; i < NP; ++i) x[i] = part[(int64_t)min(s0 + g + NG * i, n - 1) * LPR];
   }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    float y = a[e];
+    if (LPR == 16) y = sum_rows(y);
+    a[e] = sum_halves(y);
+  }
+  if (lane >= LPR) return;
   const int64_t bh = row / p.nodes;
   const int node = (int)(row - bh * p.nodes);
   const int64_t b = bh / p.heads, h = bh - b * p.heads;
-  bf16x8 out;
+  bf16x4 out;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) out[e] = (__bf16)(l == 0.f ? 0.f : o[e] / l);
-  *reinterpret_cast<bf16x8*>(p.o + b * p.q_ss + h * p.q_sh + node * p.q_sn + d) = out;
-  if (d == 0 && p.lse) p.lse[row] = l == 0.f ? kNegInf : m * p.scale + __logf(l);
+  for (int e = 0; e < 4; ++e) out[e] = (__bf16)(l == 0.f ? 0.f : a[e] / l);
+  *reinterpret_cast<bf16x4*>(p.o + b * p.q_ss + h * p.q_sh + node * p.q_sn + 4 * c) = out;
+  if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? kNegInf : m * p.scale + __logf(l);
 }
 
 template <int D, int FMT>
@@ -282,8 +307,8 @@ hipError_t launch_dim(const CacheAttnParams& p, hipStream_t stream) {
     e = hipGetLastError();
   }
   if (e != hipSuccess || p.num_splits == 1) return e;
-  const int64_t rows = (int64_t)p.nseq * p.heads * p.nodes, per = 256 / (D / 8);
-  hipLaunchKernelGGL((cache_attn_merge_kernel<D>), dim3((unsigned)((rows + per - 1) / per)), dim3(256), 0, stream, p);
+  const int64_t rows = (int64_t)p.nseq * p.heads * p.nodes;
+  hipLaunchKernelGGL((cache_attn_merge_kernel<D>), dim3((unsigned)((rows + 3) / 4)), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
