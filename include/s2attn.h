@@ -468,7 +468,7 @@ int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void
 int s2_kv_read_paged(const s2_paged_cache* c, const s2_kv_read_args* a, void* stream);
 
 /* s2_attn_decode_paged / s2_attn_decode_paged_layout over a cache of any format (over S2_KV_BF16, with q and o contiguous, it is that
- * call).  The mask's block size and heads are the cache's.  Workspace as for s2_attn_decode with max_len = max_blocks * block_size.
+ * call).  The mask's block size and heads are the cache's.  Workspace: s2_attn_tree_workspace_bytes with nodes = 1.
  * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
 int s2_attn_decode_paged_cache(const s2_layout_params* p, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
                                void* workspace, size_t workspace_bytes, void* stream);
@@ -482,7 +482,8 @@ int s2_attn_decode_paged_cache_layout(const s2_layout* layout, const s2_paged_ca
  * its lse -inf, and its q, k, v are not looked at.  What a node does not attend stays out of its result whatever it
  * holds.  Kept blocks that are not resident contribute nothing and are counted, as in s2_attn_decode_paged.
  * workspace: s2_attn_tree_workspace_bytes(..., max_blocks * block_size, num_splits) bytes, DEVICE, 256-byte aligned, contents
- * undefined on entry and exit.  With a layout, it covers the cache.
+ * undefined on entry and exit (with num_splits = 0 less will do, down to the size for one split: the call then takes fewer splits).  With a
+ * layout, it covers the cache.
  * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
 int s2_attn_tree_paged(const s2_layout_params* p, const s2_paged_cache* c, const s2_tree_args* a, float scale,
                        void* workspace, size_t workspace_bytes, void* stream);

@@ -831,14 +831,24 @@ int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, cons
   return hip_ok(s2::launch_kv_rows(p, (int)grid, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
-// The splits of a call over a cache when the caller leaves them to the library: about two workgroups to a compute unit, and a
-// unit of 64 tokens at least to each of a workgroup's wavefronts.
-int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, int nseq, int heads, int max_len) {
+// The most splits that the library takes for a call over a cache of any format.
+int most_cache_splits(int64_t pairs, int64_t max_len) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, (1024 + pairs - 1) / pairs, (max_len + 127) / 128}));
+}
+
+// The splits of a call over a cache when the caller leaves them to the library.
+// A decode step over 8 or 4 bits: as many workgroups of eight wavefronts as there are compute units, while each wavefront but one in four has a unit of 64
+// tokens (e4m3, D = 128, us: 8 heads of 47 units in 4 splits 13.2, 8 10.0, 16 9.0; 32 in 4 13.6, 8 11.2, 16 11.5; of 19 units in 4 10.1, 8 8.7, 16 10.3;
+// 64 of 31 to 46 units in 2 20.0, 4 15.3, 8 15.7), and else four workgroups of four to a compute unit where that leaves 24 units to each (512
+// of up to 46 units in one split 62.6, in two 65.6).
+// Trees: about two workgroups to a compute unit, and a unit at least to each of a workgroup's wavefronts.
+int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, bool tree, int nseq, int heads, int max_len) {
   const int S = lp->block_size;
   const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / S, nullptr, 0);
   const int64_t units = (blocks * S + 63) / 64, pairs = (int64_t)nseq * heads;
-  const int64_t want = std::min<int64_t>((512 + pairs - 1) / pairs, units / 4);
-  return (int)std::max<int64_t>(1, std::min<int64_t>(want, s2_attn_decode_default_splits(nseq, heads, max_len)));
+  const int64_t want = tree ? std::min<int64_t>((512 + pairs - 1) / pairs, units / 4)
+                            : std::max(std::min<int64_t>(s2::kCacheWideGroups / pairs, units / 2), std::min<int64_t>(1024 / pairs, units / 24));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(want, most_cache_splits(pairs, max_len)));
 }
 
 int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, s2::CacheAttnParams& p, float scale,
@@ -860,9 +870,12 @@ int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
       (reinterpret_cast<uintptr_t>(p.parents) & 3u) != 0 || (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0 ||
       (reinterpret_cast<uintptr_t>(p.missing) & 3u) != 0)
     return S2_ERR_ALIGN;
-  const int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, c->nseq, c->heads, max_len);
+  int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, p.parents != nullptr, c->nseq, c->heads, max_len);
   if ((int64_t)c->nseq * c->heads * splits > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
-  const size_t need = s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, splits);
+  auto bytes = [&](int n) { return s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, n); };
+  // (a smaller workspace is for fewer splits, where the caller has not asked for a number)
+  while (num_splits == 0 && splits > 1 && bytes(splits) > workspace_bytes) --splits;
+  const size_t need = bytes(splits);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < need) return S2_ERR_WORKSPACE;
   p.part_acc = static_cast<float*>(workspace);
   p.part_ml = p.part_acc + (size_t)c->nseq * c->heads * p.nodes * splits * c->head_dim;
@@ -1000,7 +1013,7 @@ int s2_attn_tree_paged_layout(const s2_layout* layout, const s2_paged_cache* c, 
 
 size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, int32_t head_dim, int32_t max_len, int32_t num_splits) {
   if (nseq < 1 || heads < 1 || nodes < 1 || head_dim < 1) return 0;
-  if (num_splits <= 0) num_splits = s2_attn_decode_default_splits(nseq, heads, max_len);
+  if (num_splits <= 0) num_splits = most_cache_splits((int64_t)nseq * heads, max_len);
   const size_t items = (size_t)nseq * heads * nodes * num_splits;
   return ((items * (head_dim + 2) * sizeof(float) + 255) / 256) * 256;
 }

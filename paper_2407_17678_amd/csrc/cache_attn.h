@@ -265,6 +265,8 @@ __device__ __forceinline__ void put_result(const CacheAttnParams& p, int b, int 
   }
 }
 
+// The launch of a decode step over 8 or 4 bits (all but the merge of splits).
+hipError_t launch_cache_decode(const CacheAttnParams& p, hipStream_t stream);
 // The launch for more than 16 nodes (all but the merge of splits).
 hipError_t launch_cache_attn_shared(const CacheAttnParams& p, hipStream_t stream);
 

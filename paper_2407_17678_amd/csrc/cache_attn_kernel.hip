@@ -296,7 +296,9 @@ void launch_blocks(const CacheAttnParams& p, hipStream_t stream) {
 template <int D>
 hipError_t launch_dim(const CacheAttnParams& p, hipStream_t stream) {
   hipError_t e;
-  if (p.nodes > 16) {
+  if (!p.parents && p.c.format != S2_KV_BF16) {
+    e = launch_cache_decode(p, stream);
+  } else if (p.nodes > 16) {
     e = launch_cache_attn_shared(p, stream);
   } else {
     switch (p.c.format) {

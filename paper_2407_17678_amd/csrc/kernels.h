@@ -207,6 +207,8 @@ hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
 // The workgroups of a launch over rows of a cache (sets the tile fields), and the launch.
 int64_t kv_rows_tiles(KvRowsParams& p, int nseq);
 hipError_t launch_kv_rows(const KvRowsParams& p, int grid, hipStream_t stream);
+// Up to so many workgroups a decode step over 8 or 4 bits takes eight wavefronts to each instead of four.
+constexpr int kCacheWideGroups = 256;
 hipError_t launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);
 
 }  // namespace s2

@@ -113,6 +113,29 @@ struct CacheRows {
       for (int kk = 0; kk < kFrags; ++kk) out[kk] = values4(p.x[kk], s);
     }
   }
+
+  // acc[8 * kk + e] += pr * (feature e of operand kk), in 32 bits
+  __device__ static __forceinline__ void add_times(const Part& p, int g, float pr, float (&acc)[D / 4]) {
+    static_assert(kScaled, "");
+    const uint32_t mine = p.scales >> (8 * (FMT == S2_KV_MXFP4 && D == 128 ? g : g >> 1));
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {  // pairs
+      typedef float f32x2_ __attribute__((ext_vector_type(2)));
+      const float s = scale_of((FMT == S2_KV_MXFP8 ? mine >> (16 * (i / 8)) : mine) & 255);
+      f32x2_ v;
+      if constexpr (FMT == S2_KV_MXFP8) {
+        v = i % 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(p.x[i / 2], s, true) : __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(p.x[i / 2], s, false);
+      } else {
+        const uint32_t x = p.x[i / 4];
+        v = i % 4 == 0   ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, s, 0)
+            : i % 4 == 1 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, s, 1)
+            : i % 4 == 2 ? __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, s, 2)
+                         : __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(x, s, 3);
+      }
+      acc[2 * i] = __builtin_fmaf(pr, v[0], acc[2 * i]);
+      acc[2 * i + 1] = __builtin_fmaf(pr, v[1], acc[2 * i + 1]);
+    }
+  }
 };
 
 }  // namespace s2

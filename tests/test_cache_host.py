@@ -158,7 +158,10 @@ def test_workspaces():
     f = B.s2_attn_tree_workspace_bytes
     assert f(2, 3, 4, 128, 448, 5) == (2 * 3 * 4 * 5 * 130 * 4 + 255) // 256 * 256
     assert f(2, 3, 1, 64, 448, 3) == B.s2_attn_decode_workspace_bytes(2, 3, 64, 448, 3)
-    assert f(2, 3, 4, 128, 40000, 0) == f(2, 3, 4, 128, 40000, B.s2_attn_decode_default_splits(2, 3, 40000))
+    assert f(2, 3, 4, 128, 40000, 0) == f(2, 3, 4, 128, 40000, 64) and f(64, 8, 4, 128, 40000, 0) == f(64, 8, 4, 128, 40000, 2)
+    assert f(1, 1, 4, 128, 256, 0) == f(1, 1, 4, 128, 256, 2) and f(1000, 8, 4, 128, 256, 0) == f(1000, 8, 4, 128, 256, 1)
+    for nseq, heads, length in ((1, 1, 100), (1, 32, 4096), (7, 13, 30000), (300, 40, 1 << 20)):  # enough for the bf16 call as well
+        assert f(nseq, heads, 1, 128, length) >= B.s2_attn_decode_workspace_bytes(nseq, heads, 128, length)
     assert f(0, 3, 4, 128, 448, 5) == f(2, 3, 0, 128, 448, 5) == f(2, -1, 4, 128, 448, 5) == 0
     assert f(64, 32, 64, 128, 1 << 20, 64) == 64 * 32 * 64 * 64 * 130 * 4
 
