@@ -53,113 +53,138 @@ __device__ __forceinline__ Nodes nodes_of(const CacheAttnParams& p, int b, int L
   return x;
 }
 
+// The kernel's parameters as they lie in memory, for what is done once or rarely: read there they do not occupy scalar registers in between (which the
+// loops of these kernels have none to spare of: spilled to lanes, about 100 to a unit of 64 tokens, they took a third of its time).
+__device__ __forceinline__ const CacheAttnParams& params_in_memory() {
+  auto at = (const __attribute__((address_space(4))) CacheAttnParams*)(uintptr_t)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(at));
+  return *(const CacheAttnParams*)at;
+}
+
 // 64 tokens: of one block, or (SMALL: blocks of 16 or 32) four pieces of 16 of the list's blocks; or the drafted ones.
 template <bool SMALL>
 struct Unit {
   static constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB;
-  int page[NB], skip[NB], rows[NB], bits[NB];  // (bits: which block rows keep it)
+  int page[NB];
+  int info[NB];          // tokens to read | block rows that keep it << 8 | tokens of the block before them << 16
+  int my_page, my_info;  // SMALL: of the walk's own piece
   bool drafts;
+  bool some;   // some query may not attend some token
+  bool mixed;  // some query does not attend a token that is there
+  __device__ static int rows(int info) { return info & 255; }
+  __device__ static int bits(int info) { return info >> 8 & 255; }
+  __device__ static int skip(int info) { return info >> 16; }
 };
 
-// The units of a split, block row by block row: each block in the turn of the first row that keeps it.
+// The units of a split, block row by block row: each block in the turn of the first row that keeps it.  Lanes look them up 64 at a time (SMALL: 16, a
+// lane to a piece), so that a unit costs a few lane reads where it is used: looked up one by one by scalar instructions it is about 150 of them and two
+// trips to the L2, in each wavefront.
 template <bool SMALL>
 struct Walk {
-  const CacheAttnParams& p;
-  const int32_t* table;
-  int h, L, row0, n_rows, split, first, step;  // unit `first` of the split, and every step-th
+  static constexpr int NB = Unit<SMALL>::NB, kTokens = Unit<SMALL>::kTokens, kUnits = 64 / NB;
+  int b, h, L, row0, n_rows, split, first, step, piece;  // unit `first` of the split, and every step-th
   bool drafts_left;
+  int lane;
   int n_missing = 0;
   int r_now = -1, u_now = 0, u_end = 0;
-  RowBlocks rb{};
+  int page = 0, info = 0;            // of this lane's unit (piece)
+  uint64_t live = 0, some = 0, mixed = 0;
 
-  __device__ __forceinline__ Walk(const CacheAttnParams& p_, int b, int h_, int L_, const Nodes& x, int split_, int first_, int step_, bool drafts)
-      : p(p_), table(p_.c.table + ((int64_t)b * p_.heads + h_) * p_.c.max_blocks), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_),
-        first(first_), step(step_), drafts_left(drafts), u_now(-step_) {}
+  __device__ __forceinline__ Walk(int b_, int h_, int L_, const Nodes& x, int split_, int first_, int step_, int piece_, bool drafts, int lane_)
+      : b(b_), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_), first(first_), step(step_), piece(piece_), drafts_left(drafts), lane(lane_) {}
 
-  // The next unit with a token to read.
-  __device__ __forceinline__ bool next(Unit<SMALL>& w) {
-    constexpr int NB = Unit<SMALL>::NB, kTokens = Unit<SMALL>::kTokens;
+  // bit NB * i: whether any of the NB bits from there on is set
+  __device__ static uint64_t of_units(uint64_t pieces) {
+    if (!SMALL) return pieces;
+    pieces |= pieces >> 1;
+    return (pieces | pieces >> 2) & 0x1111111111111111ull;
+  }
+
+  __device__ __forceinline__ void look_up(const CacheAttnParams& p) {
     const int S = p.block_size, sh = p.c.block_shift;
-    w.drafts = false;
-    for (;;) {
-      u_now += step;
-      while (u_now >= u_end) {
-        if (r_now + 1 >= n_rows) {
-          if (!drafts_left) return false;
-          drafts_left = false;
-          w.drafts = true;
-          return true;
-        }
-        ++r_now;
-        rb = row_blocks(p, h, row0 + r_now);
-        const int units = ((rb.count << sh) + 63) >> 6;
-        const int even = units / p.by_splits, rest = units - even * p.num_splits;
-        u_now = even * split + rest * split / p.by_splits + first;
-        u_end = even * (split + 1) + rest * (split + 1) / p.by_splits;
-      }
-      // (all lookups of a unit together: one after the other each is a trip to the L2 that the wavefront waits for)
-      int blk[NB], page[NB], skip[NB], in_list[NB];
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        const int l = 64 * u_now + 16 * i;
-        in_list[i] = l >> sh;
-        skip[i] = l & (S - 1);
-        blk[i] = rb.block(SMALL ? min(in_list[i], rb.count - 1) : in_list[i]);
-      }
-#pragma unroll
-      for (int i = 0; i < NB; ++i) page[i] = load_const<int32_t>(table + blk[i]);
-      int any = 0;
-#pragma unroll
-      for (int i = 0; i < NB; ++i) {
-        int rows = min(max(L - (blk[i] * S + skip[i]), 0), kTokens), bits = 1 << r_now;
-        if (SMALL && in_list[i] >= rb.count) rows = 0;
-        if (n_rows > 1 && rows > 0) {
-#pragma unroll 1
-          for (int r = 0; r < n_rows; ++r) {
-            if (r == r_now || !row_keeps(p, row_blocks(p, h, row0 + r), h, row0 + r, blk[i], in_list[i])) continue;
-            if (r < r_now) rows = 0;  // (read in that row's turn)
-            bits |= 1 << r;
-          }
-        }
-        const bool held = page[i] >= 0 && page[i] < p.c.num_pages;
-        n_missing += rows > 0 && !held && skip[i] == 0;
-        rows = held ? rows : 0;
-        w.page[i] = held ? page[i] : 0;
-        w.skip[i] = skip[i];
-        w.rows[i] = rows;
-        w.bits[i] = bits;
-        any |= rows;
-      }
-      if (any) return true;
+    RowBlocks rb;
+    if (u_now < u_end) rb = row_blocks(p, h, row0 + r_now);
+    while (u_now >= u_end) {
+      if (r_now + 1 >= n_rows) return;
+      ++r_now;
+      rb = row_blocks(p, h, row0 + r_now);
+      const int units = ((rb.count << sh) + 63) >> 6;
+      const int even = units / p.by_splits, rest = units - even * p.num_splits;
+      u_now = even * split + rest * split / p.by_splits + first;
+      u_end = even * (split + 1) + rest * (split + 1) / p.by_splits;
     }
+    const int u = u_now + step * (lane / NB), l = 64 * u + 16 * (lane % NB), n = l >> sh, skip = l & (S - 1);
+    u_now += step * kUnits;
+    const bool inside = u < u_end && n < rb.count;
+    const int blk = inside ? rb.block_of_lane(n) : 0;
+    int rows = inside ? min(max(L - (blk * S + skip), 0), kTokens) : 0, bits = 1 << r_now;
+    if (n_rows > 1) {
+#pragma unroll 1
+      for (int r = 0; r < n_rows; ++r) {
+        if (r == r_now) continue;
+        const RowBlocks other = row_blocks(p, h, row0 + r);
+        if (rows > 0 && row_keeps(p, other, h, row0 + r, blk, n)) {
+          if (r < r_now) rows = 0;  // (read in that row's turn)
+          bits |= 1 << r;
+        }
+      }
+    }
+    page = rows > 0 ? p.c.table[((int64_t)b * p.heads + h) * p.c.max_blocks + blk] : 0;
+    const bool held = page >= 0 && page < p.c.num_pages;
+    n_missing += __popcll(__ballot(rows > 0 && !held && skip == 0));
+    if (!held) page = rows = 0;
+    info = rows | bits << 8 | skip << 16;
+    const int all = (1 << n_rows) - 1;
+    live = of_units(__ballot(rows > 0));
+    some = of_units(__ballot(rows < kTokens || bits != all));
+    mixed = of_units(__ballot(rows > 0 && bits != all));
+  }
+
+  // The next unit with a token to read (AGAIN: the parameters are read from memory).
+  template <bool AGAIN>
+  __device__ __forceinline__ bool next(const CacheAttnParams& p, Unit<SMALL>& w) {
+    w.drafts = false;
+    while (live == 0) {
+      if (u_now >= u_end && r_now + 1 >= n_rows) {
+        if (!drafts_left) return false;
+        drafts_left = false;
+        w.drafts = w.some = w.mixed = true;
+        return true;
+      }
+      look_up(AGAIN ? params_in_memory() : p);
+    }
+    const int i = __builtin_ctzll(live);
+    live &= live - 1;
+    w.some = some >> i & 1;
+    w.mixed = mixed >> i & 1;
+#pragma unroll
+    for (int t = 0; t < NB; ++t) {
+      w.page[t] = __builtin_amdgcn_readlane(page, i + t);
+      w.info[t] = __builtin_amdgcn_readlane(info, i + t);
+    }
+    w.my_page = __builtin_amdgcn_readlane(page, i + (SMALL ? piece : 0));
+    w.my_info = __builtin_amdgcn_readlane(info, i + (SMALL ? piece : 0));
+    return true;
   }
 };
 
-// Tokens of a unit that a query in block row `rel` attends, bits; all of them are attended by all queries unless `some`; some query does not attend a
-// token that is there if `mixed`.
-template <bool SMALL>
-__device__ __forceinline__ void unit_masks(const Unit<SMALL>& w, int all_rows, bool& some, bool& mixed) {
-  some = mixed = w.drafts;
-  if (w.drafts) return;
-#pragma unroll
-  for (int i = 0; i < Unit<SMALL>::NB; ++i) {
-    some |= w.rows[i] < Unit<SMALL>::kTokens || w.bits[i] != all_rows;
-    mixed |= w.rows[i] > 0 && w.bits[i] != all_rows;
-  }
-}
+// Tokens of a unit that a query in block row `rel` attends, bits.
 template <bool SMALL>
 __device__ __forceinline__ uint64_t unit_seen(const Unit<SMALL>& w, int rel) {
   uint64_t seen = 0;
 #pragma unroll
-  for (int i = 0; i < Unit<SMALL>::NB; ++i)
-    if (w.bits[i] >> rel & 1) seen |= (w.rows[i] >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << w.rows[i]) - 1) << (16 * i);
+  for (int i = 0; i < Unit<SMALL>::NB; ++i) {
+    const int rows = Unit<SMALL>::rows(w.info[i]);
+    if (Unit<SMALL>::bits(w.info[i]) >> rel & 1) seen |= (rows >= 64 ? ~(uint64_t)0 : ((uint64_t)1 << rows) - 1) << (16 * i);
+  }
   return seen;
 }
 // Drafted nodes that the query of node `node` attends: it and those above it, in blocks that its row keeps.
-__device__ __forceinline__ uint64_t drafts_seen(const CacheAttnParams& p, const Nodes& x, int h, int node, int rel) {
+__device__ __forceinline__ uint64_t drafts_seen(const Nodes& x, int h, int node, int rel) {
   const uint32_t lo = __shfl((uint32_t)x.above, node, 64), hi = __shfl((uint32_t)(x.above >> 32), node, 64);
   uint64_t seen = (uint64_t)hi << 32 | lo;
   if (x.n_rows == 1) return seen;
+  const CacheAttnParams& p = params_in_memory();
 #pragma unroll 1
   for (int r = 0; r < x.n_rows; ++r) {
     const RowBlocks row = row_blocks(p, h, x.row0 + r);
@@ -236,8 +261,10 @@ __device__ __forceinline__ void put_odd(f32x4& acc, uint32_t found) {
 
 // Rows 16 t .. 16 t + 15 of drafted K or V, a lane's quarter of row c; a node that is not there may hold anything, nobody attends it, and it is
 // not fetched.
-template <class ROWS, int KK>
-__device__ __forceinline__ void draft_rows(const CacheAttnParams& p, const uint16_t* of, uint64_t nodes, int b, int h, int t, int c, int g, u32x4 (&x)[KK]) {
+template <class ROWS, bool V, int KK>
+__device__ __forceinline__ void draft_rows(uint64_t nodes, int b, int h, int t, int c, int g, u32x4 (&x)[KK]) {
+  const CacheAttnParams& p = params_in_memory();
+  const uint16_t* const of = V ? p.v_draft : p.k_draft;
   const bool here = nodes >> (16 * t + c) & 1;
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk)

@@ -43,7 +43,6 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
   const int item = blockIdx.x;
   const int bh = item / p.by_splits, split = item - bh * p.num_splits;
   const int b = bh / p.by_heads, h = bh - b * p.heads;
-  const int T = p.nodes;
   const bool tree = p.parents != nullptr;
   const float cl = p.scale_log2e;
 
@@ -69,17 +68,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
 
   uint16_t* const my_v = sh_v[wave];
   const uint32_t v_write = lds_addr(my_v) + c * Tile::RB, v_read = lds_addr(my_v) + Tile::tr_lane(lane);
-  const int all_rows = (1 << nodes.n_rows) - 1;
-  Walk<SMALL> walk(p, b, h, L, nodes, split, wave, W, tree && split == p.num_splits - 1 && wave == W - 1 && nodes.all);
+  Walk<SMALL> walk(b, h, L, nodes, split, wave, W, 0, tree && split == p.num_splits - 1 && wave == W - 1 && nodes.all, lane);
 
   typename Rows::Part kr[4], vr[4];
-  auto load = [&](const Unit<SMALL>& w, const uint8_t* pool, const uint8_t* scales, const uint16_t* drafted, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
+  auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
+    constexpr bool V = decltype(is_v)::value;
     if (w.drafts) {
       if constexpr (!Rows::kScaled) {
 #pragma unroll
         for (int t = 0; t < 4; ++t) {
           u32x4 rows[KK];
-          draft_rows<Rows>(p, drafted, nodes.all, b, h, t, c, g, rows);
+          draft_rows<Rows, V>(nodes.all, b, h, t, c, g, rows);
           Rows::take(x[t], rows);
         }
       }
@@ -87,33 +86,34 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
     }
 #pragma unroll
     for (int i = 0; i < Unit<SMALL>::NB; ++i) {
-      const uint8_t* const at = pool + w.page[i] * p.c.page + w.skip[i] * p.c.tok;
-      const uint8_t* const scale_at = Rows::kScaled ? scales + w.page[i] * p.c.scale_page + w.skip[i] * p.c.scale_tok : nullptr;
+      const int page = w.page[i], skip = Unit<SMALL>::skip(w.info[i]);
+      const uint8_t* const at = (V ? p.c.v : p.c.k) + page * p.c.page + skip * p.c.tok;
+      const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
 #pragma unroll
-      for (int t = 0; t < 4 / Unit<SMALL>::NB; ++t) Rows::load(x[i + t], at, scale_at, w.rows[i], p.c.tok, p.c.scale_tok, 16 * t + c, g);
+      for (int t = 0; t < 4 / Unit<SMALL>::NB; ++t) Rows::load(x[i + t], at, scale_at, Unit<SMALL>::rows(w.info[i]), p.c.tok, p.c.scale_tok, 16 * t + c, g);
     }
   };
-  auto operands = [&](const Unit<SMALL>& w, int t, const typename Rows::Part& x, const uint16_t* drafted, u32x4 (&out)[KK]) __attribute__((always_inline)) {
+  constexpr std::false_type kK{};
+  constexpr std::true_type kV{};
+  auto operands = [&](auto is_v, const Unit<SMALL>& w, int t, const typename Rows::Part& x, u32x4 (&out)[KK]) __attribute__((always_inline)) {
     if (Rows::kScaled && w.drafts)
-      draft_rows<Rows>(p, drafted, nodes.all, b, h, t, c, g, out);
+      draft_rows<Rows, decltype(is_v)::value>(nodes.all, b, h, t, c, g, out);
     else
       Rows::operands(x, g, out);
   };
 
   f32x4 s[4];
   uint64_t seen;
-  bool some, mixed;
   auto scores = [&](const Unit<SMALL>& w) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 4; ++t) {
       u32x4 k[KK];
-      operands(w, t, kr[t], p.k_draft, k);
+      operands(kK, w, t, kr[t], k);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) s[t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[kk], kk ? s[t] : f32x4{});
     }
-    unit_masks(w, all_rows, some, mixed);
-    if (some) {
-      seen = w.drafts ? drafts_seen(p, nodes, h, c, rel_q) : unit_seen(w, rel_q);
+    if (w.some) {
+      seen = w.drafts ? drafts_seen(nodes, h, c, rel_q) : unit_seen(w, rel_q);
 #pragma unroll
       for (int t = 0; t < 4; ++t) mask_scores(s[t], seen, t, g);
     }
@@ -146,13 +146,18 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
       u32x4 v[2][KK];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        operands(w, 2 * half + i, vr[2 * half + i], p.v_draft, v[i]);
+        operands(kV, w, 2 * half + i, vr[2 * half + i], v[i]);
 #pragma unroll
         for (int kk = 0; kk < KK; ++kk)
           *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * i * Tile::RB + 2 * Rows::feature(kk, g)) = v[i][kk];
       }
       wait_lds();
-      if (mixed && __any((odd_bits(v[0]) | odd_bits(v[1])) != 0)) {
+      bool odd = false;
+      if (w.mixed) {
+        asm volatile("");  // (else looked for in every unit)
+        odd = __any((odd_bits(v[0]) | odd_bits(v[1])) != 0);
+      }
+      if (odd) {
         count_odd<D>(v_read, (uint32_t)(seen >> (32 * half)), sh_odd, &sh_any_odd, lane);
         wait_lds();
         clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
@@ -170,26 +175,27 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
   };
   {
     Unit<SMALL> w;
-    if (walk.next(w)) {
-      load(w, p.c.k, p.c.ks, p.k_draft, kr);
-      load(w, p.c.v, p.c.vs, p.v_draft, vr);
+    if (walk.template next<false>(p, w)) {
+      load(kK, w, kr);
+      load(kV, w, vr);
       for (;;) {
         Unit<SMALL> next;
-        const bool more = walk.next(next);
+        const bool more = walk.template next<true>(p, next);
         // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
         scores(w);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load(next, p.c.k, p.c.ks, p.k_draft, kr);
+        if (more) load(kK, next, kr);
         __builtin_amdgcn_sched_barrier(0);
         sums(w);
         __builtin_amdgcn_sched_barrier(0);
         if (!more) break;
-        load(next, p.c.v, p.c.vs, p.v_draft, vr);
+        load(kV, next, vr);
         w = next;
       }
     }
   }
-  if (p.missing && lane == 0 && walk.n_missing > 0) atomicAdd(p.missing, walk.n_missing);
+  const CacheAttnParams& pe = params_in_memory();
+  if (pe.missing && lane == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 
   // the wavefronts' sums, through where V was
   l_run = sum_groups(l_run);
@@ -213,7 +219,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
   __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
   const int i = tid / TPR, d = 8 * (tid % TPR);
-  if (i >= 16 || i >= T) return;
+  if (i >= 16 || i >= pe.nodes) return;
   float mt = kNegInf, l = 0.f, o[8];
 #pragma unroll
   for (int w = 0; w < W; ++w) mt = fmaxf(mt, sh_m[w][i]);
@@ -225,7 +231,7 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] += reinterpret_cast<const float*>(sh_v[w])[i * RS + d + e];
   }
-  put_result<D>(p, b, h, i, split, d, o, mt, l);
+  put_result<D>(pe, b, h, i, split, d, o, mt, l);
 }
 
 // Merges the splits, a wavefront to a row of the result: lane i holds the weight of split i, groups of D/4 lanes add up the splits of their own, four

@@ -62,44 +62,40 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   const uint32_t at_k = lds_addr(sh_kv[0]), at_v = lds_addr(sh_kv[1]);
   const uint32_t write = (16 * wave + c) * Tile::RB;
   const uint32_t k_read = at_k + Tile::row_lane(lane), v_read = at_v + Tile::tr_lane(lane);
-  const int all_rows = (1 << nodes.n_rows) - 1;
-  Walk<SMALL> walk(p, b, h, L, nodes, split, 0, 1, split == p.num_splits - 1 && nodes.all);
+  Walk<SMALL> walk(b, h, L, nodes, split, 0, 1, wave, split == p.num_splits - 1 && nodes.all, lane);
 
   typename Rows::Part kr, vr;
   // My piece of a unit.
-  auto load = [&](const Unit<SMALL>& w, const uint8_t* pool, const uint8_t* scales, const uint16_t* drafted, typename Rows::Part& x) __attribute__((always_inline)) {
+  auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part& x) __attribute__((always_inline)) {
+    constexpr bool V = decltype(is_v)::value;
     if (w.drafts) {
       if constexpr (!Rows::kScaled) {
         u32x4 rows[KK];
-        draft_rows<Rows>(p, drafted, nodes.all, b, h, wave, c, g, rows);
+        draft_rows<Rows, V>(nodes.all, b, h, wave, c, g, rows);
         Rows::take(x, rows);
       }
       return;  // (else fetched where they are used)
     }
-    int page = w.page[0], skip = w.skip[0], rows = w.rows[0];
-    if (SMALL) {
-      page = skip = rows = 0;
-#pragma unroll
-      for (int i = 0; i < Unit<SMALL>::NB; ++i) {  // (by masks: an index would have the unit in memory)
-        const int me = -(int)(wave == i);
-        page |= w.page[i] & me;
-        skip |= w.skip[i] & me;
-        rows |= w.rows[i] & me;
-      }
-    }
-    const uint8_t* const at = pool + page * p.c.page + skip * p.c.tok;
-    const uint8_t* const scale_at = Rows::kScaled ? scales + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
-    Rows::load(x, at, scale_at, rows, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, g);
+    const int page = w.my_page, skip = Unit<SMALL>::skip(w.my_info);
+    const uint8_t* const at = (V ? p.c.v : p.c.k) + page * p.c.page + skip * p.c.tok;
+    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
+    Rows::load(x, at, scale_at, Unit<SMALL>::rows(w.my_info), p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, g);
   };
-  auto put = [&](const Unit<SMALL>& w, const typename Rows::Part& x, const uint16_t* drafted, uint32_t to) __attribute__((always_inline)) {
+  constexpr std::false_type kK{};
+  constexpr std::true_type kV{};
+  auto put = [&](auto is_v, const Unit<SMALL>& w, const typename Rows::Part& x, uint32_t to, int turn) __attribute__((always_inline)) {
+    constexpr bool V = decltype(is_v)::value;
     u32x4 rows[KK];
     if (Rows::kScaled && w.drafts)
-      draft_rows<Rows>(p, drafted, nodes.all, b, h, wave, c, g, rows);
+      draft_rows<Rows, V>(nodes.all, b, h, wave, c, g, rows);
     else
       Rows::operands(x, g, rows);
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + write + 2 * Rows::feature(kk, g)) = rows[kk];
-    return odd_bits(rows);
+    if (V && w.mixed) {
+      asm volatile("");  // (else looked for in every unit)
+      if (odd_bits(rows)) sh_unit_odd[turn] = 1;
+    }
   };
   // (what it has asked of the LDS is done before a wavefront is past it; loads from memory stay on their way)
   auto barrier = [&]() __attribute__((always_inline)) {
@@ -109,24 +105,21 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   };
 
   Unit<SMALL> w;
-  bool more = walk.next(w);
+  bool more = walk.template next<false>(p, w);
   if (more) {
-    load(w, p.c.k, p.c.ks, p.k_draft, kr);
-    load(w, p.c.v, p.c.vs, p.v_draft, vr);
+    load(kK, w, kr);
+    load(kV, w, vr);
   }
   for (int turn = 0; more; turn ^= 1) {
     Unit<SMALL> next;
-    more = walk.next(next);
-    bool some, mixed;
-    unit_masks(w, all_rows, some, mixed);
+    more = walk.template next<true>(p, next);
     barrier();  // nobody reads the unit before any more
-    (void)put(w, kr, p.k_draft, at_k);
-    const uint32_t odd = put(w, vr, p.v_draft, at_v);
-    if (mixed && odd) sh_unit_odd[turn] = 1;
+    put(kK, w, kr, at_k, turn);
+    put(kV, w, vr, at_v, turn);
     if (tid == 0) sh_unit_odd[turn ^ 1] = 0;
     if (more) {
-      load(next, p.c.k, p.c.ks, p.k_draft, kr);
-      load(next, p.c.v, p.c.vs, p.v_draft, vr);
+      load(kK, next, kr);
+      load(kV, next, vr);
     }
     barrier();
 
@@ -139,8 +132,8 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
         s[t] = mfma16(k, qf[kk], kk ? s[t] : f32x4{});
       }
     uint64_t seen = 0;
-    if (some) {
-      seen = w.drafts ? drafts_seen(p, nodes, h, node, rel_q) : unit_seen(w, rel_q);
+    if (w.some) {
+      seen = w.drafts ? drafts_seen(nodes, h, node, rel_q) : unit_seen(w, rel_q);
       seen >>= 16 * NP * kh;
 #pragma unroll
       for (int t = 0; t < NP; ++t) mask_scores(s[t], seen, t, g);
@@ -167,7 +160,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
         s[t][e] = fast_exp2(__builtin_fmaf(s[t][e], cl, -mc));
         l_run += s[t][e];
       }
-    if (mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
+    if (w.mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
 #pragma unroll 1
       for (int u = 0; u < NP / 2; ++u)
         count_odd<D>(v_read + (16 * NP * kh + 32 * u) * Tile::RB, (uint32_t)(seen >> (32 * u)), sh_odd + qt * FT * 64, &sh_any_odd, lane);
@@ -188,7 +181,8 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
     }
     w = next;
   }
-  if (p.missing && tid == 0 && walk.n_missing > 0) atomicAdd(p.missing, walk.n_missing);
+  const CacheAttnParams& pe = params_in_memory();
+  if (pe.missing && tid == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 
   // results from query-on-lane to rows, through where K and V were
   l_run = sum_groups(l_run);
@@ -212,7 +206,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] * weight : f32x4{};
   __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
-  for (int i = tid / TPR; i < 16 * QT && i < p.nodes; i += 64 * W / TPR) {
+  for (int i = tid / TPR; i < 16 * QT && i < pe.nodes; i += 64 * W / TPR) {
     const int d = 8 * (tid % TPR), tile = i / 16, q = i % 16;
     float mt = kNegInf, l = 0.f, o[8];
 #pragma unroll
@@ -226,7 +220,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
 #pragma unroll
       for (int e = 0; e < 8; ++e) o[e] += sums[(16 * of + q) * RS + d + e];
     }
-    put_result<D>(p, b, h, i, split, d, o, mt, l);
+    put_result<D>(pe, b, h, i, split, d, o, mt, l);
   }
 }
 

@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
   Nodes one{};
   one.row0 = (L - 1) >> p.c.block_shift;
   one.n_rows = 1;
-  Walk<SMALL> walk(p, b, h, L, one, split, wave, W, false);
+  Walk<SMALL> walk(b, h, L, one, split, wave, W, 0, false, lane);
   u32x4 q[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(p.q + b * p.q_ss + h * p.q_sh + Rows::feature(kk, g));
@@ -56,10 +56,11 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
   auto load = [&](const Unit<SMALL>& w, const uint8_t* pool, const uint8_t* scales, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
 #pragma unroll
     for (int i = 0; i < Unit<SMALL>::NB; ++i) {
-      const uint8_t* const at = pool + w.page[i] * p.c.page + w.skip[i] * p.c.tok;
-      const uint8_t* const scale_at = scales + w.page[i] * p.c.scale_page + w.skip[i] * p.c.scale_tok;
+      const int page = w.page[i], skip = Unit<SMALL>::skip(w.info[i]);
+      const uint8_t* const at = pool + page * p.c.page + skip * p.c.tok;
+      const uint8_t* const scale_at = scales + page * p.c.scale_page + skip * p.c.scale_tok;
 #pragma unroll
-      for (int t = 0; t < 4 / Unit<SMALL>::NB; ++t) Rows::load(x[i + t], at, scale_at, w.rows[i], p.c.tok, p.c.scale_tok, 16 * t + c, g);
+      for (int t = 0; t < 4 / Unit<SMALL>::NB; ++t) Rows::load(x[i + t], at, scale_at, Unit<SMALL>::rows(w.info[i]), p.c.tok, p.c.scale_tok, 16 * t + c, g);
     }
   };
 
@@ -80,7 +81,7 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
         y = dot2(k[kk][3], q[kk][3], y);
       }
       x = sum_groups(x + y);
-      const int rows = SMALL ? w.rows[t] : w.rows[0] - 16 * t;
+      const int rows = Unit<SMALL>::rows(w.info[SMALL ? t : 0]) - (SMALL ? 0 : 16 * t);
       s[t] = c < rows ? x : kNegInf;
     }
   };
@@ -109,12 +110,12 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
 
   {
     Unit<SMALL> w;
-    if (walk.next(w)) {
+    if (walk.template next<false>(p, w)) {
       load(w, p.c.k, p.c.ks, kr);
       load(w, p.c.v, p.c.vs, vr);
       for (;;) {
         Unit<SMALL> next;
-        const bool more = walk.next(next);
+        const bool more = walk.template next<true>(p, next);
         // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
         scores(w);
         __builtin_amdgcn_sched_barrier(0);
@@ -128,7 +129,8 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
       }
     }
   }
-  if (p.missing && lane == 0 && walk.n_missing > 0) atomicAdd(p.missing, walk.n_missing);
+  const CacheAttnParams& pe = params_in_memory();
+  if (pe.missing && lane == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 
   // the rows of the wavefront, then the wavefronts
   auto over_rows = [](float x) __attribute__((always_inline)) {
@@ -165,7 +167,7 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
 #pragma unroll
     for (int e = 0; e < 8; ++e) o[e] += sh_acc[w][d + e] * weight;
   }
-  put_result<D>(p, b, h, 0, split, d, o, m, l);
+  put_result<D>(pe, b, h, 0, split, d, o, m, l);
 }
 
 template <int D, int FMT, int W>

@@ -17,6 +17,12 @@ struct RowBlocks {
     if (cols) return load_const<int32_t>(cols + n);
     return n < n_stripe ? striped : local;
   }
+  // the same for an n that is a lane's own
+  __device__ int block_of_lane(int n) const {
+    const int striped = first_stripe + n * stride, local = local_lo + (n - n_stripe);
+    if (cols) return cols[n];
+    return n < n_stripe ? striped : local;
+  }
 };
 
 template <class PARAMS>
@@ -53,34 +59,33 @@ __device__ inline RowBlocks row_blocks(const PARAMS& p, int head, int i) {
   return r;
 }
 
-// Whether row i keeps block j <= i.  With lists, n is where j is likely to be in row i's: the rows of neighbouring tokens differ in few
+// Whether row i keeps block j, a lane's own.  With lists, n is where j is likely to be in row i's: the rows of neighbouring tokens differ in few
 // places, so that the search goes from there in steps that double, and then halves.
 template <class PARAMS>
 __device__ inline bool row_keeps(const PARAMS& p, const RowBlocks& rb, int head, int i, int j, int n) {
-  if (p.row_ptr) {
-    if (rb.count == 0) return false;
-    int lo = min(max(n, 0), rb.count - 1), hi = lo;  // the last entry <= j, if there is one, is brought into [lo, hi]
-    int at = rb.block(lo);
+  if (rb.cols) {
+    int lo = min(max(n, 0), rb.count - 1), hi = lo;  // (a row keeps its own block: count > 0)
+    const int at = rb.cols[lo];
     if (at == j) return true;
     if (at > j) {
-      for (int step = 1; lo > 0 && rb.block(lo) > j; step *= 2) {
+      for (int step = 1; lo > 0 && rb.cols[lo] > j; step *= 2) {
         hi = lo;
         lo = max(lo - step, 0);
       }
     } else {
-      for (int step = 1; hi < rb.count - 1 && rb.block(hi) < j; step *= 2) {
+      for (int step = 1; hi < rb.count - 1 && rb.cols[hi] < j; step *= 2) {
         lo = hi;
         hi = min(hi + step, rb.count - 1);
       }
     }
     while (lo < hi) {  // (the last entry <= j)
       const int mid = (lo + hi + 1) / 2;
-      if (rb.block(mid) > j)
+      if (rb.cols[mid] > j)
         hi = mid - 1;
       else
         lo = mid;
     }
-    return rb.block(lo) == j;
+    return rb.cols[lo] == j;
   }
   if (j > i) return false;
   if (p.dense || i - j < p.local_blocks) return true;
