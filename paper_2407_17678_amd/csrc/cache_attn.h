@@ -67,7 +67,7 @@ struct Unit {
   static constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB;
   int page[NB];
   int info[NB];          // tokens to read | block rows that keep it << 8 | tokens of the block before them << 16
-  int my_page, my_info;  // SMALL: of the walk's own piece
+  int my_page[2], my_info[2];  // SMALL: of the walk's own piece and the one after it
   bool drafts;
   bool some;   // some query may not attend some token
   bool mixed;  // some query does not attend a token that is there
@@ -84,14 +84,13 @@ struct Walk {
   static constexpr int NB = Unit<SMALL>::NB, kTokens = Unit<SMALL>::kTokens, kUnits = 64 / NB;
   int b, h, L, row0, n_rows, split, first, step, piece;  // unit `first` of the split, and every step-th
   bool drafts_left;
-  int lane;
   int n_missing = 0;
   int r_now = -1, u_now = 0, u_end = 0;
   int page = 0, info = 0;            // of this lane's unit (piece)
   uint64_t live = 0, some = 0, mixed = 0;
 
-  __device__ __forceinline__ Walk(int b_, int h_, int L_, const Nodes& x, int split_, int first_, int step_, int piece_, bool drafts, int lane_)
-      : b(b_), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_), first(first_), step(step_), piece(piece_), drafts_left(drafts), lane(lane_) {}
+  __device__ __forceinline__ Walk(int b_, int h_, int L_, const Nodes& x, int split_, int first_, int step_, int piece_, bool drafts)
+      : b(b_), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_), first(first_), step(step_), piece(piece_), drafts_left(drafts) {}
 
   // bit NB * i: whether any of the NB bits from there on is set
   __device__ static uint64_t of_units(uint64_t pieces) {
@@ -113,6 +112,7 @@ struct Walk {
       u_now = even * split + rest * split / p.by_splits + first;
       u_end = even * (split + 1) + rest * (split + 1) / p.by_splits;
     }
+    const int lane = lane_now();
     const int u = u_now + step * (lane / NB), l = 64 * u + 16 * (lane % NB), n = l >> sh, skip = l & (S - 1);
     u_now += step * kUnits;
     const bool inside = u < u_end && n < rb.count;
@@ -162,8 +162,11 @@ struct Walk {
       w.page[t] = __builtin_amdgcn_readlane(page, i + t);
       w.info[t] = __builtin_amdgcn_readlane(info, i + t);
     }
-    w.my_page = __builtin_amdgcn_readlane(page, i + (SMALL ? piece : 0));
-    w.my_info = __builtin_amdgcn_readlane(info, i + (SMALL ? piece : 0));
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {  // (of the last piece there is none after it, and it is not used)
+      w.my_page[t] = SMALL ? __builtin_amdgcn_readlane(page, i + ((piece + t) & 3)) : w.page[0];
+      w.my_info[t] = SMALL ? __builtin_amdgcn_readlane(info, i + ((piece + t) & 3)) : w.info[0];
+    }
     return true;
   }
 };

@@ -24,9 +24,12 @@ namespace s2 {
 
 namespace {
 
+// Wavefronts to a SIMD that the registers are limited for: as many as they fit without spilling.
+constexpr int waves_for(int D, int FMT) { return D == 64 ? 4 : FMT == S2_KV_BF16 ? 2 : 3; }
+
 // SMALL: blocks of 16 or 32 tokens, so that a unit of 64 is gathered from four or two of the list's blocks; else it is a piece of one block.
 template <int D, int FMT, bool SMALL>
-__global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParams p) {
+__global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(const CacheAttnParams p) {
   using Rows = CacheRows<D, FMT>;
   using Tile = ChunkTile<D>;
   constexpr int W = 4, KK = D / 32, FT = D / 16;
@@ -68,15 +71,17 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
 
   uint16_t* const my_v = sh_v[wave];
   const uint32_t v_write = lds_addr(my_v) + c * Tile::RB, v_read = lds_addr(my_v) + Tile::tr_lane(lane);
-  Walk<SMALL> walk(b, h, L, nodes, split, wave, W, 0, tree && split == p.num_splits - 1 && wave == W - 1 && nodes.all, lane);
+  // two wavefronts to a unit of 64 tokens, half of it each
+  const int half = wave & 1;
+  Walk<SMALL> walk(b, h, L, nodes, split, wave >> 1, W / 2, 2 * half, tree && split == p.num_splits - 1 && wave == 0 && nodes.all);
 
-  typename Rows::Part kr[4], vr[4];
-  auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part (&x)[4]) __attribute__((always_inline)) {
+  typename Rows::Part kr[2], vr[2];
+  auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part (&x)[2]) __attribute__((always_inline)) {
     constexpr bool V = decltype(is_v)::value;
     if (w.drafts) {
       if constexpr (!Rows::kScaled) {
 #pragma unroll
-        for (int t = 0; t < 4; ++t) {
+        for (int t = 0; t < 2; ++t) {
           u32x4 rows[KK];
           draft_rows<Rows, V>(nodes.all, b, h, t, c, g, rows);
           Rows::take(x[t], rows);
@@ -85,12 +90,11 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
       return;  // (else fetched where they are used)
     }
 #pragma unroll
-    for (int i = 0; i < Unit<SMALL>::NB; ++i) {
-      const int page = w.page[i], skip = Unit<SMALL>::skip(w.info[i]);
+    for (int t = 0; t < 2; ++t) {
+      const int page = w.my_page[t], skip = Unit<SMALL>::skip(w.my_info[t]);
       const uint8_t* const at = (V ? p.c.v : p.c.k) + page * p.c.page + skip * p.c.tok;
       const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
-#pragma unroll
-      for (int t = 0; t < 4 / Unit<SMALL>::NB; ++t) Rows::load(x[i + t], at, scale_at, Unit<SMALL>::rows(w.info[i]), p.c.tok, p.c.scale_tok, 16 * t + c, g);
+      Rows::load(x[t], at, scale_at, Unit<SMALL>::rows(w.my_info[t]), p.c.tok, p.c.scale_tok, (SMALL ? 0 : 32 * half + 16 * t) + c, g);
     }
   };
   constexpr std::false_type kK{};
@@ -102,26 +106,26 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
       Rows::operands(x, g, out);
   };
 
-  f32x4 s[4];
-  uint64_t seen;
+  f32x4 s[2];
+  uint32_t seen;
   auto scores = [&](const Unit<SMALL>& w) __attribute__((always_inline)) {
 #pragma unroll
-    for (int t = 0; t < 4; ++t) {
+    for (int t = 0; t < 2; ++t) {
       u32x4 k[KK];
       operands(kK, w, t, kr[t], k);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) s[t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[kk], kk ? s[t] : f32x4{});
     }
     if (w.some) {
-      seen = w.drafts ? drafts_seen(nodes, h, c, rel_q) : unit_seen(w, rel_q);
+      seen = (uint32_t)((w.drafts ? drafts_seen(nodes, h, c, rel_q) : unit_seen(w, rel_q)) >> (32 * half));
 #pragma unroll
-      for (int t = 0; t < 4; ++t) mask_scores(s[t], seen, t, g);
+      for (int t = 0; t < 2; ++t) mask_scores(s[t], seen, t, g);
     }
   };
   auto sums = [&](const Unit<SMALL>& w) __attribute__((always_inline)) {
     float mx = kNegInf;
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
     mx = max_halves(max_rows(mx));
@@ -135,43 +139,39 @@ __global__ __launch_bounds__(256, 2) void cache_attn_kernel(const CacheAttnParam
       for (int ft = 0; ft < FT; ++ft) acc[ft] *= alpha;
     }
 #pragma unroll
-    for (int t = 0; t < 4; ++t)
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         s[t][e] = fast_exp2(__builtin_fmaf(s[t][e], cl, -mc));
         l_run += s[t][e];
       }
+    u32x4 v[2][KK];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      u32x4 v[2][KK];
+    for (int i = 0; i < 2; ++i) {
+      operands(kV, w, i, vr[i], v[i]);
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        operands(kV, w, 2 * half + i, vr[2 * half + i], v[i]);
-#pragma unroll
-        for (int kk = 0; kk < KK; ++kk)
-          *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * i * Tile::RB + 2 * Rows::feature(kk, g)) = v[i][kk];
-      }
-      wait_lds();
-      bool odd = false;
-      if (w.mixed) {
-        asm volatile("");  // (else looked for in every unit)
-        odd = __any((odd_bits(v[0]) | odd_bits(v[1])) != 0);
-      }
-      if (odd) {
-        count_odd<D>(v_read, (uint32_t)(seen >> (32 * half)), sh_odd, &sh_any_odd, lane);
-        wait_lds();
-        clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
-        wait_lds();
-      }
-      const f32x4 lo = s[2 * half], hi = s[2 * half + 1];
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack2(lo[0], lo[1]), pack2(lo[2], lo[3]), pack2(hi[0], hi[1]), pack2(hi[2], hi[3])});
-#pragma unroll
-      for (int ft = 0; ft < FT; ++ft) {
-        const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(v_read, v_read, Tile::tr_off(0, ft), Tile::tr_off(0, ft) + 16 * Tile::RB));
-        acc[ft] = mfma16(vf, pf, acc[ft]);
-      }
-      asm volatile("" ::: "memory");
+      for (int kk = 0; kk < KK; ++kk)
+        *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * i * Tile::RB + 2 * Rows::feature(kk, g)) = v[i][kk];
     }
+    wait_lds();
+    bool odd = false;
+    if (w.mixed) {
+      asm volatile("");  // (else looked for in every unit)
+      odd = __any((odd_bits(v[0]) | odd_bits(v[1])) != 0);
+    }
+    if (odd) {
+      count_odd<D>(v_read, seen, sh_odd, &sh_any_odd, lane);
+      wait_lds();
+      clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
+      wait_lds();
+    }
+    const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack2(s[0][0], s[0][1]), pack2(s[0][2], s[0][3]), pack2(s[1][0], s[1][1]), pack2(s[1][2], s[1][3])});
+#pragma unroll
+    for (int ft = 0; ft < FT; ++ft) {
+      const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(v_read, v_read, Tile::tr_off(0, ft), Tile::tr_off(0, ft) + 16 * Tile::RB));
+      acc[ft] = mfma16(vf, pf, acc[ft]);
+    }
+    asm volatile("" ::: "memory");
   };
   {
     Unit<SMALL> w;

@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   const uint32_t at_k = lds_addr(sh_kv[0]), at_v = lds_addr(sh_kv[1]);
   const uint32_t write = (16 * wave + c) * Tile::RB;
   const uint32_t k_read = at_k + Tile::row_lane(lane), v_read = at_v + Tile::tr_lane(lane);
-  Walk<SMALL> walk(b, h, L, nodes, split, 0, 1, wave, split == p.num_splits - 1 && nodes.all, lane);
+  Walk<SMALL> walk(b, h, L, nodes, split, 0, 1, wave, split == p.num_splits - 1 && nodes.all);
 
   typename Rows::Part kr, vr;
   // My piece of a unit.
@@ -76,10 +76,10 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
       }
       return;  // (else fetched where they are used)
     }
-    const int page = w.my_page, skip = Unit<SMALL>::skip(w.my_info);
+    const int page = w.my_page[0], skip = Unit<SMALL>::skip(w.my_info[0]);
     const uint8_t* const at = (V ? p.c.v : p.c.k) + page * p.c.page + skip * p.c.tok;
     const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
-    Rows::load(x, at, scale_at, Unit<SMALL>::rows(w.my_info), p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, g);
+    Rows::load(x, at, scale_at, Unit<SMALL>::rows(w.my_info[0]), p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, g);
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};

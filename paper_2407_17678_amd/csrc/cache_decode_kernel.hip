@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
   Nodes one{};
   one.row0 = (L - 1) >> p.c.block_shift;
   one.n_rows = 1;
-  Walk<SMALL> walk(b, h, L, one, split, wave, W, 0, false, lane);
+  Walk<SMALL> walk(b, h, L, one, split, wave, W, 0, false);
   u32x4 q[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(p.q + b * p.q_ss + h * p.q_sh + Rows::feature(kk, g));
