@@ -61,14 +61,13 @@ __device__ __forceinline__ const CacheAttnParams& params_in_memory() {
   return *(const CacheAttnParams*)at;
 }
 
-// 64 tokens: of one block, or (SMALL: blocks of 16 or 32) four pieces of 16 of the list's blocks; or the drafted ones.
+// 64 tokens: of one block, or (SMALL: blocks of 16 or 32) four pieces of 16 of the list's blocks.
 template <bool SMALL>
 struct Unit {
   static constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB;
   int page[NB];
   int info[NB];          // tokens to read | block rows that keep it << 8 | tokens of the block before them << 16
   int my_page[2], my_info[2];  // SMALL: of the walk's own piece and the one after it
-  bool drafts;
   bool some;   // some query may not attend some token
   bool mixed;  // some query does not attend a token that is there
   __device__ static int rows(int info) { return info & 255; }
@@ -83,14 +82,13 @@ template <bool SMALL>
 struct Walk {
   static constexpr int NB = Unit<SMALL>::NB, kTokens = Unit<SMALL>::kTokens, kUnits = 64 / NB;
   int b, h, L, row0, n_rows, split, first, step, piece;  // unit `first` of the split, and every step-th
-  bool drafts_left;
   int n_missing = 0;
   int r_now = -1, u_now = 0, u_end = 0;
   int page = 0, info = 0;            // of this lane's unit (piece)
   uint64_t live = 0, some = 0, mixed = 0;
 
-  __device__ __forceinline__ Walk(int b_, int h_, int L_, const Nodes& x, int split_, int first_, int step_, int piece_, bool drafts)
-      : b(b_), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_), first(first_), step(step_), piece(piece_), drafts_left(drafts) {}
+  __device__ __forceinline__ Walk(int b_, int h_, int L_, const Nodes& x, int split_, int first_, int step_, int piece_)
+      : b(b_), h(h_), L(L_), row0(x.row0), n_rows(x.n_rows), split(split_), first(first_), step(step_), piece(piece_) {}
 
   // bit NB * i: whether any of the NB bits from there on is set
   __device__ static uint64_t of_units(uint64_t pieces) {
@@ -143,13 +141,15 @@ struct Walk {
   // The next unit with a token to read (AGAIN: the parameters are read from memory).
   template <bool AGAIN>
   __device__ __forceinline__ bool next(const CacheAttnParams& p, Unit<SMALL>& w) {
-    w.drafts = false;
     while (live == 0) {
       if (u_now >= u_end && r_now + 1 >= n_rows) {
-        if (!drafts_left) return false;
-        drafts_left = false;
-        w.drafts = w.some = w.mixed = true;
-        return true;
+        // (no rows, so that loading it fetches nothing: the loads are issued in any case, for where a load might not have been issued
+        // the compiler waits as if it had not, that is for what was issued after it)
+#pragma unroll
+        for (int t = 0; t < NB; ++t) w.page[t] = w.info[t] = 0;
+        w.my_page[0] = w.my_page[1] = w.my_info[0] = w.my_info[1] = 0;
+        w.some = w.mixed = false;
+        return false;
       }
       look_up(AGAIN ? params_in_memory() : p);
     }

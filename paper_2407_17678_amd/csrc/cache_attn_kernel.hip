@@ -73,22 +73,11 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   const uint32_t v_write = lds_addr(my_v) + c * Tile::RB, v_read = lds_addr(my_v) + Tile::tr_lane(lane);
   // two wavefronts to a unit of 64 tokens, half of it each
   const int half = wave & 1;
-  Walk<SMALL> walk(b, h, L, nodes, split, wave >> 1, W / 2, 2 * half, tree && split == p.num_splits - 1 && wave == 0 && nodes.all);
+  Walk<SMALL> walk(b, h, L, nodes, split, wave >> 1, W / 2, 2 * half);
 
   typename Rows::Part kr[2], vr[2];
   auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part (&x)[2]) __attribute__((always_inline)) {
     constexpr bool V = decltype(is_v)::value;
-    if (w.drafts) {
-      if constexpr (!Rows::kScaled) {
-#pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          u32x4 rows[KK];
-          draft_rows<Rows, V>(nodes.all, b, h, t, c, g, rows);
-          Rows::take(x[t], rows);
-        }
-      }
-      return;  // (else fetched where they are used)
-    }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int page = w.my_page[t], skip = Unit<SMALL>::skip(w.my_info[t]);
@@ -99,8 +88,11 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};
-  auto operands = [&](auto is_v, const Unit<SMALL>& w, int t, const typename Rows::Part& x, u32x4 (&out)[KK]) __attribute__((always_inline)) {
-    if (Rows::kScaled && w.drafts)
+  constexpr std::false_type kCached{};
+  constexpr std::true_type kDrafts{};
+  // (DRAFTS: the unit of drafted tokens, fetched where it is used)
+  auto operands = [&](auto is_v, auto drafts, int t, const typename Rows::Part& x, u32x4 (&out)[KK]) __attribute__((always_inline)) {
+    if constexpr (decltype(drafts)::value)
       draft_rows<Rows, decltype(is_v)::value>(nodes.all, b, h, t, c, g, out);
     else
       Rows::operands(x, g, out);
@@ -108,21 +100,21 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
 
   f32x4 s[2];
   uint32_t seen;
-  auto scores = [&](const Unit<SMALL>& w) __attribute__((always_inline)) {
+  auto scores = [&](auto drafts, bool some, auto see) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       u32x4 k[KK];
-      operands(kK, w, t, kr[t], k);
+      operands(kK, drafts, t, kr[t], k);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk) s[t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[kk], kk ? s[t] : f32x4{});
     }
-    if (w.some) {
-      seen = (uint32_t)((w.drafts ? drafts_seen(nodes, h, c, rel_q) : unit_seen(w, rel_q)) >> (32 * half));
+    if (some) {
+      seen = (uint32_t)(see() >> (32 * half));
 #pragma unroll
       for (int t = 0; t < 2; ++t) mask_scores(s[t], seen, t, g);
     }
   };
-  auto sums = [&](const Unit<SMALL>& w) __attribute__((always_inline)) {
+  auto sums = [&](auto drafts, bool mixed) __attribute__((always_inline)) {
     float mx = kNegInf;
 #pragma unroll
     for (int t = 0; t < 2; ++t)
@@ -148,14 +140,14 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
     u32x4 v[2][KK];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      operands(kV, w, i, vr[i], v[i]);
+      operands(kV, drafts, i, vr[i], v[i]);
 #pragma unroll
       for (int kk = 0; kk < KK; ++kk)
         *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(v_write + 16 * i * Tile::RB + 2 * Rows::feature(kk, g)) = v[i][kk];
     }
     wait_lds();
     bool odd = false;
-    if (w.mixed) {
+    if (mixed) {
       asm volatile("");  // (else looked for in every unit)
       odd = __any((odd_bits(v[0]) | odd_bits(v[1])) != 0);
     }
@@ -178,21 +170,25 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
     if (walk.template next<false>(p, w)) {
       load(kK, w, kr);
       load(kV, w, vr);
-      for (;;) {
+      for (bool more = true; more;) {
         Unit<SMALL> next;
-        const bool more = walk.template next<true>(p, next);
+        more = walk.template next<true>(p, next);
         // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
-        scores(w);
+        scores(kCached, w.some, [&] { return unit_seen(w, rel_q); });
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load(kK, next, kr);
+        load(kK, next, kr);
         __builtin_amdgcn_sched_barrier(0);
-        sums(w);
+        sums(kCached, w.mixed);
         __builtin_amdgcn_sched_barrier(0);
-        if (!more) break;
         load(kV, next, vr);
         w = next;
       }
     }
+  }
+  // the drafted tokens, 16 at most: the first half of a unit of their own
+  if (tree && split == p.num_splits - 1 && wave == 0 && nodes.all) {
+    scores(kDrafts, true, [&] { return drafts_seen(nodes, h, c, rel_q); });
+    sums(kDrafts, true);
   }
   const CacheAttnParams& pe = params_in_memory();
   if (pe.missing && lane == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);

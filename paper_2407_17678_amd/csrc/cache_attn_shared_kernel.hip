@@ -62,20 +62,12 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   const uint32_t at_k = lds_addr(sh_kv[0]), at_v = lds_addr(sh_kv[1]);
   const uint32_t write = (16 * wave + c) * Tile::RB;
   const uint32_t k_read = at_k + Tile::row_lane(lane), v_read = at_v + Tile::tr_lane(lane);
-  Walk<SMALL> walk(b, h, L, nodes, split, 0, 1, wave, split == p.num_splits - 1 && nodes.all);
+  Walk<SMALL> walk(b, h, L, nodes, split, 0, 1, wave);
 
   typename Rows::Part kr, vr;
   // My piece of a unit.
   auto load = [&](auto is_v, const Unit<SMALL>& w, typename Rows::Part& x) __attribute__((always_inline)) {
     constexpr bool V = decltype(is_v)::value;
-    if (w.drafts) {
-      if constexpr (!Rows::kScaled) {
-        u32x4 rows[KK];
-        draft_rows<Rows, V>(nodes.all, b, h, wave, c, g, rows);
-        Rows::take(x, rows);
-      }
-      return;  // (else fetched where they are used)
-    }
     const int page = w.my_page[0], skip = Unit<SMALL>::skip(w.my_info[0]);
     const uint8_t* const at = (V ? p.c.v : p.c.k) + page * p.c.page + skip * p.c.tok;
     const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
@@ -83,16 +75,10 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};
-  auto put = [&](auto is_v, const Unit<SMALL>& w, const typename Rows::Part& x, uint32_t to, int turn) __attribute__((always_inline)) {
-    constexpr bool V = decltype(is_v)::value;
-    u32x4 rows[KK];
-    if (Rows::kScaled && w.drafts)
-      draft_rows<Rows, V>(nodes.all, b, h, wave, c, g, rows);
-    else
-      Rows::operands(x, g, rows);
+  auto put = [&](auto is_v, const u32x4 (&rows)[KK], uint32_t to, bool mixed, int turn) __attribute__((always_inline)) {
 #pragma unroll
     for (int kk = 0; kk < KK; ++kk) *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + write + 2 * Rows::feature(kk, g)) = rows[kk];
-    if (V && w.mixed) {
+    if (decltype(is_v)::value && mixed) {
       asm volatile("");  // (else looked for in every unit)
       if (odd_bits(rows)) sh_unit_odd[turn] = 1;
     }
@@ -104,25 +90,8 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
     asm volatile("" ::: "memory");
   };
 
-  Unit<SMALL> w;
-  bool more = walk.template next<false>(p, w);
-  if (more) {
-    load(kK, w, kr);
-    load(kV, w, vr);
-  }
-  for (int turn = 0; more; turn ^= 1) {
-    Unit<SMALL> next;
-    more = walk.template next<true>(p, next);
-    barrier();  // nobody reads the unit before any more
-    put(kK, w, kr, at_k, turn);
-    put(kV, w, vr, at_v, turn);
-    if (tid == 0) sh_unit_odd[turn ^ 1] = 0;
-    if (more) {
-      load(kK, next, kr);
-      load(kV, next, vr);
-    }
-    barrier();
-
+  // A unit in LDS against my queries.
+  auto attend = [&](bool some, bool mixed, int turn, auto see) __attribute__((always_inline)) {
     f32x4 s[NP];
 #pragma unroll
     for (int t = 0; t < NP; ++t)
@@ -132,9 +101,8 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
         s[t] = mfma16(k, qf[kk], kk ? s[t] : f32x4{});
       }
     uint64_t seen = 0;
-    if (w.some) {
-      seen = w.drafts ? drafts_seen(nodes, h, node, rel_q) : unit_seen(w, rel_q);
-      seen >>= 16 * NP * kh;
+    if (some) {
+      seen = see() >> (16 * NP * kh);
 #pragma unroll
       for (int t = 0; t < NP; ++t) mask_scores(s[t], seen, t, g);
     }
@@ -160,7 +128,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
         s[t][e] = fast_exp2(__builtin_fmaf(s[t][e], cl, -mc));
         l_run += s[t][e];
       }
-    if (w.mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
+    if (mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
 #pragma unroll 1
       for (int u = 0; u < NP / 2; ++u)
         count_odd<D>(v_read + (16 * NP * kh + 32 * u) * Tile::RB, (uint32_t)(seen >> (32 * u)), sh_odd + qt * FT * 64, &sh_any_odd, lane);
@@ -179,7 +147,40 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
         acc[ft] = mfma16(vf, pf, acc[ft]);
       }
     }
-    w = next;
+  };
+
+  int turn = 0;
+  {
+    Unit<SMALL> w;
+    bool more = walk.template next<false>(p, w);
+    load(kK, w, kr);
+    load(kV, w, vr);
+    for (; more; turn ^= 1) {
+      Unit<SMALL> next;
+      more = walk.template next<true>(p, next);
+      barrier();  // nobody reads the unit before any more
+      u32x4 rows[KK];
+      Rows::operands(kr, g, rows);
+      put(kK, rows, at_k, w.mixed, turn);
+      Rows::operands(vr, g, rows);
+      put(kV, rows, at_v, w.mixed, turn);
+      if (tid == 0) sh_unit_odd[turn ^ 1] = 0;
+      load(kK, next, kr);
+      load(kV, next, vr);
+      barrier();
+      attend(w.some, w.mixed, turn, [&] { return unit_seen(w, rel_q); });
+      w = next;
+    }
+  }
+  if (split == p.num_splits - 1 && nodes.all) {  // the drafted tokens: a unit of their own
+    barrier();
+    u32x4 rows[KK];
+    draft_rows<Rows, false>(nodes.all, b, h, wave, c, g, rows);
+    put(kK, rows, at_k, true, turn);
+    draft_rows<Rows, true>(nodes.all, b, h, wave, c, g, rows);
+    put(kV, rows, at_v, true, turn);
+    barrier();
+    attend(true, true, turn, [&] { return drafts_seen(nodes, h, node, rel_q); });
   }
   const CacheAttnParams& pe = params_in_memory();
   if (pe.missing && tid == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);

@@ -24,11 +24,11 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
 
 // Wavefronts to a SIMD that the registers are limited for: as many as they fit without spilling (e4m3, D = 128, 20 registers spilled for three: 213 -> 394 us
 // for 64 x 32 heads of 8192 to 32768).
-constexpr int waves_for(int D, int FMT, bool SMALL) { return D == 64 ? 4 : FMT == S2_KV_MXFP8 ? 2 : SMALL ? 4 : 3; }
+constexpr int waves_for(int D, int FMT) { return D == 128 && FMT == S2_KV_MXFP8 ? 3 : 4; }
 
 // W: wavefronts to a workgroup.
 template <int D, int FMT, bool SMALL, int W>
-__global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode_kernel(const CacheAttnParams p) {
+__global__ __launch_bounds__(64 * W, waves_for(D, FMT)) void cache_decode_kernel(const CacheAttnParams p) {
   using Rows = CacheRows<D, FMT>;
   constexpr int KK = D / 32, NF = D / 4;  // operands of eight features, features to a lane
 
@@ -47,7 +47,7 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
   Nodes one{};
   one.row0 = (L - 1) >> p.c.block_shift;
   one.n_rows = 1;
-  Walk<SMALL> walk(b, h, L, one, split, wave, W, 0, false);
+  Walk<SMALL> walk(b, h, L, one, split, wave, W, 0);
   u32x4 q[KK];
 #pragma unroll
   for (int kk = 0; kk < KK; ++kk) q[kk] = *reinterpret_cast<const u32x4*>(p.q + b * p.q_ss + h * p.q_sh + Rows::feature(kk, g));
@@ -113,17 +113,16 @@ __global__ __launch_bounds__(64 * W, waves_for(D, FMT, SMALL)) void cache_decode
     if (walk.template next<false>(p, w)) {
       load(w, p.c.k, p.c.ks, kr);
       load(w, p.c.v, p.c.vs, vr);
-      for (;;) {
+      for (bool more = true; more;) {
         Unit<SMALL> next;
-        const bool more = walk.template next<true>(p, next);
+        more = walk.template next<true>(p, next);
         // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
         scores(w);
         __builtin_amdgcn_sched_barrier(0);
-        if (more) load(next, p.c.k, p.c.ks, kr);
+        load(next, p.c.k, p.c.ks, kr);
         __builtin_amdgcn_sched_barrier(0);
         sums();
         __builtin_amdgcn_sched_barrier(0);
-        if (!more) break;
         load(next, p.c.v, p.c.vs, vr);
         w = next;
       }
