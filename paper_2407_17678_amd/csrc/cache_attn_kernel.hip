@@ -191,7 +191,8 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
     sums(kDrafts, true);
   }
   const CacheAttnParams& pe = params_in_memory();
-  if (pe.missing && lane == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
+  // (both halves have walked the same units)
+  if (pe.missing && lane == 0 && half == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 
   // the wavefronts' sums, through where V was
   l_run = sum_groups(l_run);
@@ -205,13 +206,15 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   for (int w = 0; w < W; ++w) m = fmaxf(m, sh_m[w][c]);
   // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
   const float weight = sh_l[wave][c] == 0.f ? 0.f : fast_exp2((m_run - m) * cl);
-  if (sh_any_odd && wave == 0) {
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) acc[ft] *= weight;
+  if (sh_any_odd && wave == 0) {  // (after the weight: it may be another wavefront that the query has its tokens of)
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft) put_odd(acc[ft], sh_odd[ft * 64 + lane]);
   }
   float* const mine = reinterpret_cast<float*>(my_v) + c * RS + 4 * g;
 #pragma unroll
-  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] * weight : f32x4{};
+  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] : f32x4{};
   __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
   const int i = tid / TPR, d = 8 * (tid % TPR);

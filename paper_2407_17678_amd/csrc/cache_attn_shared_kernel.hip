@@ -197,14 +197,16 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   for (int i = 0; i < KH; ++i) m = fmaxf(m, sh_m[qt + QT * i][c]);
   // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
   const float weight = sh_l[wave][c] == 0.f ? 0.f : KH == 1 ? 1.f : fast_exp2((m_run - m) * cl);
-  if (sh_any_odd && kh == 0) {
+#pragma unroll
+  for (int ft = 0; ft < FT; ++ft) acc[ft] *= weight;
+  if (sh_any_odd && kh == 0) {  // (after the weight: it may be another wavefront that the query has its tokens of)
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft) put_odd(acc[ft], sh_odd[(qt * FT + ft) * 64 + lane]);
   }
   float* const sums = reinterpret_cast<float*>(sh_kv[0]);
   float* const mine = sums + (16 * wave + c) * RS + 4 * g;
 #pragma unroll
-  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] * weight : f32x4{};
+  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] : f32x4{};
   __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
   for (int i = tid / TPR; i < 16 * QT && i < pe.nodes; i += 64 * W / TPR) {

@@ -210,6 +210,42 @@ def test_strides_head_base_splits_and_missing_blocks(fmt):
     c.check(splits=2)
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("T", [1, 5, 16, 40])
+def test_missing_blocks_are_counted_once(fmt, T):
+    rng = np.random.default_rng(T)
+    par = np.stack([random_tree(rng, T), random_tree(rng, T)])
+    for S, lens, gone in ((16, [250, 40], [(0, 0, 15), (0, 1, 14), (0, 1, 3), (1, 0, 0), (1, 0, 1), (1, 0, 2)]), (64, [700, 66], [(0, 0, 10), (0, 1, 9), (1, 1, 0)])):
+        for splits in (0, 1, 3):
+            Case(fmt, 64, S, lens, 2, par, evict=gone, local=4).check(splits=splits)
+        if T == 1:
+            Case(fmt, 64, S, lens, 2, None, evict=gone, local=4).check(strided=True)
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("T", [12, 24, 40])
+def test_an_infinity_that_one_wavefront_meets(fmt, T):
+    """A token of V that is infinite, in blocks that the first row of the tree keeps and the second does not: the nodes of the first row have the
+    infinity, whichever wavefront met it; those of the second stay finite."""
+    S, L = 16, 16 * 9 + 15
+    par = np.stack([np.arange(-1, T - 1, dtype=np.int32)])
+    c = Case(fmt, 64, S, [L], 1, par, local=6, stride=0)
+    bits = np.full((S, 64), 0x3F80, dtype=np.uint16)
+    bits[3, 5] = 0x7F80
+    held, byte, _ = U.held_rows(bits, fmt)
+    blk = L // S - 5  # the last that row L // S keeps
+    c.pools.put(1, c.table[0, 0, blk], 0, held, None if byte is None else byte)
+    o, _, _ = c.run(splits=1)
+    first = [i for i in range(T) if (L + i) // S == L // S]
+    assert first and len(first) < T
+    rest = [i for i in range(T) if i not in first]
+    assert np.all(np.isfinite(o[0, 0, rest]))
+    if fmt == "bf16":
+        assert np.all(o[0, 0, first, 5] == np.inf) and np.all(np.isfinite(np.delete(o[0, 0, first], 5, -1)))
+    else:  # (a scale stands for 32 features: none of them is a number)
+        assert np.all(np.isnan(o[0, 0, first, :32])) and np.all(np.isfinite(o[0, 0, first, 32:]))
+
+
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
 def test_no_room_for_the_deeper_nodes(fmt):
     """Nodes at positions that the table has no block for do not exist."""
