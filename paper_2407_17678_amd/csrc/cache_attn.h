@@ -220,8 +220,8 @@ __device__ __forceinline__ uint32_t odd_bits(const u32x4 (&v)[KK]) {
     for (int e = 0; e < 4; ++e) top |= (v[kk][e] & 0x7fff7fffu) + 0x00800080u;
   return top & 0x80008000u;
 }
-// For a tile of 16 queries and 32 tokens of V in LDS (transposed reads at v_read; seen: bits of the 32): ors into found[feature tile * 64 + lane] a byte to
-// each of the lane's four features: 1 infinity, 2 minus infinity, 4 NaN.
+// For a tile of 16 queries and 32 tokens of V in LDS (transposed reads at v_read; seen: bits of the 32): ors two bits to each of the lane's four features of
+// feature tile ft into byte ft % 4 of found[ft / 4 * 64 + lane]: 1 infinity, 2 minus infinity, 3 NaN (or both).
 template <int D>
 __device__ __forceinline__ void count_odd(uint32_t v_read, uint32_t seen, uint32_t* found, uint32_t* any, int lane) {
   const uint32_t mine = seen >> (4 * (lane >> 4));  // tokens 4 g .. and 16 + 4 g ..
@@ -229,18 +229,18 @@ __device__ __forceinline__ void count_odd(uint32_t v_read, uint32_t seen, uint32
 #pragma unroll
   for (int e = 0; e < 4; ++e) w[e] = ((mine >> (16 * (e / 2) + 2 * (e % 2))) & 1) * 0x3f80u + ((mine >> (16 * (e / 2) + 2 * (e % 2) + 1)) & 1) * 0x3f800000u;
 #pragma unroll 1
-  for (int i = 0; i < 3 * (D / 16); ++i) {
-    const int ft = i / 3, kind = i % 3;
-    auto ones = [&](uint32_t x) { return (kind == 0 ? x == 0x7f80u : kind == 1 ? x == 0xff80u : (x & 0x7fffu) > 0x7f80u) ? 0x3f80u : 0u; };
+  for (int i = 0; i < 2 * (D / 16); ++i) {
+    const int ft = i / 2, kind = i % 2;
+    auto ones = [&](uint32_t x) { return x == (kind ? 0xff80u : 0x7f80u) || (x & 0x7fffu) > 0x7f80u ? 0x3f80u : 0u; };
     u32x4 vf = lds_read_tr2(v_read + 32 * ft, v_read + 32 * ft, 0, 16 * ChunkTile<D>::RB);
 #pragma unroll
     for (int e = 0; e < 4; ++e) vf[e] = ones(vf[e] & 0xffffu) | ones(vf[e] >> 16) << 16;
     const f32x4 count = mfma16(__builtin_bit_cast(bf16x8, vf), __builtin_bit_cast(bf16x8, w), f32x4{});
     uint32_t x = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) x |= (count[e] > 0.f ? 1u : 0u) << (8 * e + kind);
+    for (int e = 0; e < 4; ++e) x |= (count[e] > 0.f ? 1u : 0u) << (2 * e + kind);
     if (x) {
-      atomicOr(&found[ft * 64 + lane], x);
+      atomicOr(&found[ft / 4 * 64 + lane], x << (8 * (ft % 4)));
       *any = 1;
     }
   }
@@ -253,13 +253,16 @@ __device__ __forceinline__ void clean_words(uint32_t* words, int n, int lane) {
     words[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
   }
 }
-// The results that found bytes stand for, in place of the sums.
-__device__ __forceinline__ void put_odd(f32x4& acc, uint32_t found) {
+// The results that what was found stands for, in place of the sums.
+template <int FT>
+__device__ __forceinline__ void put_odd(f32x4 (&acc)[FT], const uint32_t* found, int lane) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    const uint32_t x = found >> (8 * e) & 7;
-    if (x) acc[e] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
-  }
+  for (int ft = 0; ft < FT; ++ft)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const uint32_t x = found[ft / 4 * 64 + lane] >> (8 * (ft % 4) + 2 * e) & 3;
+      if (x) acc[ft][e] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
+    }
 }
 
 // Rows 16 t .. 16 t + 15 of drafted K or V, a lane's quarter of row c; a node that is not there may hold anything, nobody attends it, and it is

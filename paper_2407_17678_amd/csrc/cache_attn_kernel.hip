@@ -38,7 +38,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
 
   __shared__ __align__(16) uint16_t sh_v[W][32 * Tile::kStride];
   __shared__ float sh_m[W][16], sh_l[W][16];
-  __shared__ uint32_t sh_odd[FT * 64];  // (count_odd)
+  __shared__ uint32_t sh_odd[FT / 4 * 64];  // (count_odd)
   __shared__ uint32_t sh_any_odd;
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
@@ -60,7 +60,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   for (int kk = 0; kk < KK; ++kk)
     qf[kk] = there_q ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + c * p.q_sn + Rows::feature(kk, g)) : bf16x8{};
 
-  for (int i = tid; i < FT * 64; i += 64 * W) sh_odd[i] = 0;
+  for (int i = tid; i < FT / 4 * 64; i += 64 * W) sh_odd[i] = 0;
   if (tid == 0) sh_any_odd = 0;
   __syncthreads();
 
@@ -208,10 +208,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   const float weight = sh_l[wave][c] == 0.f ? 0.f : fast_exp2((m_run - m) * cl);
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) acc[ft] *= weight;
-  if (sh_any_odd && wave == 0) {  // (after the weight: it may be another wavefront that the query has its tokens of)
-#pragma unroll
-    for (int ft = 0; ft < FT; ++ft) put_odd(acc[ft], sh_odd[ft * 64 + lane]);
-  }
+  if (sh_any_odd && wave == 0) put_odd(acc, sh_odd, lane);  // (after the weight: it may be another wavefront that the query has its tokens of)
   float* const mine = reinterpret_cast<float*>(my_v) + c * RS + 4 * g;
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] : f32x4{};

@@ -16,8 +16,11 @@ namespace s2 {
 
 namespace {
 
+// Wavefronts to a SIMD that the registers are limited for: as many as they fit without spilling (64 and 48 queries over 4 bits would by 2 registers with four).
+constexpr int waves_for(int D, int FMT, int QT) { return D == 64 || (FMT != S2_KV_BF16 && QT == 2) ? 4 : 3; }
+
 template <int D, int FMT, int QT, bool SMALL>
-__global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAttnParams p) {
+__global__ __launch_bounds__(256, waves_for(D, FMT, QT)) void cache_attn_shared_kernel(const CacheAttnParams p) {
   using Rows = CacheRows<D, FMT>;
   using Tile = ChunkTile<D>;
   constexpr int W = 4, KK = D / 32, FT = D / 16;
@@ -28,7 +31,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
 
   __shared__ __align__(16) uint16_t sh_kv[2][Tile::kElems];
   __shared__ float sh_m[W][16], sh_l[W][16];
-  __shared__ uint32_t sh_odd[QT * FT * 64];  // (count_odd)
+  __shared__ uint32_t sh_odd[QT * FT / 4 * 64];  // (count_odd)
   __shared__ uint32_t sh_any_odd, sh_unit_odd[2];
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
@@ -51,7 +54,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   for (int kk = 0; kk < KK; ++kk)
     qf[kk] = there_q ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + node * p.q_sn + 32 * kk + 8 * g) : bf16x8{};
 
-  for (int i = tid; i < QT * FT * 64; i += 64 * W) sh_odd[i] = 0;
+  for (int i = tid; i < QT * FT / 4 * 64; i += 64 * W) sh_odd[i] = 0;
   if (tid == 0) sh_any_odd = sh_unit_odd[0] = sh_unit_odd[1] = 0;
 
   f32x4 acc[FT];
@@ -131,7 +134,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
     if (mixed && sh_unit_odd[turn]) {  // (the same for all wavefronts)
 #pragma unroll 1
       for (int u = 0; u < NP / 2; ++u)
-        count_odd<D>(v_read + (16 * NP * kh + 32 * u) * Tile::RB, (uint32_t)(seen >> (32 * u)), sh_odd + qt * FT * 64, &sh_any_odd, lane);
+        count_odd<D>(v_read + (16 * NP * kh + 32 * u) * Tile::RB, (uint32_t)(seen >> (32 * u)), sh_odd + qt * FT / 4 * 64, &sh_any_odd, lane);
       barrier();
       clean_words(reinterpret_cast<uint32_t*>(sh_kv[1]) + 16 * wave * Tile::RB / 4, 16 * Tile::RB / 4, lane);
       barrier();
@@ -199,10 +202,7 @@ __global__ __launch_bounds__(256, 3) void cache_attn_shared_kernel(const CacheAt
   const float weight = sh_l[wave][c] == 0.f ? 0.f : KH == 1 ? 1.f : fast_exp2((m_run - m) * cl);
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) acc[ft] *= weight;
-  if (sh_any_odd && kh == 0) {  // (after the weight: it may be another wavefront that the query has its tokens of)
-#pragma unroll
-    for (int ft = 0; ft < FT; ++ft) put_odd(acc[ft], sh_odd[(qt * FT + ft) * 64 + lane]);
-  }
+  if (sh_any_odd && kh == 0) put_odd(acc, sh_odd + qt * FT / 4 * 64, lane);  // (after the weight: it may be another wavefront that the query has its tokens of)
   float* const sums = reinterpret_cast<float*>(sh_kv[0]);
   float* const mine = sums + (16 * wave + c) * RS + 4 * g;
 #pragma unroll
