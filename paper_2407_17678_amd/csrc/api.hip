@@ -826,9 +826,8 @@ int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, cons
   if (p.stride_row < 0 || (p.stride_row & 7) != 0 || p.stride_head < 0 || (p.stride_head & 7) != 0) return S2_ERR_ALIGN;
   if (p.stride_row > (int64_t)1 << 40 || p.stride_head > (int64_t)1 << 40) return S2_ERR_SHAPE;
   if (p.max_rows == 0) return S2_OK;
-  const int64_t grid = s2::kv_rows_tiles(p, c->nseq);
-  if (grid > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
-  return hip_ok(s2::launch_kv_rows(p, (int)grid, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+  if (s2::kv_rows_tiles(p, c->nseq) > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  return hip_ok(s2::launch_kv_rows(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
 // The most splits that the library takes for a call over a cache of any format.

@@ -8,6 +8,9 @@
 // Both move bytes and nothing else; D/8 lanes take a row, 16 bytes of bf16 each.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
+#include <limits>
+
 #include "kernels.h"
 #include "kv_cache.h"
 
@@ -15,90 +18,122 @@ namespace s2 {
 
 namespace {
 
-// Where the kv_rows grid's workgroup begins: rows [row, row + p.tile_rows) of the sequence's new ones, for p.tile_heads heads from `head`.
-struct Slot {
+// Tile `i` of a call: rows [row, row + p.tile_rows) of the sequence's own, for p.tile_heads heads from `head`.
+struct Tile {
   int b, row, head;
 };
-__device__ __forceinline__ Slot slot_of(const KvRowsParams& p, int wg) {
-  Slot s;
-  const int groups = p.by_heads_groups;  // workgroups side by side take heads of the same rows
-  const int t = wg / p.div_groups;
-  s.head = (wg - t * groups) * p.tile_heads;
+__device__ __forceinline__ Tile tile_of(const KvRowsParams& p, int i) {
+  Tile s;
+  const int groups = p.by_heads_groups;  // tiles side by side take heads of the same rows
+  const int t = i / p.div_groups;
+  s.head = (i - t * groups) * p.tile_heads;
   s.b = t / p.div_tiles;
   s.row = (t - s.b * p.row_tiles) * p.tile_rows;
   return s;
 }
 
+// A lane's eight features of a row, quantised, to `pool` (+ its lane's bytes) and the scale's byte to `scale` (a lane in four).
+template <int D, int FMT>
+__device__ __forceinline__ void put_row(const u32x4& x, int c, uint8_t* pool, uint8_t* scale_to) {
+  if constexpr (FMT == S2_KV_BF16) {
+    *reinterpret_cast<u32x4*>(pool + 16 * c) = x;
+  } else {
+    uint32_t a = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) a = max(a, max(x[e] & 0x7fffu, (x[e] >> 16) & 0x7fffu));
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xf, 0xf, true));  // (quads of lanes: 1032, 2301)
+    a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xf, 0xf, true));
+    constexpr int kCarry = FMT == S2_KV_MXFP8 ? 24 : 32, kTop = FMT == S2_KV_MXFP8 ? 8 : 2;
+    const bool held = a < 0x7f00u;
+    const uint32_t byte = held ? (uint32_t)max((int)((a + kCarry) >> 7) - kTop, 17) : 255u;
+    const float scale = scale_of(held ? byte : 127u);
+    if constexpr (FMT == S2_KV_MXFP8) {
+      u32x2 w;
+#pragma unroll
+      for (int e = 0; e < 2; ++e) {
+        s16x2_ r = {0, 0};
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e]), scale, false);
+        r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e + 1]), scale, true);
+        w[e] = held ? __builtin_bit_cast(uint32_t, r) : 0u;
+      }
+      *reinterpret_cast<u32x2*>(pool + 8 * c) = w;
+    } else {
+      uint32_t w = 0;
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[0]), scale, 0);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[1]), scale, 1);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[2]), scale, 2);
+      w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[3]), scale, 3);
+      *reinterpret_cast<uint32_t*>(pool + 4 * c) = held ? w : 0u;
+    }
+    if (c % 4 == 0) scale_to[c / 4] = (uint8_t)byte;
+  }
+}
+
+// A tile is a wavefront's: a lane looks the page of one of its (row, head) pairs up, and what then moves, 64 * 8 / D pairs to an instruction and two such
+// in flight at a time, are those that the cache holds: of a long prompt it is a few, and a tile without one costs a lookup.
 template <int D, int FMT>
 __global__ __launch_bounds__(256) void kv_append_kernel(const KvRowsParams p) {
-  constexpr int LPR = D / 8, RPI = 256 / LPR;  // lanes to a row, rows to a pass of the workgroup
-  const Slot s = slot_of(p, blockIdx.x);
-  const int tid = threadIdx.x, c = tid % LPR, first = tid / LPR;
+  constexpr int LPR = D / 8, RPI = 64 / LPR;  // lanes to a row, rows to an instruction
+  const int lane = threadIdx.x & 63, c = lane % LPR, mine = lane / LPR;
+  const int at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  if (at >= p.num_tiles) return;
+  const Tile s = tile_of(p, at);
   const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
   const int start = load_const<int32_t>(p.start + s.b);
-  int left_out = 0;
-  for (int i = first; i < p.tile_rows * p.tile_heads; i += RPI) {
-    const int head = s.head + i / p.tile_rows, item = s.row + i % p.tile_rows;
-    if (item >= n || head >= p.c.heads) continue;
-    const int64_t pos = (int64_t)start + item;
-    int row = lo + item;
-    if (p.rows) row = row >= 0 && row < p.num_items ? p.rows[row] : -1;
-    const int64_t blk = pos >> p.c.block_shift;
-    int page = -1;
-    if (pos >= 0 && blk < p.c.max_blocks && row >= 0 && row < p.num_rows) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
-    if (page < 0 || page >= p.c.num_pages) {
-      left_out += c == 0;
-      continue;
-    }
-    const int in_page = (int)(pos & ((1 << p.c.block_shift) - 1));
-    const int64_t from = row * p.stride_row + head * p.stride_head + 8 * c;
-    const int64_t to = page * p.c.page + (int64_t)in_page * p.c.tok;
-    const int64_t scale_to = page * p.c.scale_page + (int64_t)in_page * p.c.scale_tok;
+  if (s.row >= n) return;
+  // my pair
+  const int pairs = p.tile_rows * p.tile_heads;
+  const int head = s.head + (lane >> p.tile_shift), item = s.row + (lane & (p.tile_rows - 1));
+  const bool there = lane < pairs && item < n && head < p.c.heads;
+  const int64_t pos = (int64_t)start + item, blk = pos >> p.c.block_shift;
+  const int in_page = (int)(pos & ((1 << p.c.block_shift) - 1));
+  int row = lo + item, page = -1;
+  if (there && pos >= 0 && blk < p.c.max_blocks) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
+  if (there && p.rows) row = row >= 0 && row < p.num_items ? p.rows[row] : -1;
+  const bool held = row >= 0 && row < p.num_rows && page >= 0 && page < p.c.num_pages;
+  if (p.skipped) {
+    const int left_out = __popcll(__ballot(there && !held));
+    if (lane == 0 && left_out > 0) atomicAdd(p.skipped, left_out);
+  }
+  for (uint64_t todo = __ballot(held); todo;) {
+    constexpr int NI = 2;
+    u32x4 x[NI][2];
+    int from[NI];
+    bool good[NI];
 #pragma unroll
-    for (int kv = 0; kv < 2; ++kv) {
-      const u32x4 x = *reinterpret_cast<const u32x4*>((kv ? p.v : p.k) + from);
-      uint8_t* const pool = (kv ? p.c.v : p.c.k) + to;
-      if constexpr (FMT == S2_KV_BF16) {
-        *reinterpret_cast<u32x4*>(pool + 16 * c) = x;
-      } else {
-        uint32_t a = 0;
+    for (int i = 0; i < NI; ++i) {
+      // pairs that are held, RPI at a time: the one of my lanes
+      from[i] = 0;
+      good[i] = false;
 #pragma unroll
-        for (int e = 0; e < 4; ++e) a = max(a, max(x[e] & 0x7fffu, (x[e] >> 16) & 0x7fffu));
-        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0xB1, 0xf, 0xf, true));  // (quads of lanes: 1032, 2301)
-        a = max(a, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, 0x4E, 0xf, 0xf, true));
-        constexpr int kCarry = FMT == S2_KV_MXFP8 ? 24 : 32, kTop = FMT == S2_KV_MXFP8 ? 8 : 2;
-        const bool held = a < 0x7f00u;
-        const uint32_t byte = held ? (uint32_t)max((int)((a + kCarry) >> 7) - kTop, 17) : 255u;
-        const float scale = scale_of(held ? byte : 127u);
-        if constexpr (FMT == S2_KV_MXFP8) {
-          u32x2 w;
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            s16x2_ r = {0, 0};
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e]), scale, false);
-            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, two_of(x[2 * e + 1]), scale, true);
-            w[e] = held ? __builtin_bit_cast(uint32_t, r) : 0u;
-          }
-          *reinterpret_cast<u32x2*>(pool + 8 * c) = w;
-        } else {
-          uint32_t w = 0;
-          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[0]), scale, 0);
-          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[1]), scale, 1);
-          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[2]), scale, 2);
-          w = __builtin_amdgcn_cvt_scalef32_pk_fp4_bf16(w, two_of(x[3]), scale, 3);
-          *reinterpret_cast<uint32_t*>(pool + 4 * c) = held ? w : 0u;
+      for (int r = 0; r < RPI; ++r) {
+        if (mine == r) {
+          from[i] = todo ? __builtin_ctzll(todo) : 0;
+          good[i] = todo != 0;
         }
-        if (c % 4 == 0) (kv ? p.c.vs : p.c.ks)[scale_to + c / 4] = (uint8_t)byte;
+        todo &= todo - 1;
       }
+      const int r = __shfl(row, from[i], 64);
+      const int64_t src = r * p.stride_row + (s.head + (from[i] >> p.tile_shift)) * p.stride_head + 8 * c;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv)
+        if (good[i]) x[i][kv] = *reinterpret_cast<const u32x4*>((kv ? p.v : p.k) + src);
+    }
+#pragma unroll
+    for (int i = 0; i < NI; ++i) {
+      const int pg = __shfl(page, from[i], 64), in = __shfl(in_page, from[i], 64);
+      const int64_t to = pg * p.c.page + (int64_t)in * p.c.tok, scale_to = pg * p.c.scale_page + (int64_t)in * p.c.scale_tok;
+      if (!good[i]) continue;
+#pragma unroll
+      for (int kv = 0; kv < 2; ++kv) put_row<D, FMT>(x[i][kv], c, (kv ? p.c.v : p.c.k) + to, (kv ? p.c.vs : p.c.ks) + scale_to);
     }
   }
-  if (p.skipped && left_out > 0) atomicAdd(p.skipped, left_out);
 }
 
 template <int D, int FMT>
 __global__ __launch_bounds__(256) void kv_read_kernel(const KvRowsParams p) {
   constexpr int LPR = D / 8, RPI = 256 / LPR;
-  const Slot s = slot_of(p, blockIdx.x);
+  const Tile s = tile_of(p, blockIdx.x);
   const int tid = threadIdx.x, c = tid % LPR, first = tid / LPR;
   const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
   const int start = load_const<int32_t>(p.start + s.b);
@@ -141,38 +176,48 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const KvRowsParams p) {
 }
 
 template <int D, int FMT>
-hipError_t launch_rows(const KvRowsParams& p, int grid, hipStream_t stream) {
+hipError_t launch_rows(const KvRowsParams& p, hipStream_t stream) {
   if (p.k_out)
-    hipLaunchKernelGGL((kv_read_kernel<D, FMT>), dim3(grid), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((kv_read_kernel<D, FMT>), dim3(p.num_tiles), dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL((kv_append_kernel<D, FMT>), dim3(grid), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((kv_append_kernel<D, FMT>), dim3((unsigned)(((int64_t)p.num_tiles + 3) / 4)), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
 template <int D>
-hipError_t launch_format(const KvRowsParams& p, int grid, hipStream_t stream) {
+hipError_t launch_format(const KvRowsParams& p, hipStream_t stream) {
   switch (p.c.format) {
-    case S2_KV_BF16: return launch_rows<D, S2_KV_BF16>(p, grid, stream);
-    case S2_KV_MXFP8: return launch_rows<D, S2_KV_MXFP8>(p, grid, stream);
-    default: return launch_rows<D, S2_KV_MXFP4>(p, grid, stream);
+    case S2_KV_BF16: return launch_rows<D, S2_KV_BF16>(p, stream);
+    case S2_KV_MXFP8: return launch_rows<D, S2_KV_MXFP8>(p, stream);
+    default: return launch_rows<D, S2_KV_MXFP4>(p, stream);
   }
 }
 
 }  // namespace
 
 int64_t kv_rows_tiles(KvRowsParams& p, int nseq) {
-  p.tile_rows = 1;
-  while (p.tile_rows < 16 && p.tile_rows < p.max_rows) p.tile_rows *= 2;
-  p.tile_heads = 16 / p.tile_rows;
-  p.row_tiles = (int)(((int64_t)p.max_rows + p.tile_rows - 1) / p.tile_rows);
-  p.by_heads_groups = (p.c.heads + p.tile_heads - 1) / p.tile_heads;
+  // Pairs of a row and a head to a tile: of a wavefront that writes, as many as there are lanes, or fewer where there would not be eight wavefronts
+  // to a compute unit; 16 of a workgroup that reads.
+  auto tiles = [&](int pairs) {
+    p.tile_shift = 0;
+    while ((1 << p.tile_shift) < pairs && (1 << p.tile_shift) < p.max_rows) ++p.tile_shift;
+    p.tile_rows = 1 << p.tile_shift;
+    p.tile_heads = pairs / p.tile_rows;
+    p.row_tiles = (int)(((int64_t)p.max_rows + p.tile_rows - 1) / p.tile_rows);
+    p.by_heads_groups = (p.c.heads + p.tile_heads - 1) / p.tile_heads;
+    return (int64_t)nseq * p.row_tiles * p.by_heads_groups;
+  };
+  int pairs = p.k_out ? 16 : 64;
+  while (!p.k_out && pairs > 512 / p.c.head_dim && tiles(pairs) < 2048) pairs /= 2;
+  const int64_t n = tiles(pairs);
   p.div_groups = fast_div(p.by_heads_groups);
   p.div_tiles = fast_div(p.row_tiles);
-  return (int64_t)nseq * p.row_tiles * p.by_heads_groups;
+  p.num_tiles = (int)std::min<int64_t>(n, std::numeric_limits<int32_t>::max());
+  return n;
 }
 
-hipError_t launch_kv_rows(const KvRowsParams& p, int grid, hipStream_t stream) {
-  return p.c.head_dim == 128 ? launch_format<128>(p, grid, stream) : launch_format<64>(p, grid, stream);
+hipError_t launch_kv_rows(const KvRowsParams& p, hipStream_t stream) {
+  return p.c.head_dim == 128 ? launch_format<128>(p, stream) : launch_format<64>(p, stream);
 }
 
 }  // namespace s2
