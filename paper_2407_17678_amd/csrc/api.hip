@@ -840,7 +840,7 @@ int most_cache_splits(int64_t pairs, int64_t max_len) {
 // tokens (e4m3, D = 128, us: 8 heads of 47 units in 4 splits 13.2, 8 10.0, 16 9.0; 32 in 4 13.6, 8 11.2, 16 11.5; of 19 units in 4 10.1, 8 8.7, 16 10.3;
 // 64 of 31 to 46 units in 2 20.0, 4 15.3, 8 15.7), and else four workgroups of four to a compute unit where that leaves 24 units to each (512
 // of up to 46 units in one split 62.6, in two 65.6).
-// Trees of up to 16 nodes: a workgroup to a compute unit, and three units to it (it takes two at a time; bf16, D = 128, us: 32 pairs of 47 units in 4
+// Trees of up to 32 nodes: a workgroup to a compute unit, and three units to it (it takes two at a time; bf16, D = 128, us: 32 pairs of 47 units in 4
 // splits 19.8, 8 16.3, 12 19.0, 16 16.6; e4m3: 8 of 47 in 6 13.2, 16 11.0, 32 11.6; 256 of 46 in one 38.5, in two 41.6).
 // Larger ones, whose workgroups take a unit at a time between two barriers: two to a compute unit, and two units to each (64 nodes, bf16: 32 pairs of
 // 47 units in 4 27.4, 8 21.1, 16 22.0, 24 24.3; 40 nodes, e2m1: 4 of 47 in 12 15.0, 24 12.8, 32 13.6; 33 nodes, D = 64: 91 of 9 in 2 17.9, 6 15.9, 8 17.4).
@@ -848,7 +848,7 @@ int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, int
   const int S = lp->block_size;
   const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / S, nullptr, 0);
   const int64_t units = (blocks * S + 63) / 64, pairs = (int64_t)nseq * heads;
-  const int64_t want = nodes > 16  ? std::min<int64_t>((512 + pairs - 1) / pairs, units / 2)
+  const int64_t want = nodes > 32  ? std::min<int64_t>((512 + pairs - 1) / pairs, units / 2)
                        : nodes > 0 ? std::min<int64_t>(256 / pairs, units / 3)
                                    : std::max(std::min<int64_t>(s2::kCacheWideGroups / pairs, units / 2), std::min<int64_t>(1024 / pairs, units / 24));
   return (int)std::max<int64_t>(1, std::min<int64_t>(want, most_cache_splits(pairs, max_len)));

@@ -4,17 +4,21 @@
 // and, in a tree, over the node itself and those above it.  All nodes of a sequence share what they read: 4 D T flops to a
 // cached token's 2 rows, so that bytes bound it as long as products are matrix instructions and a row is brought to bf16 once.
 //
-// This kernel is for up to 16 queries, one tile of the 16x16x32 MFMA.  A wavefront takes 64 cached tokens at a time for all queries of a
+// This kernel is for up to 32 queries, one or two tiles of the 16x16x32 MFMA.  A wavefront takes 32 cached tokens at a time for all queries of a
 // (sequence, head), and nothing of the cache is shared between wavefronts: no barrier, four streams to a workgroup.  Scores are
 // formed as keys x queries: K comes from memory straight into the layout of the first operand (16 rows, four lanes to a row: CacheRows), a
 // lane of the result holds one query, and the probabilities are the second operand of the product with V as they stand.  V needs its tokens along the
-// contraction: its rows go through a piece of LDS that is the wavefront's own, written as they come and read by the transpose read.
+// contraction: its rows go through a piece of LDS that is the wavefront's own, written as they come and read by the transpose read.  (With K and V
+// shared by a workgroup in LDS, as for more queries, 24 nodes of 64 sequences over e4m3 took 251 us instead of 242, 20 of 8 sequences 27.4 instead of 23.1.)
 //
 // A tree's nodes lie in up to five block rows (64 nodes, blocks of 16).  The blocks that any of them keeps are walked once: row by row,
 // each block in the first row that keeps it, with one bit to a row that does.
 //
-// The units of 64 tokens of a (sequence, head) are shared by num_splits workgroups of four wavefronts; wavefronts merge through LDS,
-// splits through a second launch.
+// The units of 64 tokens of a (sequence, head) are shared by num_splits workgroups of four wavefronts, two of them to a unit; wavefronts merge through
+// LDS, splits through a second launch.
+//
+// The cache's bytes bound it: 4 nodes of 64 sequences over bf16 (32 heads of 31 to 47 blocks of 64 tokens, D = 128) 400 us, 5.7 TB/s; 24 nodes over e4m3
+// 242 us, 5.0 TB/s; 12 over e2m1 132 us, 4.7 TB/s.  8 nodes of one sequence of 32768 tokens take 16 us, of which the bytes are 8.
 #include <hip/hip_runtime.h>
 
 #include "cache_attn.h"
@@ -24,12 +28,12 @@ namespace s2 {
 
 namespace {
 
-// Wavefronts to a SIMD that the registers are limited for: as many as they fit without spilling.
-constexpr int waves_for(int D, int FMT) { return D == 64 ? 4 : FMT == S2_KV_BF16 ? 2 : 3; }
+// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling.
+constexpr int waves_for(int D, int FMT, int NQ) { return NQ == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : FMT == S2_KV_BF16 ? 2 : 3; }
 
 // SMALL: blocks of 16 or 32 tokens, so that a unit of 64 is gathered from four or two of the list's blocks; else it is a piece of one block.
-template <int D, int FMT, bool SMALL>
-__global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(const CacheAttnParams p) {
+template <int D, int FMT, int NQ, bool SMALL>
+__global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(const CacheAttnParams p) {
   using Rows = CacheRows<D, FMT>;
   using Tile = ChunkTile<D>;
   constexpr int W = 4, KK = D / 32, FT = D / 16;
@@ -37,8 +41,8 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   static_assert(16 * RS * 4 <= 32 * Tile::RB, "a tile of sums fits where V was");
 
   __shared__ __align__(16) uint16_t sh_v[W][32 * Tile::kStride];
-  __shared__ float sh_m[W][16], sh_l[W][16];
-  __shared__ uint32_t sh_odd[FT / 4 * 64];  // (count_odd)
+  __shared__ float sh_m[W][16 * NQ], sh_l[W][16 * NQ];
+  __shared__ uint32_t sh_odd[NQ * FT / 4 * 64];  // (count_odd)
   __shared__ uint32_t sh_any_odd;
 
   const int tid = threadIdx.x, lane = tid & 63, c = lane & 15, g = lane >> 4;
@@ -52,22 +56,33 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
   int L = load_const<int32_t>(p.seq_lens + b);
   L = min(max(L, tree ? 0 : 1), p.max_len);
   const Nodes nodes = nodes_of(p, b, L, lane);
-  // the query of my column
-  const int rel_q = __shfl(nodes.rel, c, 64);
-  const bool there_q = nodes.all >> c & 1;
-  bf16x8 qf[KK];
+  // the queries of my column
+  int rel_q[NQ];
+  bool there_q[NQ];
+  bf16x8 qf[NQ][KK];
 #pragma unroll
-  for (int kk = 0; kk < KK; ++kk)
-    qf[kk] = there_q ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + c * p.q_sn + Rows::feature(kk, g)) : bf16x8{};
+  for (int n = 0; n < NQ; ++n) {
+    const int node = 16 * n + c;
+    rel_q[n] = __shfl(nodes.rel, node, 64);
+    there_q[n] = nodes.all >> node & 1;
+#pragma unroll
+    for (int kk = 0; kk < KK; ++kk)
+      qf[n][kk] = there_q[n] ? *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + node * p.q_sn + Rows::feature(kk, g)) : bf16x8{};
+  }
 
-  for (int i = tid; i < FT / 4 * 64; i += 64 * W) sh_odd[i] = 0;
+  for (int i = tid; i < NQ * FT / 4 * 64; i += 64 * W) sh_odd[i] = 0;
   if (tid == 0) sh_any_odd = 0;
   __syncthreads();
 
-  f32x4 acc[FT];
-  float m_run = kNegInf, l_run = 0.f;
+  f32x4 acc[NQ][FT];
+  float m_run[NQ], l_run[NQ];
 #pragma unroll
-  for (int ft = 0; ft < FT; ++ft) acc[ft] = f32x4{};
+  for (int n = 0; n < NQ; ++n) {
+    m_run[n] = kNegInf;
+    l_run[n] = 0.f;
+#pragma unroll
+    for (int ft = 0; ft < FT; ++ft) acc[n][ft] = f32x4{};
+  }
 
   uint16_t* const my_v = sh_v[wave];
   const uint32_t v_write = lds_addr(my_v) + c * Tile::RB, v_read = lds_addr(my_v) + Tile::tr_lane(lane);
@@ -98,45 +113,53 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
       Rows::operands(x, g, out);
   };
 
-  f32x4 s[2];
-  uint32_t seen;
+  f32x4 s[NQ][2];
+  uint32_t seen[NQ];
   auto scores = [&](auto drafts, bool some, auto see) __attribute__((always_inline)) {
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       u32x4 k[KK];
       operands(kK, drafts, t, kr[t], k);
 #pragma unroll
-      for (int kk = 0; kk < KK; ++kk) s[t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[kk], kk ? s[t] : f32x4{});
+      for (int kk = 0; kk < KK; ++kk)
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) s[n][t] = mfma16(__builtin_bit_cast(bf16x8, k[kk]), qf[n][kk], kk ? s[n][t] : f32x4{});
     }
     if (some) {
-      seen = (uint32_t)(see() >> (32 * half));
 #pragma unroll
-      for (int t = 0; t < 2; ++t) mask_scores(s[t], seen, t, g);
+      for (int n = 0; n < NQ; ++n) {
+        seen[n] = (uint32_t)(see(n) >> (32 * half));
+#pragma unroll
+        for (int t = 0; t < 2; ++t) mask_scores(s[n][t], seen[n], t, g);
+      }
     }
   };
   auto sums = [&](auto drafts, bool mixed) __attribute__((always_inline)) {
-    float mx = kNegInf;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
+    for (int n = 0; n < NQ; ++n) {
+      float mx = kNegInf;
 #pragma unroll
-      for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[t][e]);
-    mx = max_halves(max_rows(mx));
-    const float m_new = fmaxf(m_run, mx);
-    const float mc = m_new == kNegInf ? 0.f : m_new * cl;
-    if (__any(m_new > m_run)) {
-      const float alpha = fast_exp2(m_run * cl - mc);  // (-inf before the first token: 0)
-      l_run *= alpha;
-      m_run = m_new;
+      for (int t = 0; t < 2; ++t)
 #pragma unroll
-      for (int ft = 0; ft < FT; ++ft) acc[ft] *= alpha;
-    }
+        for (int e = 0; e < 4; ++e) mx = fmaxf(mx, s[n][t][e]);
+      mx = max_halves(max_rows(mx));
+      const float m_new = fmaxf(m_run[n], mx);
+      const float mc = m_new == kNegInf ? 0.f : m_new * cl;
+      if (__any(m_new > m_run[n])) {
+        const float alpha = fast_exp2(m_run[n] * cl - mc);  // (-inf before the first token: 0)
+        l_run[n] *= alpha;
+        m_run[n] = m_new;
 #pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        s[t][e] = fast_exp2(__builtin_fmaf(s[t][e], cl, -mc));
-        l_run += s[t][e];
+        for (int ft = 0; ft < FT; ++ft) acc[n][ft] *= alpha;
       }
+#pragma unroll
+      for (int t = 0; t < 2; ++t)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s[n][t][e] = fast_exp2(__builtin_fmaf(s[n][t][e], cl, -mc));
+          l_run[n] += s[n][t][e];
+        }
+    }
     u32x4 v[2][KK];
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -152,16 +175,22 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
       odd = __any((odd_bits(v[0]) | odd_bits(v[1])) != 0);
     }
     if (odd) {
-      count_odd<D>(v_read, seen, sh_odd, &sh_any_odd, lane);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) count_odd<D>(v_read, seen[n], sh_odd + n * FT / 4 * 64, &sh_any_odd, lane);
       wait_lds();
       clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
       wait_lds();
     }
-    const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack2(s[0][0], s[0][1]), pack2(s[0][2], s[0][3]), pack2(s[1][0], s[1][1]), pack2(s[1][2], s[1][3])});
+    bf16x8 pf[NQ];
+#pragma unroll
+    for (int n = 0; n < NQ; ++n)
+      pf[n] = __builtin_bit_cast(
+          bf16x8, u32x4{pack2(s[n][0][0], s[n][0][1]), pack2(s[n][0][2], s[n][0][3]), pack2(s[n][1][0], s[n][1][1]), pack2(s[n][1][2], s[n][1][3])});
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft) {
       const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(v_read, v_read, Tile::tr_off(0, ft), Tile::tr_off(0, ft) + 16 * Tile::RB));
-      acc[ft] = mfma16(vf, pf, acc[ft]);
+#pragma unroll
+      for (int n = 0; n < NQ; ++n) acc[n][ft] = mfma16(vf, pf[n], acc[n][ft]);
     }
     asm volatile("" ::: "memory");
   };
@@ -174,7 +203,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
         Unit<SMALL> next;
         more = walk.template next<true>(p, next);
         // the next unit's K goes into the registers that the scores have freed, its V into those that the sums free
-        scores(kCached, w.some, [&] { return unit_seen(w, rel_q); });
+        scores(kCached, w.some, [&](int n) { return unit_seen(w, rel_q[n]); });
         __builtin_amdgcn_sched_barrier(0);
         load(kK, next, kr);
         __builtin_amdgcn_sched_barrier(0);
@@ -185,49 +214,57 @@ __global__ __launch_bounds__(256, waves_for(D, FMT)) void cache_attn_kernel(cons
       }
     }
   }
-  // the drafted tokens, 16 at most: the first half of a unit of their own
+  // the drafted tokens, 32 at most: the first half of a unit of their own
   if (tree && split == p.num_splits - 1 && wave == 0 && nodes.all) {
-    scores(kDrafts, true, [&] { return drafts_seen(nodes, h, c, rel_q); });
+    scores(kDrafts, true, [&](int n) { return drafts_seen(nodes, h, 16 * n + c, rel_q[n]); });
     sums(kDrafts, true);
   }
   const CacheAttnParams& pe = params_in_memory();
   // (both halves have walked the same units)
   if (pe.missing && lane == 0 && half == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 
-  // the wavefronts' sums, through where V was
-  l_run = sum_groups(l_run);
-  if (g == 0) {
-    sh_m[wave][c] = there_q ? m_run : kNegInf;
-    sh_l[wave][c] = there_q ? l_run : 0.f;
+  // the wavefronts' sums, a tile of queries at a time, through where V was
+#pragma unroll
+  for (int n = 0; n < NQ; ++n) {
+    l_run[n] = sum_groups(l_run[n]);
+    if (g == 0) {
+      sh_m[wave][16 * n + c] = there_q[n] ? m_run[n] : kNegInf;
+      sh_l[wave][16 * n + c] = there_q[n] ? l_run[n] : 0.f;
+    }
   }
-  __syncthreads();
-  float m = kNegInf;
-#pragma unroll
-  for (int w = 0; w < W; ++w) m = fmaxf(m, sh_m[w][c]);
-  // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
-  const float weight = sh_l[wave][c] == 0.f ? 0.f : fast_exp2((m_run - m) * cl);
-#pragma unroll
-  for (int ft = 0; ft < FT; ++ft) acc[ft] *= weight;
-  if (sh_any_odd && wave == 0) put_odd(acc, sh_odd, lane);  // (after the weight: it may be another wavefront that the query has its tokens of)
-  float* const mine = reinterpret_cast<float*>(my_v) + c * RS + 4 * g;
-#pragma unroll
-  for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] : f32x4{};
-  __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
   const int i = tid / TPR, d = 8 * (tid % TPR);
-  if (i >= 16 || i >= pe.nodes) return;
-  float mt = kNegInf, l = 0.f, o[8];
 #pragma unroll
-  for (int w = 0; w < W; ++w) mt = fmaxf(mt, sh_m[w][i]);
+  for (int n = 0; n < NQ; ++n) {
+    __syncthreads();
+    float m = kNegInf;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) o[e] = 0.f;
+    for (int w = 0; w < W; ++w) m = fmaxf(m, sh_m[w][16 * n + c]);
+    // (no maximum and no sum: no token; scores that are all NaN leave a sum of NaN)
+    const float weight = sh_l[wave][16 * n + c] == 0.f ? 0.f : fast_exp2((m_run[n] - m) * cl);
 #pragma unroll
-  for (int w = 0; w < W; ++w) {
-    if (sh_l[w][i] != 0.f) l += sh_l[w][i] * fast_exp2((sh_m[w][i] - mt) * cl);
+    for (int ft = 0; ft < FT; ++ft) acc[n][ft] *= weight;
+    // (after the weight: it may be another wavefront that the query has its tokens of)
+    if (sh_any_odd && wave == 0) put_odd(acc[n], sh_odd + n * FT / 4 * 64, lane);
+    float* const mine = reinterpret_cast<float*>(my_v) + c * RS + 4 * g;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) o[e] += reinterpret_cast<const float*>(sh_v[w])[i * RS + d + e];
+    for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q[n] ? acc[n][ft] : f32x4{};
+    __syncthreads();
+    const int node = 16 * n + i;
+    if (i >= 16 || node >= pe.nodes) continue;
+    float mt = kNegInf, l = 0.f, o[8];
+#pragma unroll
+    for (int w = 0; w < W; ++w) mt = fmaxf(mt, sh_m[w][node]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) o[e] = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (sh_l[w][node] != 0.f) l += sh_l[w][node] * fast_exp2((sh_m[w][node] - mt) * cl);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) o[e] += reinterpret_cast<const float*>(sh_v[w])[i * RS + d + e];
+    }
+    put_result<D>(pe, b, h, node, split, d, o, mt, l);
   }
-  put_result<D>(pe, b, h, i, split, d, o, mt, l);
 }
 
 // Merges the splits, a wavefront to a row of the result: lane i holds the weight of split i, groups of D/4 lanes add up the splits of their own, four
@@ -286,13 +323,21 @@ __global__ __launch_bounds__(256) void cache_attn_merge_kernel(const CacheAttnPa
   if (lane == 0 && p.lse) p.lse[row] = l == 0.f ? kNegInf : m * p.scale + __logf(l);
 }
 
-template <int D, int FMT>
+template <int D, int FMT, int NQ>
 void launch_blocks(const CacheAttnParams& p, hipStream_t stream) {
   const dim3 grid(p.nseq * p.heads * p.num_splits), block(256);
   if (p.block_size < 64)
-    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, true>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, NQ, true>), grid, block, 0, stream, p);
   else
-    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, false>), grid, block, 0, stream, p);
+    hipLaunchKernelGGL((cache_attn_kernel<D, FMT, NQ, false>), grid, block, 0, stream, p);
+}
+
+template <int D, int FMT>
+void launch_tiles(const CacheAttnParams& p, hipStream_t stream) {
+  if (p.nodes <= 16)
+    launch_blocks<D, FMT, 1>(p, stream);
+  else
+    launch_blocks<D, FMT, 2>(p, stream);
 }
 
 template <int D>
@@ -300,13 +345,13 @@ hipError_t launch_dim(const CacheAttnParams& p, hipStream_t stream) {
   hipError_t e;
   if (!p.parents && p.c.format != S2_KV_BF16) {
     e = launch_cache_decode(p, stream);
-  } else if (p.nodes > 16) {
+  } else if (p.nodes > 32) {
     e = launch_cache_attn_shared(p, stream);
   } else {
     switch (p.c.format) {
-      case S2_KV_BF16: launch_blocks<D, S2_KV_BF16>(p, stream); break;
-      case S2_KV_MXFP8: launch_blocks<D, S2_KV_MXFP8>(p, stream); break;
-      default: launch_blocks<D, S2_KV_MXFP4>(p, stream); break;
+      case S2_KV_BF16: launch_tiles<D, S2_KV_BF16>(p, stream); break;
+      case S2_KV_MXFP8: launch_tiles<D, S2_KV_MXFP8>(p, stream); break;
+      default: launch_tiles<D, S2_KV_MXFP4>(p, stream); break;
     }
     e = hipGetLastError();
   }

@@ -83,15 +83,6 @@ struct CacheRows {
     }
   }
 
-  // bf16 rows that are operands already
-  __device__ static __forceinline__ void take(Part& p, const u32x4 (&rows)[kFrags]) {
-    static_assert(!kScaled, "");
-#pragma unroll
-    for (int kk = 0; kk < kFrags; ++kk)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) p.x[4 * kk + e] = rows[kk][e];
-  }
-
   // its operands
   __device__ static __forceinline__ void operands(const Part& p, int g, u32x4 (&out)[kFrags]) {
     if constexpr (FMT == S2_KV_BF16) {
@@ -112,6 +103,18 @@ struct CacheRows {
 #pragma unroll
       for (int kk = 0; kk < kFrags; ++kk) out[kk] = values4(p.x[kk], s);
     }
+  }
+
+  // 8 or 4 bits: a lane's bytes with the operands 2 i and 2 i + 1 in each other's place
+  __device__ static __forceinline__ void turn(Part& p, bool turned) {
+    constexpr int N = FMT == S2_KV_MXFP8 ? 2 : 1;  // dwords to an operand
+#pragma unroll
+    for (int i = 0; i < kDwords; ++i)
+      if (i % (2 * N) < N) {
+        const uint32_t x = p.x[i], y = p.x[i + N];
+        p.x[i] = turned ? y : x;
+        p.x[i + N] = turned ? x : y;
+      }
   }
 
   // acc[8 * kk + e] += pr * (feature e of operand kk), in 32 bits
