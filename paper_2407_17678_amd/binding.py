@@ -482,7 +482,8 @@ def paged_cache(fmt, block_size, k_pages, v_pages, block_table, k_scales=None, v
 
 
 def s2_kv_append_paged(cache, k, v, cu_new, start, max_new, rows=None, skipped=None, stream=None):
-    """k, v: bf16 [rows, heads, D]; cu_new: device int32 [nseq + 1]; start: [nseq]; rows: int32, the row each item takes (None: its own)."""
+    """k, v: bf16 [rows, heads, D]; cu_new: device int32 [nseq + 1]; start: [nseq]; rows: int32, at least one, the row each item takes
+    (None: its own)."""
     _check(_marshal().kv_append(cache.raw, k, v, cu_new, start, max_new, rows, skipped, _stream(stream)), "s2_kv_append_paged")
 
 

@@ -816,6 +816,9 @@ int check_cache(const s2_paged_cache* c, s2::CacheRef& r) {
   return S2_OK;
 }
 
+// Workgroups of 256 threads to a launch: fewer than 2^32 threads.
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
+
 // What s2_kv_append_paged and s2_kv_read_paged have in common, and the launch.
 int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, const void* v, void* stream) {
   if (!p.cu || !p.start) return S2_ERR_NULL;
@@ -825,8 +828,10 @@ int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, cons
     return S2_ERR_ALIGN;
   if (p.stride_row < 0 || (p.stride_row & 7) != 0 || p.stride_head < 0 || (p.stride_head & 7) != 0) return S2_ERR_ALIGN;
   if (p.stride_row > (int64_t)1 << 40 || p.stride_head > (int64_t)1 << 40) return S2_ERR_SHAPE;
+  // (items beyond the last row or index are none that is moved)
+  if (!p.skipped) p.max_rows = std::min(p.max_rows, p.rows ? p.num_items : p.num_rows);
   if (p.max_rows == 0) return S2_OK;
-  if (s2::kv_rows_tiles(p, c->nseq) > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  if (s2::kv_rows_groups(p, c->nseq) > kMostGroups) return S2_ERR_SHAPE;
   return hip_ok(s2::launch_kv_rows(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
@@ -873,8 +878,10 @@ int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
       (reinterpret_cast<uintptr_t>(p.parents) & 3u) != 0 || (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0 ||
       (reinterpret_cast<uintptr_t>(p.missing) & 3u) != 0)
     return S2_ERR_ALIGN;
-  int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, p.parents ? p.nodes : 0, c->nseq, c->heads, max_len);
-  if ((int64_t)c->nseq * c->heads * splits > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  const bool decode = !p.parents && c->format != S2_KV_BF16;
+  int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, decode ? 0 : p.nodes, c->nseq, c->heads, max_len);
+  const int64_t pairs = (int64_t)c->nseq * c->heads;
+  if (pairs * splits > kMostGroups || (pairs * p.nodes + 3) / 4 > kMostGroups) return S2_ERR_SHAPE;
   auto bytes = [&](int n) { return s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, n); };
   // (a smaller workspace is for fewer splits, where the caller has not asked for a number)
   while (num_splits == 0 && splits > 1 && bytes(splits) > workspace_bytes) --splits;

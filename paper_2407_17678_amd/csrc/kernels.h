@@ -148,7 +148,7 @@ struct KvRowsParams {
   int32_t* skipped;
   int num_rows, num_items, max_rows;
   int64_t stride_row, stride_head;
-  // set by kv_rows_tiles: a tile is tile_rows = 1 << tile_shift rows of tile_heads heads
+  // set by kv_rows_groups: a tile is tile_rows = 1 << tile_shift rows of tile_heads heads
   int tile_rows, tile_shift, tile_heads, row_tiles, by_heads_groups, num_tiles;
   FastDiv div_groups, div_tiles;
 };
@@ -204,8 +204,8 @@ constexpr int decode_wide_groups(int block_size, int head_dim) {
   return block_size == 16 && head_dim == 64 ? 2 * kDecodeWideGroups : kDecodeWideGroups;
 }
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
-// The tiles of a launch over rows of a cache (sets the tile fields), and the launch.
-int64_t kv_rows_tiles(KvRowsParams& p, int nseq);
+// The workgroups of a launch over rows of a cache (sets the tile fields), and the launch.
+int64_t kv_rows_groups(KvRowsParams& p, int nseq);
 hipError_t launch_kv_rows(const KvRowsParams& p, hipStream_t stream);
 // Up to so many workgroups a decode step over 8 or 4 bits takes eight wavefronts to each instead of four.
 constexpr int kCacheWideGroups = 256;

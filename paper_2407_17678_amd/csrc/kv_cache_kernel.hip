@@ -180,7 +180,7 @@ hipError_t launch_rows(const KvRowsParams& p, hipStream_t stream) {
   if (p.k_out)
     hipLaunchKernelGGL((kv_read_kernel<D, FMT>), dim3(p.num_tiles), dim3(256), 0, stream, p);
   else
-    hipLaunchKernelGGL((kv_append_kernel<D, FMT>), dim3((unsigned)(((int64_t)p.num_tiles + 3) / 4)), dim3(256), 0, stream, p);
+    hipLaunchKernelGGL((kv_append_kernel<D, FMT>), dim3((p.num_tiles + 3) / 4), dim3(256), 0, stream, p);
   return hipGetLastError();
 }
 
@@ -195,7 +195,7 @@ hipError_t launch_format(const KvRowsParams& p, hipStream_t stream) {
 
 }  // namespace
 
-int64_t kv_rows_tiles(KvRowsParams& p, int nseq) {
+int64_t kv_rows_groups(KvRowsParams& p, int nseq) {
   // Pairs of a row and a head to a tile: 16 of a workgroup that reads, 16 of a wavefront that writes (8 prompts over e4m3: 8 53 us, 16 50, 32 54, 64 61: with
   // more the last ones run alone, with fewer more is looked up at a time than moved), or fewer where there would not be eight wavefronts to a compute unit.
   auto tiles = [&](int pairs) {
@@ -213,7 +213,7 @@ int64_t kv_rows_tiles(KvRowsParams& p, int nseq) {
   p.div_groups = fast_div(p.by_heads_groups);
   p.div_tiles = fast_div(p.row_tiles);
   p.num_tiles = (int)std::min<int64_t>(n, std::numeric_limits<int32_t>::max());
-  return n;
+  return p.k_out ? n : (n + 3) / 4;
 }
 
 hipError_t launch_kv_rows(const KvRowsParams& p, hipStream_t stream) {

@@ -100,6 +100,16 @@ def test_grids_beyond_int32_are_refused():
     assert _read(wide, num_rows=INT_MAX, max_rows=INT_MAX) == SHAPE
 
 
+def test_launches_of_more_than_32_bits_of_threads_are_refused():
+    few = _cache(nseq=1, heads=3)
+    assert _append(few, skipped=0xd000, max_new=INT_MAX) == SHAPE  # (without a counter it is the rows that there are)
+    assert _read(_cache(nseq=64, heads=256), num_rows=1 << 20, max_rows=1 << 20) == SHAPE
+    many = dict(nseq=4096, heads=8000)
+    for call in (_decode, _tree):
+        assert call(_cache(**many), params=dict(PARAMS, num_heads=8000), ws_bytes=1 << 60) == SHAPE
+    assert _tree(_cache(nseq=1024, heads=8000), params=dict(PARAMS, num_heads=8000), nodes=64, ws_bytes=1 << 60) == SHAPE
+
+
 def test_no_rows_need_no_memory():
     assert _append(_cache(), k=None, v=None, num_rows=0, max_new=0) == 0
     assert _read(_cache(), k=None, v=None, num_rows=0, max_rows=7) == 0

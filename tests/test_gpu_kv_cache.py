@@ -232,6 +232,27 @@ def test_pages_far_apart(fmt):
     assert int(torch.count_nonzero(raw[:1 << 20])) == 0
 
 
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
+def test_no_limit_on_the_rows(fmt):
+    """max_new and max_rows as large as they can be: the rows that there are."""
+    S, D, H = 16, 64, 3
+    rng = np.random.default_rng(12)
+    bits = synth.normal_bf16(rng, (70, H, D))
+    table, pages = _table(2, H, 5, rng)
+    pools = U.Pools(fmt, pages, S, D)
+    cache = pools.cache(_ints(table.tolist()))
+    k, cu, start = G.to_dev(bits), _ints([0, 1, 70]), _ints([3, 0])
+    most = 2 ** 31 - 1
+    B.s2_kv_append_paged(cache, k, k, cu, start, most)
+    outs = [torch.full((H, 71, D), 5.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    B.s2_kv_read_paged(cache, outs[0], outs[1], cu, start, most)
+    torch.cuda.synchronize()
+    value = U.held_rows(bits, fmt)[2].transpose(1, 0, 2)
+    for got in outs:
+        got = G.to_f64(got)
+        assert np.array_equal(got[:, :70], value) and np.all(got[:, 70] == 5)
+
+
 def test_nothing_to_write_or_read():
     pools = U.Pools("mxfp8", 2, 16, 64)
     cache = pools.cache(_ints([[[0]], [[1]]]))
