@@ -1,5 +1,5 @@
-// Internal: what the two kernels of attention over a paged cache (cache_attn_kernel.hip, cache_attn_shared_kernel.hip) have in common: the nodes of
-// a tree, the walk over the blocks that their rows keep, masks, and what is done about values of V that are not numbers.
+// Internal: what the kernels of attention over a paged cache (cache_attn_kernel.hip, cache_attn_shared_kernel.hip, cache_decode_kernel.hip) have in common: the
+// nodes of a tree, the walk over the blocks that their rows keep, masks, and what is done about values of V that are not numbers.
 #pragma once
 #include <hip/hip_runtime.h>
 

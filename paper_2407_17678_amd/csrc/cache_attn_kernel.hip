@@ -18,7 +18,8 @@
 // LDS, splits through a second launch.
 //
 // The cache's bytes bound it: 4 nodes of 64 sequences over bf16 (32 heads of 31 to 47 blocks of 64 tokens, D = 128) 400 us, 5.7 TB/s; 24 nodes over e4m3
-// 242 us, 5.0 TB/s; 12 over e2m1 132 us, 4.7 TB/s.  8 nodes of one sequence of 32768 tokens take 16 us, of which the bytes are 8.
+// 242 us, 5.0 TB/s; 12 over e2m1 132 us, 4.7 TB/s.  8 nodes of one sequence of 32768 tokens take 16 us, of which the bytes are 8.  Loads two units ahead
+// instead of one gain nothing (the registers that they take cost 2 to 10 %), nor does V in LDS before the softmax.
 #include <hip/hip_runtime.h>
 
 #include "cache_attn.h"
@@ -28,7 +29,8 @@ namespace s2 {
 
 namespace {
 
-// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling.
+// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling (D = 128: 141 over
+// e2m1, 152 over e4m3, 178 over bf16, and with two tiles 206, 217 and 239).
 constexpr int waves_for(int D, int FMT, int NQ) { return NQ == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : FMT == S2_KV_BF16 ? 2 : 3; }
 
 // SMALL: blocks of 16 or 32 tokens, so that a unit of 64 is gathered from four or two of the list's blocks; else it is a piece of one block.
@@ -181,6 +183,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
       clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
       wait_lds();
     }
+    // (P rounded to bf16, as everywhere in this library where it meets V in a matrix product; its sums are those of the unrounded ones)
     bf16x8 pf[NQ];
 #pragma unroll
     for (int n = 0; n < NQ; ++n)

@@ -6,8 +6,8 @@
 // forms its quarter of a row's score, the four quarters are added by lane permutations, and the row's probability is then where its V
 // is: a lane accumulates its quarter of the features over the rows of its own, and rows are added up once at the end.  Probabilities stay in 32 bits.
 //
-// 64 x 32 heads of 8192 to 32768 x 128: e4m3 213 us (5.5 TB/s), e2m1 in blocks of 16 76 us (4.8 TB/s); one sequence of 32768 over e4m3 11.1 us with
-// its merge. The matrix kernel of cache_attn_kernel.hip with one of its 16 columns in use, where a unit is a chain of LDS round trips (1250 cycles for its
+// 64 x 32 heads of 8192 to 32768 x 128: e4m3 213 us (5.5 TB/s), e2m1 in blocks of 16 73 us (5.0 TB/s); one sequence of 32768 over e4m3 11.8 us with
+// its merge.  The matrix kernel of cache_attn_kernel.hip with one of its 16 columns in use, where a unit is a chain of LDS round trips (1250 cycles for its
 // scores, 2850 for its sums): 217, 119 and 16.7 us.
 #include <hip/hip_runtime.h>
 
@@ -22,8 +22,8 @@ __device__ __forceinline__ float dot2(uint32_t a, uint32_t b, float c) {
   return __builtin_amdgcn_fdot2_f32_bf16(two_of(a), two_of(b), c, false);
 }
 
-// Wavefronts to a SIMD that the registers are limited for: as many as they fit without spilling (e4m3, D = 128, 20 registers spilled for three: 213 -> 394 us
-// for 64 x 32 heads of 8192 to 32768).
+// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling (e4m3, D = 128, with two instead of three: 213 and 213 us for 64 x 32
+// heads of 8192 to 32768, 3 to 6 % slower at 256 to 1024 (sequence, head) pairs).
 constexpr int waves_for(int D, int FMT) { return D == 128 && FMT == S2_KV_MXFP8 ? 3 : 4; }
 
 // W: wavefronts to a workgroup.
