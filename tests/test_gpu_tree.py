@@ -55,8 +55,9 @@ class Case:
                         self.pools.put(which, table[b, h, j], 0, held[cut], None if byte is None else byte[cut])
             self.k.append(ks)
             self.v.append(vs)
-        for b, h, j in evict:
-            table[b, h, j] = -1
+        for b, h, j in evict:  # (not a page: negative, or beyond the last)
+            table[b, h, j] = (-1, nseq * H * self.max_blocks + 1, 2 ** 31 - 1)[j % 3]
+        self.pages = nseq * H * self.max_blocks + 1
         self.table = table
 
     def keeps(self, h):
@@ -106,7 +107,7 @@ class Case:
         for b in range(n):
             L = self.lens[b]
             for h in range(H):
-                keeps, held = self.keeps(h), lambda j: self.table[b, h, j] >= 0  # noqa: B023
+                keeps, held = self.keeps(h), lambda j: 0 <= self.table[b, h, j] < self.pages  # noqa: B023
                 if self.tree:
                     o[b, h], lse[b, h], weight[b, h] = orc.tree_attention(q[b, h], self.k[b][h], self.v[b][h], kd[b, h], vd[b, h], self.parents[b], L, keeps,
                                                                           self.S, self.scale, self.max_blocks * self.S, held)
@@ -318,6 +319,70 @@ def test_decode_leaves_stale_rows_alone(fmt):
     """Rows behind the last token hold what was there before (the pools are filled with 0xFF: NaN)."""
     o, lse = Case(fmt, 128, 64, [1, 63, 65, 129], 2, None, local=4).check()
     assert np.all(np.isfinite(o))
+
+
+# ------------------------------------------------------------------------------------ far away
+
+
+def _attend(cache, H, D, S, L, T, params, splits=1):
+    """A decode step and a tree of T nodes (chains of three) over a cache of one sequence."""
+    rng = np.random.default_rng([T, D])
+    q, kd, vd = (G.to_dev(synth.normal_bf16(rng, (1, H, T, D))) for _ in range(3))
+    par = _ints([[i - 1 if i % 3 else -1 for i in range(T)]])
+    max_len = cache.tensors[2].shape[2] * S
+    ws = torch.empty(B.s2_attn_tree_workspace_bytes(1, H, T, D, max_len, splits), dtype=torch.uint8, device="cuda")
+    o, lse = torch.empty_like(q), torch.empty((1, H, T), dtype=torch.float32, device="cuda")
+    o1, lse1 = torch.empty_like(q[:, :, 0]), torch.empty((1, H), dtype=torch.float32, device="cuda")
+    missing = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.s2_attn_tree_paged(params, cache, q, kd, vd, par, _ints([L]), o, lse, 0.125, ws, missing=missing, num_splits=splits)
+    B.s2_attn_decode_paged_cache(params, cache, q[:, :, 0], _ints([L]), o1, lse1, 0.125, ws, missing=missing, num_splits=splits)
+    torch.cuda.synchronize()
+    assert int(missing.item()) == 0
+    return [x.clone() for x in (o, lse, o1, lse1)]
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("T", [3, 20, 50])
+def test_pages_far_apart(fmt, T):
+    """Pages more than 2^32 bytes from the pool's beginning: the same to the last bit as pages side by side."""
+    S, D, L = 16, 64, 40
+    far = 5 << 30
+    rb, e = U.row_bytes(D, fmt), 2 if fmt == "bf16" else 1
+    raw = torch.zeros(far + (1 << 20), dtype=torch.uint8, device="cuda")
+    make = lambda at: (raw[at:].view(torch.bfloat16) if fmt == "bf16" else raw[at:]).as_strided(  # noqa: E731
+        (2, S, rb // e), ((far - 4096) // e, rb // e, 1))
+    scale = lambda at: raw[at:].as_strided((2, S, D // 32), (far - 4096, D // 32, 1)) if fmt != "bf16" else None  # noqa: E731
+    table = _ints([[[1, 0, 1]]])  # (the third block is the first's page)
+    caches = [B.paged_cache(U.FORMATS[fmt], S, make(4096), make(65536), table, scale(131072), scale(196608)), U.Pools(fmt, 2, S, D).cache(table)]
+    k, v = (G.to_dev(synth.normal_bf16(np.random.default_rng(x), (2 * S, 1, D))) for x in (1, 2))
+    results = []
+    for cache in caches:
+        B.s2_kv_append_paged(cache, k, v, _ints([0, 2 * S]), _ints([0]), 2 * S)
+        results.append(_attend(cache, 1, D, S, L, T, B.layout_params(1, 1, S, 8, 2)))
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8"])
+@pytest.mark.parametrize("T", [3, 20, 50])
+@pytest.mark.parametrize("S", [16, 64])
+def test_a_billion_tokens(fmt, T, S):
+    """One sequence of nearly 2^30 tokens, of which the mask keeps twelve blocks: what attention of these side by side gives, to the last bit."""
+    D, blocks, every = 64, (1 << 30) // S, (1 << 28) // S
+    row = blocks - 3
+    kept = [0, every, 2 * every, 3 * every] + list(range(row - 7, row + 1))
+    table = np.full((1, 1, blocks), -1, dtype=np.int32)
+    table[0, 0, kept] = np.arange(12)
+    results = []
+    k, v = (G.to_dev(synth.normal_bf16(np.random.default_rng([S, x]), (S, 1, D))) for x in (1, 2))
+    for table, at, params in ((table, kept, B.layout_params(1, 1, S, 8, every)),
+                              (np.arange(13, dtype=np.int32).reshape(1, 1, 13) % 12, range(12), B.layout_params(1, 1, S, 1, 0, dense=1))):
+        cache = U.Pools(fmt, 12, S, D).cache(torch.from_numpy(table).cuda())
+        for i, j in enumerate(at):  # (each block other rows: the same in another order)
+            B.s2_kv_append_paged(cache, k, v, _ints([0, S]), _ints([j * S]), S, rows=_ints(np.roll(np.arange(S), i)))
+        results.append(_attend(cache, 1, D, S, at[-1] * S + 5, T, params))  # (nodes of three to a chain stay in the block row)
+    for a, b in zip(*results):
+        assert torch.equal(a, b) and bool(torch.isfinite(a).all())
 
 
 # ------------------------------------------------------------------------------------ as a program uses it
