@@ -33,6 +33,7 @@ __device__ __forceinline__ Nodes nodes_of(const CacheAttnParams& p, int b, int L
     x.above = (uint64_t)1 << lane;
 #pragma unroll
     for (int i = 0; i < 6; ++i) {  // (the chain above a node doubles each time)
+      if (!__any(up >= 0)) break;
       const int from = max(up, 0);
       const uint32_t lo = __shfl((uint32_t)x.above, from, 64), hi = __shfl((uint32_t)(x.above >> 32), from, 64);
       const int next = __shfl(up, from, 64);
@@ -253,16 +254,14 @@ __device__ __forceinline__ void clean_words(uint32_t* words, int n, int lane) {
     words[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
   }
 }
-// The results that what was found stands for, in place of the sums.
-template <int FT>
-__device__ __forceinline__ void put_odd(f32x4 (&acc)[FT], const uint32_t* found, int lane) {
-#pragma unroll
-  for (int ft = 0; ft < FT; ++ft)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const uint32_t x = found[ft / 4 * 64 + lane] >> (8 * (ft % 4) + 2 * e) & 3;
-      if (x) acc[ft][e] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
-    }
+// The results that what was found stands for, in place of a lane's sums (feature tile ft: four from sums[16 * ft]).
+template <int D>
+__device__ __forceinline__ void put_odd(float* sums, const uint32_t* found, int lane) {
+#pragma unroll 1
+  for (int i = 0; i < D / 4; ++i) {
+    const uint32_t x = found[i / 16 * 64 + lane] >> (2 * (i % 16)) & 3;
+    if (x) sums[16 * (i / 4) + i % 4] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
+  }
 }
 
 // Rows 16 t .. 16 t + 15 of drafted K or V, a lane's quarter of row c; a node that is not there may hold anything, nobody attends it, and it is
