@@ -148,7 +148,9 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
       const float m_new = fmaxf(m_run[n], mx);
       const float mc = m_new == kNegInf ? 0.f : m_new * cl;
       if (__any(m_new > m_run[n])) {
-        const float alpha = fast_exp2(m_run[n] * cl - mc);  // (-inf before the first token: 0)
+        // (0 before the first token; where the maximum stays exactly 1, which the difference of the two roundings does not give: a query's result
+        // is not to depend on whether another one's maximum has moved)
+        const float alpha = m_new > m_run[n] ? fast_exp2(m_run[n] * cl - mc) : 1.f;
         l_run[n] *= alpha;
         m_run[n] = m_new;
 #pragma unroll

@@ -131,7 +131,7 @@ __global__ __launch_bounds__(256, waves_for(D)) void cache_attn_shared_kernel(co
       const float m_new = fmaxf(m_run, mx);
       const float mc = m_new == kNegInf ? 0.f : m_new * cl;
       if (__any(m_new > m_run)) {
-        const float alpha = fast_exp2(m_run * cl - mc);  // (-inf before the first token: 0)
+        const float alpha = m_new > m_run ? fast_exp2(m_run * cl - mc) : 1.f;  // (see cache_attn_kernel.hip)
         l_run *= alpha;
         m_run = m_new;
 #pragma unroll

@@ -315,6 +315,38 @@ def test_nothing_of_what_a_node_does_not_attend(fmt, S, local):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("T", [14, 30, 64])
+@pytest.mark.parametrize("D, S, splits", [(64, 16, 1), (128, 16, 3), (128, 64, 2), (64, 128, 1)])
+def test_who_meets_what_is_no_number(fmt, T, D, S, splits):
+    """NaN and infinities in one cached block and in two nodes: whoever attends none of them has what it had, to the last bit."""
+    par = np.arange(-1, T - 1, dtype=np.int32)
+    par[T - 5:] = [-1, 0, T - 5, 1, -1]
+    L = 6 * S + S - 6
+    make = lambda: Case(fmt, D, S, [L, L - 2 * S], 2, np.stack([par, par]), local=2, stride=4, window=5)  # noqa: E731
+    clean, dirty = make(), make()
+    o, lse = clean.check(splits=splits)
+    bits = np.full((S, D), 0x7F80, dtype=np.uint16)
+    bits[::3], bits[1::3] = 0x7FC0, 0xFF80
+    held, byte, _ = U.held_rows(bits, fmt)
+    chains = orc.tree_chains(par)
+    meets = np.zeros((2, 2, T), dtype=bool)
+    for b, n in enumerate(clean.lens):
+        blk = n // S - 1  # kept by the row of the first nodes, and not by the next ones (unless it is a stripe of the head's)
+        for h in range(2):
+            for which in range(2):
+                dirty.pools.put(which, dirty.table[b, h, blk], 0, held, byte)
+            keeps = clean.keeps(h)
+            for i, chain in enumerate(chains):
+                row = (n + len(chain) - 1) // S
+                meets[b, h, i] = keeps(row, blk) or any(x in chain and keeps(row, (n + len(chains[x]) - 1) // S) for x in (T - 5, T - 2))
+    dirty.kd[:, :, T - 5], dirty.vd[:, :, T - 2] = 0x7FC0, 0xFF80
+    got, got_lse, _ = dirty.run(splits=splits)
+    assert meets.any()
+    assert np.array_equal(got[~meets], o[~meets]) and np.array_equal(got_lse[~meets], lse[~meets])
+    assert not np.isfinite(got[meets]).all(-1).any()
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
 def test_decode_leaves_stale_rows_alone(fmt):
     """Rows behind the last token hold what was there before (the pools are filled with 0xFF: NaN)."""
     o, lse = Case(fmt, 128, 64, [1, 63, 65, 129], 2, None, local=4).check()
