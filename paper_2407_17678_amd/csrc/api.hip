@@ -921,7 +921,15 @@ int decode_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
     d.num_splits = a->num_splits;
     d.page_stride = c->page_stride;
     d.tok_stride = c->tok_stride;
-    return decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+    int st = decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+    if (st == S2_ERR_WORKSPACE && a->num_splits == 0) {
+      // (a smaller workspace is for fewer splits, as below)
+      auto bytes = [&](int n) { return s2_attn_decode_workspace_bytes(c->nseq, c->heads, c->head_dim, c->max_blocks * c->block_size, n); };
+      d.num_splits = s2_attn_decode_default_splits(c->nseq, c->heads, c->max_blocks * c->block_size);
+      while (d.num_splits > 1 && bytes(d.num_splits) > workspace_bytes) --d.num_splits;
+      st = decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+    }
+    return st;
   }
   s2::CacheAttnParams p{};
   p.q = static_cast<const uint16_t*>(a->q);

@@ -421,6 +421,32 @@ def test_a_billion_tokens(fmt, T, S):
 
 
 @pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
+@pytest.mark.parametrize("T", [0, 9, 24, 45])
+def test_workspaces_of_any_size(fmt, T):
+    """With the splits left to the library any workspace from the size for one split on will do, and nothing behind it is written."""
+    par = np.stack([random_tree(np.random.default_rng(T), T)]) if T else None
+    c = Case(fmt, 128, 64, [4000], 2, par, local=30)
+    cache, lens, nodes = c.pools.cache(_ints(c.table)), _ints(c.lens), max(T, 1)
+    q, kd, vd = (G.to_dev(x) for x in (c.q, c.kd, c.vd))
+    size = lambda n: B.s2_attn_tree_workspace_bytes(1, 2, nodes, 128, c.max_blocks * 64, n)  # noqa: E731
+    want, _, weight, _ = c.oracle()
+    for given in [size(1), size(2), size(3) + 100, size(0)]:
+        raw = torch.full((size(0) + 4096,), 0xA5, dtype=torch.uint8, device="cuda")
+        if T:
+            o = torch.empty_like(q)
+            B.s2_attn_tree_paged(c.params, cache, q, kd, vd, _ints(par), lens, o, None, c.scale, raw[:given])
+        else:
+            o = torch.empty_like(q[:, :, 0])
+            B.s2_attn_decode_paged_cache(c.params, cache, q[:, :, 0].contiguous(), lens, o, None, c.scale, raw[:given])
+            o = o[:, :, None]
+        torch.cuda.synchronize()
+        assert np.all(np.abs(G.to_f64(o) - want) <= U.attention_bound(want, weight))
+        assert bool((raw[given:] == 0xA5).all())
+    with pytest.raises(B.S2Error):
+        B.s2_attn_decode_paged_cache(c.params, cache, q[:, :, 0].contiguous(), lens, o[:, :, 0].contiguous(), None, c.scale, raw[:size(1) // nodes - 256])
+
+
+@pytest.mark.parametrize("fmt", ["bf16", "mxfp8", "mxfp4"])
 def test_prompt_tree_accept_and_decode(fmt):
     """A prompt is written, a tree verified, the nodes accepted written by index, and the next decode step reads them: every
     step against the oracle on the rows as the cache holds them."""
