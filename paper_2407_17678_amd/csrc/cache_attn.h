@@ -209,7 +209,8 @@ __device__ __forceinline__ void mask_scores(f32x4& s, uint64_t seen, int t, int 
 
 // What a query does not attend stays out of its result whatever it holds; but its probability of 0 times an infinity or NaN in V is none.  Where
 // some query does not attend some token of a unit and V holds such values, they are taken out of V, and which of them a query attends is found by
-// products of ones and zeros and kept until the end, when they decide the result.
+// products of ones and zeros and kept until the end, when they are added to its sums: those of units that all queries attend are in them already, and an
+// infinity beside a NaN or the other infinity is a NaN.
 //
 // any_odd: whether one of these bf16 pairs is not finite (an exponent field of ones carries into its value's sign)
 template <int KK>
@@ -254,13 +255,13 @@ __device__ __forceinline__ void clean_words(uint32_t* words, int n, int lane) {
     words[i] = ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
   }
 }
-// The results that what was found stands for, in place of a lane's sums (feature tile ft: four from sums[16 * ft]).
+// What was found, added to a lane's sums (feature tile ft: four from sums[16 * ft]).
 template <int D>
-__device__ __forceinline__ void put_odd(float* sums, const uint32_t* found, int lane) {
+__device__ __forceinline__ void add_odd(float* sums, const uint32_t* found, int lane) {
 #pragma unroll 1
   for (int i = 0; i < D / 4; ++i) {
     const uint32_t x = found[i / 16 * 64 + lane] >> (2 * (i % 16)) & 3;
-    if (x) sums[16 * (i / 4) + i % 4] = x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
+    if (x) sums[16 * (i / 4) + i % 4] += x == 1 ? -kNegInf : x == 2 ? kNegInf : __builtin_nanf("");
   }
 }
 

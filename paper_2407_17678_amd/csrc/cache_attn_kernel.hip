@@ -253,7 +253,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q[n] ? acc[n][ft] : f32x4{};
     // (not before the weight: it may be another wavefront that the query has its tokens of)
-    if (sh_any_odd && wave == 0 && there_q[n]) put_odd<D>(mine, sh_odd + n * FT / 4 * 64, lane);
+    if (sh_any_odd && wave == 0 && there_q[n]) add_odd<D>(mine, sh_odd + n * FT / 4 * 64, lane);
     __syncthreads();
     const int node = 16 * n + i;
     if (i >= 16 || node >= pe.nodes) continue;

@@ -211,7 +211,7 @@ __global__ __launch_bounds__(256, waves_for(D)) void cache_attn_shared_kernel(co
   float* const mine = sums + (16 * wave + c) * RS + 4 * g;
 #pragma unroll
   for (int ft = 0; ft < FT; ++ft) *reinterpret_cast<f32x4*>(mine + 16 * ft) = there_q ? acc[ft] : f32x4{};
-  if (sh_any_odd && there_q) put_odd<D>(mine, sh_odd + wave * FT / 4 * 64, lane);
+  if (sh_any_odd && there_q) add_odd<D>(mine, sh_odd + wave * FT / 4 * 64, lane);
   __syncthreads();
   constexpr int TPR = D / 8;  // threads to a query, eight features each
   for (int i = tid / TPR; i < pe.nodes; i += 64 * W / TPR) {
