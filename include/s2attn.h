@@ -467,8 +467,8 @@ int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void
  * sequence are left as they were.  Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
 int s2_kv_read_paged(const s2_paged_cache* c, const s2_kv_read_args* a, void* stream);
 
-/* s2_attn_decode_paged / s2_attn_decode_paged_layout over a cache of any format (over S2_KV_BF16, with q and o contiguous, it is that
- * call).  The mask's block size and heads are the cache's.  Workspace: s2_attn_tree_workspace_bytes with nodes = 1
+/* s2_attn_decode_paged / s2_attn_decode_paged_layout over a cache of any format, q and o at any strides (over S2_KV_BF16 it is that
+ * call's arithmetic, to the last bit).  The mask's block size and heads are the cache's.  Workspace: s2_attn_tree_workspace_bytes with nodes = 1
  * (with num_splits = 0 less will do, down to the size for one split: the call then takes fewer splits).
  * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
 int s2_attn_decode_paged_cache(const s2_layout_params* p, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,

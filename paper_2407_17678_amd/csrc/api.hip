@@ -709,6 +709,8 @@ int decode_contiguous(const s2_layout_params* lp, const s2_layout* layout, const
   p.head_dim = a->head_dim;
   p.max_len = a->max_len;
   p.num_splits = splits;
+  p.q_ss = (int64_t)a->heads * a->head_dim;
+  p.q_sh = a->head_dim;
   p.kv_ss = a->kv_stride_seq;
   p.kv_sh = a->kv_stride_head;
   p.kv_st = a->kv_stride_tok;
@@ -718,7 +720,8 @@ int decode_contiguous(const s2_layout_params* lp, const s2_layout* layout, const
   return hip_ok(s2::launch_decode(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
-int decode_paged(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_decode_args* a, float scale,
+// (q and o: element (b, h, d) at b * q_ss + h * q_sh + d)
+int decode_paged(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_decode_args* a, int64_t q_ss, int64_t q_sh, float scale,
                  void* workspace, size_t workspace_bytes, void* stream) {
   if (!a->q || !a->k_pages || !a->v_pages || !a->block_table || !a->seq_lens || !a->o) return S2_ERR_NULL;
   if (!(scale > 0.f) || !std::isfinite(scale)) return S2_ERR_BAD_PARAM;
@@ -758,6 +761,8 @@ int decode_paged(const s2_layout_params* lp, const s2_layout* layout, const s2_p
   p.head_dim = a->head_dim;
   p.max_len = max_len;
   p.num_splits = splits;
+  p.q_ss = q_ss;
+  p.q_sh = q_sh;
   p.kv_ss = a->page_stride;
   p.kv_sh = 0;
   p.kv_st = a->tok_stride;
@@ -859,6 +864,7 @@ int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, int
   return (int)std::max<int64_t>(1, std::min<int64_t>(want, most_cache_splits(pairs, max_len)));
 }
 
+// A tree, or (without parents) a decode step over 8 or 4 bits.
 int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, s2::CacheAttnParams& p, float scale,
                  int num_splits, void* workspace, size_t workspace_bytes, void* stream) {
   if (!p.q || !p.seq_lens || !p.o) return S2_ERR_NULL;
@@ -878,8 +884,7 @@ int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
       (reinterpret_cast<uintptr_t>(p.parents) & 3u) != 0 || (reinterpret_cast<uintptr_t>(p.lse) & 3u) != 0 ||
       (reinterpret_cast<uintptr_t>(p.missing) & 3u) != 0)
     return S2_ERR_ALIGN;
-  const bool decode = !p.parents && c->format != S2_KV_BF16;
-  int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, decode ? 0 : p.nodes, c->nseq, c->heads, max_len);
+  int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, p.parents ? p.nodes : 0, c->nseq, c->heads, max_len);
   const int64_t pairs = (int64_t)c->nseq * c->heads;
   if (pairs * splits > kMostGroups || (pairs * p.nodes + 3) / 4 > kMostGroups) return S2_ERR_SHAPE;
   auto bytes = [&](int n) { return s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, n); };
@@ -901,9 +906,12 @@ int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
 
 int decode_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, const s2_cache_decode_args* a, float scale,
                  void* workspace, size_t workspace_bytes, void* stream) {
-  if (c->format == S2_KV_BF16 && (c->heads == 1 || a->q_stride_head == c->head_dim) &&
-      (c->nseq == 1 || a->q_stride_seq == (int64_t)c->heads * c->head_dim)) {
+  if (c->format == S2_KV_BF16) {
     if (c->block_size != lp->block_size) return S2_ERR_SHAPE;
+    if ((int64_t)c->nseq * c->heads > std::numeric_limits<int32_t>::max() / 64) return S2_ERR_SHAPE;
+    const int64_t ss = a->q_stride_seq, sh = a->q_stride_head;
+    if (ss < 0 || (ss & 7) != 0 || sh < 0 || (sh & 7) != 0 || (reinterpret_cast<uintptr_t>(a->lse) & 3u) != 0) return S2_ERR_ALIGN;
+    if (ss > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return S2_ERR_SHAPE;
     s2_paged_decode_args d{};
     d.q = a->q;
     d.k_pages = c->k_pages;
@@ -921,13 +929,13 @@ int decode_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
     d.num_splits = a->num_splits;
     d.page_stride = c->page_stride;
     d.tok_stride = c->tok_stride;
-    int st = decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+    int st = decode_paged(lp, layout, &d, ss, sh, scale, workspace, workspace_bytes, stream);
     if (st == S2_ERR_WORKSPACE && a->num_splits == 0) {
       // (a smaller workspace is for fewer splits, as below)
       auto bytes = [&](int n) { return s2_attn_decode_workspace_bytes(c->nseq, c->heads, c->head_dim, c->max_blocks * c->block_size, n); };
       d.num_splits = s2_attn_decode_default_splits(c->nseq, c->heads, c->max_blocks * c->block_size);
       while (d.num_splits > 1 && bytes(d.num_splits) > workspace_bytes) --d.num_splits;
-      st = decode_paged(lp, layout, &d, scale, workspace, workspace_bytes, stream);
+      st = decode_paged(lp, layout, &d, ss, sh, scale, workspace, workspace_bytes, stream);
     }
     return st;
   }
@@ -1064,7 +1072,7 @@ int s2_attn_decode_static(const s2_layout_params* lp, const s2_decode_args* a, f
 int s2_attn_decode_paged(const s2_layout_params* lp, const s2_paged_decode_args* a, float scale,
                          void* workspace, size_t workspace_bytes, void* stream) {
   if (!lp || !a) return S2_ERR_NULL;
-  return decode_paged(lp, nullptr, a, scale, workspace, workspace_bytes, stream);
+  return decode_paged(lp, nullptr, a, (int64_t)a->heads * a->head_dim, a->head_dim, scale, workspace, workspace_bytes, stream);
 }
 
 int s2_attn_decode_layout(const s2_layout* layout, const s2_decode_args* a, float scale, void* workspace,
@@ -1076,7 +1084,7 @@ int s2_attn_decode_layout(const s2_layout* layout, const s2_decode_args* a, floa
 int s2_attn_decode_paged_layout(const s2_layout* layout, const s2_paged_decode_args* a, float scale,
                                 void* workspace, size_t workspace_bytes, void* stream) {
   if (!layout || !a) return S2_ERR_NULL;
-  return decode_paged(&layout->p, layout, a, scale, workspace, workspace_bytes, stream);
+  return decode_paged(&layout->p, layout, a, (int64_t)a->heads * a->head_dim, a->head_dim, scale, workspace, workspace_bytes, stream);
 }
 
 int s2_layout_resident_blocks(const s2_layout* L, int32_t head, int32_t length, int32_t* blocks,

@@ -13,7 +13,7 @@ namespace s2 {
 constexpr float kNegInf = -__builtin_inff();
 constexpr int kMaxNodeRows = 5;  // block rows that 64 positions can lie in, blocks of 16 tokens
 
-// Node `lane` of a sequence's tree (without a tree one query, the last cached token's).
+// Node `lane` of a sequence's tree.
 struct Nodes {
   uint64_t above;    // it and the nodes above it, bits
   bool there;
@@ -24,29 +24,24 @@ struct Nodes {
 __device__ __forceinline__ Nodes nodes_of(const CacheAttnParams& p, int b, int L, int lane) {
   Nodes x;
   const int sh = p.c.block_shift;
-  int depth = 0;
-  x.above = 1;
-  x.there = lane == 0;
-  if (p.parents) {
-    int up = lane < p.nodes ? p.parents[(int64_t)b * p.nodes + lane] : -2;
-    if (up < -1 || up >= lane) up = -2;
-    x.above = (uint64_t)1 << lane;
+  int up = lane < p.nodes ? p.parents[(int64_t)b * p.nodes + lane] : -2;
+  if (up < -1 || up >= lane) up = -2;
+  x.above = (uint64_t)1 << lane;
 #pragma unroll
-    for (int i = 0; i < 6; ++i) {  // (the chain above a node doubles each time)
-      if (!__any(up >= 0)) break;
-      const int from = max(up, 0);
-      const uint32_t lo = __shfl((uint32_t)x.above, from, 64), hi = __shfl((uint32_t)(x.above >> 32), from, 64);
-      const int next = __shfl(up, from, 64);
-      if (up >= 0) {
-        x.above |= (uint64_t)hi << 32 | lo;
-        up = next;
-      }
+  for (int i = 0; i < 6; ++i) {  // (the chain above a node doubles each time)
+    if (!__any(up >= 0)) break;
+    const int from = max(up, 0);
+    const uint32_t lo = __shfl((uint32_t)x.above, from, 64), hi = __shfl((uint32_t)(x.above >> 32), from, 64);
+    const int next = __shfl(up, from, 64);
+    if (up >= 0) {
+      x.above |= (uint64_t)hi << 32 | lo;
+      up = next;
     }
-    depth = __popcll(x.above) - 1;
-    x.there = up == -1 && L + depth < p.max_len;
   }
-  x.row0 = (p.parents ? L : L - 1) >> sh;
-  x.rel = x.there && p.parents ? ((L + depth) >> sh) - x.row0 : 0;
+  const int depth = __popcll(x.above) - 1;
+  x.there = up == -1 && L + depth < p.max_len;
+  x.row0 = L >> sh;
+  x.rel = x.there ? ((L + depth) >> sh) - x.row0 : 0;
   x.all = __ballot(x.there);
   x.n_rows = x.all ? 1 : 0;
 #pragma unroll

@@ -1,7 +1,7 @@
-// Attention over a paged cache in bf16, 8 or 4 bits (section 4.1): a decode step, or a tree of drafted tokens to each sequence.
+// Attention of a tree of drafted tokens to each sequence over a paged cache in bf16, 8 or 4 bits (section 4.1).
 //
 // o_i = sum_j p_ij v_j / sum_j p_ij, p_ij = exp(scale q_i k_j - max), over the cached tokens that the node's block row of the mask keeps
-// and, in a tree, over the node itself and those above it.  All nodes of a sequence share what they read: 4 D T flops to a
+// and over the node itself and those above it.  All nodes of a sequence share what they read: 4 D T flops to a
 // cached token's 2 rows, so that bytes bound it as long as products are matrix instructions and a row is brought to bf16 once.
 //
 // This kernel is for up to 32 queries, one or two tiles of the 16x16x32 MFMA.  A wavefront takes 32 cached tokens at a time for all queries of a
@@ -52,11 +52,10 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
   const int item = blockIdx.x;
   const int bh = item / p.by_splits, split = item - bh * p.num_splits;
   const int b = bh / p.by_heads, h = bh - b * p.heads;
-  const bool tree = p.parents != nullptr;
   const float cl = p.scale_log2e;
 
   int L = load_const<int32_t>(p.seq_lens + b);
-  L = min(max(L, tree ? 0 : 1), p.max_len);
+  L = min(max(L, 0), p.max_len);
   const Nodes nodes = nodes_of(p, b, L, lane);
   // the queries of my column
   int rel_q[NQ];
@@ -220,7 +219,7 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
     }
   }
   // the drafted tokens, 32 at most: the first half of a unit of their own
-  if (tree && split == p.num_splits - 1 && wave == 0 && nodes.all) {
+  if (split == p.num_splits - 1 && wave == 0 && nodes.all) {
     scores(kDrafts, true, [&](int n) { return drafts_seen(nodes, h, 16 * n + c, rel_q[n]); });
     sums(kDrafts, true);
   }
@@ -348,7 +347,7 @@ void launch_tiles(const CacheAttnParams& p, hipStream_t stream) {
 template <int D>
 hipError_t launch_dim(const CacheAttnParams& p, hipStream_t stream) {
   hipError_t e;
-  if (!p.parents && p.c.format != S2_KV_BF16) {
+  if (!p.parents) {
     e = launch_cache_decode(p, stream);
   } else if (p.nodes > 32) {
     e = launch_cache_attn_shared(p, stream);

@@ -82,7 +82,7 @@ __global__ __launch_bounds__(64 * W, FAR ? 1 : D == 128 ? 2 : 4) void decode_spl
   // my 8 query features, as floats
   float qv[8];
   {
-    const bf16x8 q8 = *reinterpret_cast<const bf16x8*>(p.q + ((int64_t)b * p.heads + h) * D + 8 * c);
+    const bf16x8 q8 = *reinterpret_cast<const bf16x8*>(p.q + b * p.q_ss + h * p.q_sh + 8 * c);
 #pragma unroll
     for (int e = 0; e < 8; ++e) qv[e] = (float)q8[e];
   }
@@ -256,7 +256,7 @@ __global__ __launch_bounds__(64 * W, FAR ? 1 : D == 128 ? 2 : 4) void decode_spl
       // the only split of its (sequence, head): the result itself, no partials and no second kernel
       // (l == 0 only when nothing was attended: a paged cache with every kept block missing)
       const __bf16 out = (__bf16)(l > 0.f ? a / l : 0.f);
-      p.o[(int64_t)bh * D + tid] = *reinterpret_cast<const uint16_t*>(&out);
+      p.o[b * p.q_ss + h * p.q_sh + tid] = *reinterpret_cast<const uint16_t*>(&out);
       if (tid == 0 && p.lse) p.lse[bh] = l > 0.f ? m * p.scale + __logf(l) : kNegInf;
       return;
     }
@@ -322,7 +322,8 @@ __global__ __launch_bounds__(256) void decode_reduce_kernel(const DecodeParams p
   bf16x4 out;
 #pragma unroll
   for (int e = 0; e < 4; ++e) out[e] = (__bf16)(l > 0.f ? a[e] / l : 0.f);
-  *reinterpret_cast<bf16x4*>(p.o + (int64_t)bh * D + 4 * c) = out;
+  const int b = bh / p.by_heads, h = bh - b * p.heads;
+  *reinterpret_cast<bf16x4*>(p.o + b * p.q_ss + h * p.q_sh + 4 * c) = out;
   if (tid == 0 && p.lse) p.lse[bh] = l > 0.f ? m * p.scale + __logf(l) : kNegInf;
 }
 

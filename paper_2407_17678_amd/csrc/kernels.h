@@ -108,6 +108,7 @@ struct DecodeParams {
   float* part_acc;  // [nseq*heads*splits, head_dim]
   float* part_ml;   // [nseq*heads*splits, 2]  (max, sum)
   int nseq, heads, head_dim, max_len, num_splits;
+  int64_t q_ss, q_sh;  // of q and o
   int64_t kv_ss, kv_sh, kv_st;
   float scale, scale_log2e;
   int block_size, local_blocks, stride, window_blocks, dense, head_index_base;
@@ -153,7 +154,7 @@ struct KvRowsParams {
   FastDiv div_groups, div_tiles;
 };
 
-// Attention over such a cache: a decode step (parents == nullptr) or a tree of drafted tokens to a sequence.
+// Attention over such a cache: a decode step over 8 or 4 bits (parents == nullptr) or a tree of drafted tokens to a sequence.
 struct CacheAttnParams {
   CacheRef c;
   const uint16_t* q;
