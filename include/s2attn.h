@@ -178,7 +178,8 @@ typedef struct {
   const int32_t* rows;    /* DEVICE int32 [cu_new[nseq]] or NULL: the row that an item takes
                              (NULL: item i is row i)                                          */
   int32_t* skipped;       /* DEVICE int32[1] or NULL: the call ADDS the number of (item, head)
-                             pairs it left out; the caller zeroes it                          */
+                             pairs it left out; the caller zeroes it.  With it nseq * heads *
+                             max_new is at most 2^31 - 1, what it holds                        */
   int32_t num_rows;       /* rows of k and v: an item whose row is not one of them is left out */
   int32_t num_items;      /* entries of rows (without it not looked at): no item beyond them   */
   int32_t max_new;        /* no sequence has more new tokens (>= 0; what is beyond is not looked at) */
@@ -459,12 +460,15 @@ int s2_layout_resident_blocks(const s2_layout* layout, int32_t head, int32_t len
  * a row's values alone.  An item is left out for a head whose table does not hold its block (an evicted one), and
  * for all heads where its position is not in [0, max_blocks*block_size) or its row not in [0, num_rows); nothing but the rows of
  * the items written is touched.  Two items that name one position of one page leave either, but items may take the same row.
+ * max_new is a limit, not a size: sequences of any lengths take the time of their rows.  (num_rows, or with rows num_items, + 64 * nseq) * heads
+ * below 2^28 is always taken; SHAPE where a launch would be larger than the chip allows.
  * Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
 int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void* stream);
 
 /* Rows of the cache as bf16, what their codes stand for: sequence b's row i is the token at position start[b] + i.
  * A row whose block is not resident, or whose position is outside [0, max_blocks*block_size), comes out as zeros.  Rows that belong to no
- * sequence are left as they were.  Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
+ * sequence are left as they were.  max_rows and sizes as max_new and num_rows in s2_kv_append_paged.
+ * Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
 int s2_kv_read_paged(const s2_paged_cache* c, const s2_kv_read_args* a, void* stream);
 
 /* s2_attn_decode_paged / s2_attn_decode_paged_layout over a cache of any format, q and o at any strides (over S2_KV_BF16 it is that

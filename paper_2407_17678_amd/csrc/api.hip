@@ -821,9 +821,6 @@ int check_cache(const s2_paged_cache* c, s2::CacheRef& r) {
   return S2_OK;
 }
 
-// Workgroups of 256 threads to a launch: fewer than 2^32 threads.
-constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
-
 // What s2_kv_append_paged and s2_kv_read_paged have in common, and the launch.
 int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, const void* v, void* stream) {
   if (!p.cu || !p.start) return S2_ERR_NULL;
@@ -833,10 +830,13 @@ int cache_rows(s2::KvRowsParams& p, const s2_paged_cache* c, const void* k, cons
     return S2_ERR_ALIGN;
   if (p.stride_row < 0 || (p.stride_row & 7) != 0 || p.stride_head < 0 || (p.stride_head & 7) != 0) return S2_ERR_ALIGN;
   if (p.stride_row > (int64_t)1 << 40 || p.stride_head > (int64_t)1 << 40) return S2_ERR_SHAPE;
-  // (items beyond the last row or index are none that is moved)
-  if (!p.skipped) p.max_rows = std::min(p.max_rows, p.rows ? p.num_items : p.num_rows);
+  p.nseq = c->nseq;
+  p.bound = p.rows ? p.num_items : p.num_rows;
+  // (items beyond the last row or index are none that is moved; they are counted, in 32 bits)
+  if (!p.skipped) p.max_rows = std::min(p.max_rows, p.bound);
+  if (p.skipped && p.max_rows > std::numeric_limits<int32_t>::max() / ((int64_t)c->nseq * c->heads)) return S2_ERR_SHAPE;
   if (p.max_rows == 0) return S2_OK;
-  if (s2::kv_rows_groups(p, c->nseq) > kMostGroups) return S2_ERR_SHAPE;
+  if (s2::kv_rows_groups(p) > s2::kMostGroups) return S2_ERR_SHAPE;
   return hip_ok(s2::launch_kv_rows(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
 }
 
@@ -886,7 +886,7 @@ int attend_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
     return S2_ERR_ALIGN;
   int splits = num_splits > 0 ? num_splits : choose_cache_splits(lp, layout, p.parents ? p.nodes : 0, c->nseq, c->heads, max_len);
   const int64_t pairs = (int64_t)c->nseq * c->heads;
-  if (pairs * splits > kMostGroups || (pairs * p.nodes + 3) / 4 > kMostGroups) return S2_ERR_SHAPE;
+  if (pairs * splits > s2::kMostGroups || (pairs * p.nodes + 3) / 4 > s2::kMostGroups) return S2_ERR_SHAPE;
   auto bytes = [&](int n) { return s2_attn_tree_workspace_bytes(c->nseq, c->heads, p.nodes, c->head_dim, max_len, n); };
   // (a smaller workspace is for fewer splits, where the caller has not asked for a number)
   while (num_splits == 0 && splits > 1 && bytes(splits) > workspace_bytes) --splits;

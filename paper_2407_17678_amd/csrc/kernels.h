@@ -147,9 +147,11 @@ struct KvRowsParams {
   const int32_t* start;  // [nseq]
   const int32_t* rows;   // rows that the items take, nullptr = their own
   int32_t* skipped;
-  int num_rows, num_items, max_rows;
+  int nseq, num_rows, num_items, max_rows;
+  int bound;  // what lies at or beyond it of cu's numbering is no row, or no index of one
   int64_t stride_row, stride_head;
-  // set by kv_rows_groups: a tile is tile_rows = 1 << tile_shift rows of tile_heads heads
+  // set by kv_rows_groups: a tile is tile_rows = 1 << tile_shift rows of tile_heads heads; row_tiles of them to a sequence, or (packed) to all
+  bool packed;
   int tile_rows, tile_shift, tile_heads, row_tiles, by_heads_groups, num_tiles;
   FastDiv div_groups, div_tiles;
 };
@@ -205,8 +207,10 @@ constexpr int decode_wide_groups(int block_size, int head_dim) {
   return block_size == 16 && head_dim == 64 ? 2 * kDecodeWideGroups : kDecodeWideGroups;
 }
 hipError_t launch_decode(const DecodeParams& p, hipStream_t stream);
+// Workgroups of 256 threads to a launch: fewer than 2^32 threads.
+constexpr int64_t kMostGroups = ((int64_t)1 << 24) - 1;
 // The workgroups of a launch over rows of a cache (sets the tile fields), and the launch.
-int64_t kv_rows_groups(KvRowsParams& p, int nseq);
+int64_t kv_rows_groups(KvRowsParams& p);
 hipError_t launch_kv_rows(const KvRowsParams& p, hipStream_t stream);
 // Up to so many workgroups a decode step over 8 or 4 bits takes eight wavefronts to each instead of four.
 constexpr int kCacheWideGroups = 256;

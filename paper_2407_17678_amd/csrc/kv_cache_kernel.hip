@@ -20,18 +20,50 @@ namespace s2 {
 
 namespace {
 
-// Tile `i` of a call: rows [row, row + p.tile_rows) of the sequence's own, for p.tile_heads heads from `head`.
+// Tile `i` of a call: rows [row, row + p.tile_rows) of the n of sequence b, which begin at lo of the batch's numbering and at position `start`, for
+// p.tile_heads heads from `head`.
 struct Tile {
-  int b, row, head;
+  int b, row, head, lo, n, start;
 };
+// Either each sequence has as many tiles as the longest may need, or (packed) there are those of the rows that there are: then sequence b, whose rows
+// begin at lo, has the tiles from lo / tile_rows + b on, one more at most than its rows need, and the last sequence that begins at or before a tile is
+// found 64 at a time.  Of single rows it has those from lo on, and no tile without a row is between them.
 __device__ __forceinline__ Tile tile_of(const KvRowsParams& p, int i) {
   Tile s;
   const int groups = p.by_heads_groups;  // tiles side by side take heads of the same rows
   const int t = i / p.div_groups;
   s.head = (i - t * groups) * p.tile_heads;
-  s.b = t / p.div_tiles;
-  s.row = (t - s.b * p.row_tiles) * p.tile_rows;
-  return s;
+  if (!p.packed) {
+    s.b = t / p.div_tiles;
+    s.row = (t - s.b * p.row_tiles) * p.tile_rows;
+    s.lo = load_const<int32_t>(p.cu + s.b);
+    s.n = min(load_const<int32_t>(p.cu + s.b + 1) - s.lo, p.max_rows);
+    s.start = load_const<int32_t>(p.start + s.b);
+    return s;
+  }
+  const int lane = threadIdx.x & 63;
+  int first = 0, count = p.nseq;
+  for (;;) {
+    const int step = (count + 63) >> 6;
+    const bool is = lane * step < count;
+    const int b = first + (is ? lane * step : 0);
+    const int lo = p.cu[b], hi = p.cu[b + 1], start = p.start[b];
+    const int tile = (min(max(lo, 0), p.bound) >> p.tile_shift) + (p.tile_shift ? b : 0);
+    const int before = __popcll(__ballot(is && tile <= t));
+    const int last = max(before - 1, 0);
+    if (step == 1) {
+      s.b = first + last;
+      s.lo = __builtin_amdgcn_readlane(lo, last);
+      s.start = __builtin_amdgcn_readlane(start, last);
+      const int from = min(max(s.lo, 0), p.bound) - s.lo, end = min(max(__builtin_amdgcn_readlane(hi, last), 0), p.bound) - s.lo;
+      s.row = from + (t - __builtin_amdgcn_readlane(tile, last)) * p.tile_rows;
+      s.n = before ? min(end, p.max_rows) : 0;
+      if (!before) s.row = 0;
+      return s;
+    }
+    first += last * step;
+    count = min(step, count - last * step);
+  }
 }
 
 // A lane's eight features of a row, quantised, to `pool` (+ its lane's bytes) and the scale's byte to `scale` (a lane in four).
@@ -79,17 +111,25 @@ __global__ __launch_bounds__(256) void kv_append_kernel(const KvRowsParams p) {
   const int lane = threadIdx.x & 63, c = lane % LPR, mine = lane / LPR;
   const int at = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   if (at >= p.num_tiles) return;
+  if (p.packed && p.skipped && at == 0) {  // what no tile is for: items that are none
+    int none = 0;
+    for (int b = lane; b < p.nseq; b += 64) {
+      const int lo = p.cu[b], n = min(p.cu[b + 1] - lo, p.max_rows);
+      const int from = min(max(-lo, 0), max(n, 0)), end = max(min(n, p.bound - lo), from);
+      none += max(n, 0) - (end - from);
+    }
+    for (int x = 32; x; x >>= 1) none += __shfl_xor(none, x, 64);
+    if (lane == 0 && none > 0) atomicAdd(p.skipped, none * p.c.heads);
+  }
   const Tile s = tile_of(p, at);
-  const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
-  const int start = load_const<int32_t>(p.start + s.b);
-  if (s.row >= n) return;
+  if (s.row >= s.n) return;
   // my pair
   const int pairs = p.tile_rows * p.tile_heads;
   const int head = s.head + (lane >> p.tile_shift), item = s.row + (lane & (p.tile_rows - 1));
-  const bool there = lane < pairs && item < n && head < p.c.heads;
-  const int64_t pos = (int64_t)start + item, blk = pos >> p.c.block_shift;
+  const bool there = lane < pairs && item < s.n && head < p.c.heads;
+  const int64_t pos = (int64_t)s.start + item, blk = pos >> p.c.block_shift;
   const int in_page = (int)(pos & ((1 << p.c.block_shift) - 1));
-  int row = lo + item, page = -1;
+  int row = s.lo + item, page = -1;
   if (there && pos >= 0 && blk < p.c.max_blocks) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
   if (there && p.rows) row = row >= 0 && row < p.num_items ? p.rows[row] : -1;
   const bool held = row >= 0 && row < p.num_rows && page >= 0 && page < p.c.num_pages;
@@ -137,14 +177,12 @@ __global__ __launch_bounds__(256) void kv_read_kernel(const KvRowsParams p) {
   constexpr int LPR = D / 8, RPI = 256 / LPR;
   const Tile s = tile_of(p, blockIdx.x);
   const int tid = threadIdx.x, c = tid % LPR, first = tid / LPR;
-  const int lo = load_const<int32_t>(p.cu + s.b), n = min(load_const<int32_t>(p.cu + s.b + 1) - lo, p.max_rows);
-  const int start = load_const<int32_t>(p.start + s.b);
   for (int i = first; i < p.tile_rows * p.tile_heads; i += RPI) {
     const int head = s.head + i / p.tile_rows, item = s.row + i % p.tile_rows;
-    if (item >= n || head >= p.c.heads) continue;
-    const int row = lo + item;
+    if (item >= s.n || head >= p.c.heads) continue;
+    const int row = s.lo + item;
     if (row < 0 || row >= p.num_rows) continue;
-    const int64_t pos = (int64_t)start + item, blk = pos >> p.c.block_shift;
+    const int64_t pos = (int64_t)s.start + item, blk = pos >> p.c.block_shift;
     int page = -1;
     if (pos >= 0 && blk < p.c.max_blocks) page = p.c.table[((int64_t)s.b * p.c.heads + head) * p.c.max_blocks + blk];
     const bool held = page >= 0 && page < p.c.num_pages;
@@ -197,17 +235,34 @@ hipError_t launch_format(const KvRowsParams& p, hipStream_t stream) {
 
 }  // namespace
 
-int64_t kv_rows_groups(KvRowsParams& p, int nseq) {
+int64_t kv_rows_groups(KvRowsParams& p) {
   // Pairs of a row and a head to a tile: 16 of a workgroup that reads, 16 of a wavefront that writes (8 prompts over e4m3: 8 53 us, 16 50, 32 54, 64 61: with
   // more the last ones run alone, with fewer more is looked up at a time than moved), or fewer where there would not be eight wavefronts to a compute unit.
+  // A sequence's tiles are for the rows that the longest may have, or, where that is less than a third of them, a batch's are for the rows that there are: a tile
+  // without rows costs less than a tile's search for its sequence.  us, for the longest and for the rows that there are: 8 prompts over e4m3 whose tiles have rows to
+  // 21 % 13.9 and 12.0, 30 % 16.3 and 15.2, 39 % 17.7 and 18.1, 47 % 49.0 and 50.7, 82 % 27.0 and 33.4; read back 98 and 87, 123 and 118, 149 and 151, -, 271 and
+  // 314; 63 sequences of a token and one of 8192 (1.8 %) 63 and 11, read back 387 and 21.
   auto tiles = [&](int pairs) {
-    p.tile_shift = 0;
-    while ((1 << p.tile_shift) < pairs && (1 << p.tile_shift) < p.max_rows) ++p.tile_shift;
-    p.tile_rows = 1 << p.tile_shift;
-    p.tile_heads = pairs / p.tile_rows;
+    auto shape = [&](int64_t rows) {
+      p.tile_shift = 0;
+      while ((1 << p.tile_shift) < pairs && (1 << p.tile_shift) < rows) ++p.tile_shift;
+      p.tile_rows = 1 << p.tile_shift;
+      p.tile_heads = pairs / p.tile_rows;
+      p.by_heads_groups = (p.c.heads + p.tile_heads - 1) / p.tile_heads;
+    };
+    shape(std::min<int64_t>(p.max_rows, ((int64_t)p.bound + p.nseq - 1) / p.nseq));
+    const int64_t of_all = p.tile_shift ? (p.bound >> p.tile_shift) + (int64_t)p.nseq : std::max(p.bound, 1);
+    const int64_t packed = of_all * p.by_heads_groups;
+    p.packed = true;
+    p.row_tiles = (int)std::min<int64_t>(of_all, std::numeric_limits<int32_t>::max());
+    const KvRowsParams by_rows = p;
+    shape(p.max_rows);
     p.row_tiles = (int)(((int64_t)p.max_rows + p.tile_rows - 1) / p.tile_rows);
-    p.by_heads_groups = (p.c.heads + p.tile_heads - 1) / p.tile_heads;
-    return (int64_t)nseq * p.row_tiles * p.by_heads_groups;
+    const int64_t by_longest = (int64_t)p.nseq * p.row_tiles * p.by_heads_groups;
+    p.packed = 3 * packed < by_longest || (p.k_out ? by_longest : (by_longest + 3) / 4) > kMostGroups;
+    if (!p.packed) return by_longest;
+    p = by_rows;
+    return packed;
   };
   int pairs = 16;
   while (!p.k_out && pairs > 512 / p.c.head_dim && tiles(pairs) < 2048) pairs /= 2;
