@@ -236,7 +236,8 @@ hipError_t launch_format(const KvRowsParams& p, hipStream_t stream) {
 }  // namespace
 
 int64_t kv_rows_groups(KvRowsParams& p) {
-  // Pairs of a row and a head to a tile: 16 of a workgroup that reads, 16 of a wavefront that writes (8 prompts over e4m3: 8 53 us, 16 50, 32 54, 64 61: with
+  // Pairs of a row and a head to a tile: one to each D/8 lanes of a workgroup that reads (32 at D = 64, where with 16 half of the lanes had none: 32 heads of 32768
+  // over e2m1 73 us instead of 81, 16 of 8192 over e4m3 300 instead of 314), 16 of a wavefront that writes (8 prompts over e4m3: 8 53 us, 16 50, 32 54, 64 61: with
   // more the last ones run alone, with fewer more is looked up at a time than moved), or fewer where there would not be eight wavefronts to a compute unit.
   // A sequence's tiles are for the rows that the longest may have, or, where that is less than a third of them, a batch's are for the rows that there are: a tile
   // without rows costs less than a tile's search for its sequence.  us, for the longest and for the rows that there are: 8 prompts over e4m3 whose tiles have rows to
@@ -264,7 +265,7 @@ int64_t kv_rows_groups(KvRowsParams& p) {
     p = by_rows;
     return packed;
   };
-  int pairs = 16;
+  int pairs = p.k_out ? 2048 / p.c.head_dim : 16;
   while (!p.k_out && pairs > 512 / p.c.head_dim && tiles(pairs) < 2048) pairs /= 2;
   const int64_t n = tiles(pairs);
   p.div_groups = fast_div(p.by_heads_groups);
