@@ -486,7 +486,7 @@ int s2_attn_decode_paged_cache_layout(const s2_layout* layout, const s2_paged_ca
  * A node whose parent does not exist, or whose position is max_blocks*block_size or beyond, does not exist: its o is 0 and
  * its lse -inf, and its q, k, v are not looked at.  What a node does not attend stays out of its result whatever it
  * holds.  Of what it attends, a V that is NaN, or infinities of both signs, give NaN in their feature; infinities of one sign give that infinity, or
- * NaN where a probability is too small for 32 bits.  Kept blocks that are not resident contribute nothing and are counted, as in s2_attn_decode_paged.
+ * NaN where its token's probability is below 2^-100 of the largest one's.  Kept blocks that are not resident contribute nothing and are counted, as in s2_attn_decode_paged.
  * workspace: s2_attn_tree_workspace_bytes(..., max_blocks * block_size, num_splits) bytes, DEVICE, 256-byte aligned, contents
  * undefined on entry and exit (with num_splits = 0 less will do, down to the size for one split: the call then takes fewer splits).  With a
  * layout, it covers the cache.

@@ -202,6 +202,28 @@ __device__ __forceinline__ void mask_scores(f32x4& s, uint64_t seen, int t, int 
   for (int e = 0; e < 4; ++e) s[e] = mine >> e & 1 ? s[e] : kNegInf;
 }
 
+// Probabilities on their way to V: the second operand of a matrix product holds bf16, so each goes as two terms, its first eight bits and what is left of it,
+// 16 bits together.  (One rounded term is off by up to 2^-8, which a decode step, whose probabilities stay in 32 bits, is not; it would take one product of the two:
+// us with one and with two terms, 64 x 32 heads of 31 to 47 blocks of 64 tokens, bf16 24 nodes 428 and 429, e4m3 24 nodes 243 and 246, 64 nodes 303 and 340, e2m1 12
+// nodes 132 and 136, 24 nodes 165 and 185, 64 nodes 255 and 293.)  The first is cut, not rounded, and what is left counted 2^-23 too large, so that both are above 0
+// wherever the probability is above 2^-100: twice an infinity of V is that infinity, and not NaN.
+__device__ __forceinline__ void two_terms(float a, float b, uint32_t& first, uint32_t& rest) {
+  const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+  first = __builtin_amdgcn_perm(y, x, 0x07060302);
+  constexpr float kUp = 1.f + 0x1p-23f;
+  rest = pack2(__builtin_fmaf(a, kUp, -__builtin_bit_cast(float, x & 0xffff0000u)), __builtin_fmaf(b, kUp, -__builtin_bit_cast(float, y & 0xffff0000u)));
+}
+// those of two tiles of scores, as an operand each
+__device__ __forceinline__ void two_terms(const f32x4& lo, const f32x4& hi, bf16x8& first, bf16x8& rest) {
+  uint32_t a[4], b[4];
+  two_terms(lo[0], lo[1], a[0], b[0]);
+  two_terms(lo[2], lo[3], a[1], b[1]);
+  two_terms(hi[0], hi[1], a[2], b[2]);
+  two_terms(hi[2], hi[3], a[3], b[3]);
+  first = __builtin_bit_cast(bf16x8, u32x4{a[0], a[1], a[2], a[3]});
+  rest = __builtin_bit_cast(bf16x8, u32x4{b[0], b[1], b[2], b[3]});
+}
+
 // What a query does not attend stays out of its result whatever it holds; but its probability of 0 times an infinity or NaN in V is none.  Where
 // some query does not attend some token of a unit and V holds such values, they are taken out of V, and which of them a query attends is found by
 // products of ones and zeros and kept until the end, when they are added to its sums: those of units that all queries attend are in them already, and an

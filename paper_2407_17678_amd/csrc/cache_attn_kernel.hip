@@ -17,8 +17,8 @@
 // The units of 64 tokens of a (sequence, head) are shared by num_splits workgroups of four wavefronts, two of them to a unit; wavefronts merge through
 // LDS, splits through a second launch.
 //
-// The cache's bytes bound it: 4 nodes of 64 sequences over bf16 (32 heads of 31 to 47 blocks of 64 tokens, D = 128) 400 us, 5.7 TB/s; 24 nodes over e4m3
-// 242 us, 5.0 TB/s; 12 over e2m1 132 us, 4.7 TB/s.  8 nodes of one sequence of 32768 tokens take 16 us, of which the bytes are 8.  Loads two units ahead
+// The cache's bytes bound it: 4 nodes of 64 sequences over bf16 (32 heads of 31 to 47 blocks of 64 tokens, D = 128) 403 us, 5.7 TB/s; 24 nodes over e4m3
+// 246 us, 4.9 TB/s; 12 over e2m1 136 us, 4.6 TB/s.  8 nodes of one sequence of 32768 tokens take 16 us, of which the bytes are 8.  Loads two units ahead
 // instead of one gain nothing (the registers that they take cost 2 to 10 %), nor does V in LDS before the softmax.
 #include <hip/hip_runtime.h>
 
@@ -29,8 +29,8 @@ namespace s2 {
 
 namespace {
 
-// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling (D = 128: 141 over
-// e2m1, 152 over e4m3, 178 over bf16, and with two tiles 206, 217 and 239).
+// Wavefronts to a SIMD that the registers are limited for: as many as fit without spilling (D = 128: 140 over
+// e2m1, 151 over e4m3, 176 over bf16, and with two tiles 206, 217 and 238).
 constexpr int waves_for(int D, int FMT, int NQ) { return NQ == 2 ? (D == 64 ? 3 : 2) : D == 64 ? 4 : FMT == S2_KV_BF16 ? 2 : 3; }
 
 // SMALL: blocks of 16 or 32 tokens, so that a unit of 64 is gathered from four or two of the list's blocks; else it is a piece of one block.
@@ -184,17 +184,14 @@ __global__ __launch_bounds__(256, waves_for(D, FMT, NQ)) void cache_attn_kernel(
       clean_words(reinterpret_cast<uint32_t*>(my_v), 32 * Tile::RB / 4, lane);
       wait_lds();
     }
-    // (P rounded to bf16, as everywhere in this library where it meets V in a matrix product; its sums are those of the unrounded ones)
-    bf16x8 pf[NQ];
+    bf16x8 pf[NQ], pr[NQ];
 #pragma unroll
-    for (int n = 0; n < NQ; ++n)
-      pf[n] = __builtin_bit_cast(
-          bf16x8, u32x4{pack2(s[n][0][0], s[n][0][1]), pack2(s[n][0][2], s[n][0][3]), pack2(s[n][1][0], s[n][1][1]), pack2(s[n][1][2], s[n][1][3])});
+    for (int n = 0; n < NQ; ++n) two_terms(s[n][0], s[n][1], pf[n], pr[n]);
 #pragma unroll
     for (int ft = 0; ft < FT; ++ft) {
       const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(v_read, v_read, Tile::tr_off(0, ft), Tile::tr_off(0, ft) + 16 * Tile::RB));
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) acc[n][ft] = mfma16(vf, pf[n], acc[n][ft]);
+      for (int n = 0; n < NQ; ++n) acc[n][ft] = mfma16(vf, pf[n], mfma16(vf, pr[n], acc[n][ft]));
     }
     asm volatile("" ::: "memory");
   };

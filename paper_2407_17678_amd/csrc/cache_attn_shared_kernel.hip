@@ -6,9 +6,9 @@
 // fragments without bank conflicts); then each takes one tile of queries against the whole unit.  The next unit's bytes are on their way while this one
 // is worked on; two barriers a unit, whose waits other workgroups of the compute unit fill.
 //
-// 64 nodes of 16 sequences over bf16 (32 heads of 31 to 46 blocks of 64 tokens, D = 128) take 125 us, 5.0 TB/s.  Over 4 bits it is the compute unit: a unit is 32 KB
-// of LDS writes and 128 KB of reads, 1250 of the 1700 cycles that it takes, beside 800 of vector and 512 of matrix instructions a SIMD; 64 nodes of 64 sequences 256 us
-// (266 with bank conflicts in the writes), of which the bytes are 115.  Loads two units ahead: 1 % faster for 64 sequences over bf16, else up to 13 % slower.
+// 64 nodes of 16 sequences over bf16 (32 heads of 31 to 46 blocks of 64 tokens, D = 128) take 130 us, 4.8 TB/s.  Over 4 bits it is the compute unit: a unit is 32 KB
+// of LDS writes and 128 KB of reads, 1250 of the 1950 cycles that it takes, beside 960 of vector and 768 of matrix instructions a SIMD; 64 nodes of 64 sequences 293 us,
+// of which the bytes are 115 (with bank conflicts in the writes 10 more).  Loads two units ahead: 1 % faster for 64 sequences over bf16, else up to 13 % slower.
 #include <hip/hip_runtime.h>
 
 #include "cache_attn.h"
@@ -157,12 +157,12 @@ __global__ __launch_bounds__(256, waves_for(D)) void cache_attn_shared_kernel(co
     if (!any_q) return;
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      const f32x4 lo = s[2 * u], hi = s[2 * u + 1];
-      const bf16x8 pf = __builtin_bit_cast(bf16x8, u32x4{pack2(lo[0], lo[1]), pack2(lo[2], lo[3]), pack2(hi[0], hi[1]), pack2(hi[2], hi[3])});
+      bf16x8 pf, pr;
+      two_terms(s[2 * u], s[2 * u + 1], pf, pr);
 #pragma unroll
       for (int ft = 0; ft < FT; ++ft) {
         const bf16x8 vf = __builtin_bit_cast(bf16x8, lds_read_tr2(v_read, v_read, Tile::tr_off(u, ft), Tile::tr_off(u, ft) + 16 * Tile::RB));
-        acc[ft] = mfma16(vf, pf, acc[ft]);
+        acc[ft] = mfma16(vf, pf, mfma16(vf, pr, acc[ft]));
       }
     }
   };
