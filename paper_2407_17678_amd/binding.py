@@ -463,6 +463,8 @@ def s2_attn_decode_paged_layout(layout, q, k_pages, v_pages, block_table, seq_le
                                           num_splits, _stream(stream)), "s2_attn_decode_paged_layout")
 
 
+# The calls over a cache of any format check the types of their tensors' elements (AssertionError; codes and scale bytes may be any type of one byte) and refuse
+# limits and numbers of splits that do not fit 32 bits (OverflowError).
 KV_BF16, KV_MXFP8, KV_MXFP4 = 0, 1, 2
 
 

@@ -2,8 +2,8 @@
 // structures.  The smallest calls of this library are shorter than what the interpreter needed to make them (a
 // decode step of one short sequence 4.6 us on the GPU, 9.3 through ctypes structures, of which 3.0 to ask torch for its stream object).
 //
-// A tensor is whatever has torch's methods (data_ptr, stride, shape, is_contiguous, numel, element_size): nothing of torch is
-// compiled in, nothing is kept from one call to the next, and what the assertions of the ctypes form refused is refused here in its order.
+// A tensor is whatever has torch's methods (data_ptr, stride, shape, is_contiguous, numel, element_size, and for the calls over a cache of any format
+// dtype): nothing of torch is compiled in, nothing is kept from one call to the next, and what the assertions of the ctypes form refused is refused here in its order.
 // The functions return the status of the C entry point; binding.py turns it into an exception.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
@@ -48,8 +48,12 @@ union {
 constexpr Py_ssize_t kCacheEntryPoints = sizeof(CacheApi) / sizeof(void*);
 
 struct Names {
-  PyObject *data_ptr, *stride, *shape, *is_contiguous, *numel, *element_size, *value;
+  PyObject *data_ptr, *stride, *shape, *is_contiguous, *numel, *element_size, *value, *dtype;
 } names;
+// torch's objects for the types of elements, for as long as the process lives (set by bind_cache())
+struct Types {
+  PyObject *bf16, *i32, *f32;
+} types;
 
 // An owned reference.
 struct Ref {
@@ -387,38 +391,51 @@ PyObject* decode_paged_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { ret
 
 // ------------------------------------------------------------------------------------ a cache of any format
 
-// a tensor of n sizes whose elements are `bytes` long
-bool sizes_and_element(PyObject* t, int n, int64_t bytes, int64_t* out) {
-  if (!sizes_of(t, n, out)) return false;
+// an integer of 32 bits; any other is no limit, format or number of splits
+bool as_int(PyObject* o, int32_t& out) {
+  const Ref i(PyNumber_Index(o));
+  int64_t x;
+  if (!i.o || !as_i64(i.o, x)) return false;
+  out = (int32_t)x;
+  if (out == x) return true;
+  PyErr_Format(PyExc_OverflowError, "%lld does not fit 32 bits", (long long)x);
+  return false;
+}
+// a tensor whose elements are of this type, or (nullptr) of any of one byte
+bool is_of(PyObject* t, PyObject* type) {
+  if (type) {
+    const Ref have(PyObject_GetAttr(t, names.dtype));
+    return have.o && (have.o == type || fail_assert());
+  }
   const Ref e(PyObject_CallMethodNoArgs(t, names.element_size));
   int64_t have;
-  if (!e.o || !as_i64(e.o, have)) return false;
-  return have == bytes || fail_assert();
+  return e.o && as_i64(e.o, have) && (have == 1 || fail_assert());
 }
-// int32 values side by side, `count` of them; None if it may be
-bool ints_of(PyObject* t, int64_t count, const int32_t*& at) {
-  const Ref n(PyObject_CallMethodNoArgs(t, names.numel)), e(n.o ? PyObject_CallMethodNoArgs(t, names.element_size) : nullptr);
-  int64_t have, size;
-  if (!e.o || !as_i64(n.o, have) || !as_i64(e.o, size)) return false;
-  if (size != 4 || (count >= 0 && have != count)) return fail_assert();
+// the same, of n sizes
+bool sizes_and_type(PyObject* t, int n, PyObject* type, int64_t* out) { return sizes_of(t, n, out) && is_of(t, type); }
+// elements side by side, `count` of them (any number: count < 0)
+template <class T>
+bool row_of(PyObject* t, PyObject* type, int64_t count, T*& at) {
+  const Ref n(PyObject_CallMethodNoArgs(t, names.numel));
+  int64_t have;
+  if (!n.o || !as_i64(n.o, have) || !is_of(t, type)) return false;
+  if (count >= 0 && have != count) return fail_assert();
   return contiguous(t) && data_of(t, at);
 }
+bool ints_of(PyObject* t, int64_t count, const int32_t*& at) { return row_of(t, types.i32, count, at); }
 bool counter_of(PyObject* t, int32_t*& at) {
   at = nullptr;
-  const int32_t* one;
-  if (t == Py_None) return true;
-  if (!ints_of(t, 1, one)) return false;
-  at = const_cast<int32_t*>(one);
-  return true;
+  return t == Py_None || row_of(t, types.i32, 1, at);
 }
 
 // format, block_size, k_pages, v_pages, block_table, k_scales, v_scales -> the bytes of an s2_paged_cache
 PyObject* paged_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   s2_paged_cache c{};
-  if (!count_is(n, 7) || !as_i32(a[0], c.format) || !as_i32(a[1], c.block_size)) return nullptr;
+  if (!count_is(n, 7) || !as_int(a[0], c.format) || !as_int(a[1], c.block_size)) return nullptr;
   const bool scaled = c.format != S2_KV_BF16;
   int64_t k[3], v[3], table[3];
-  if (!sizes_and_element(a[2], 3, scaled ? 1 : 2, k) || !sizes_and_element(a[3], 3, scaled ? 1 : 2, v) || !sizes_and_element(a[4], 3, 4, table)) return nullptr;
+  PyObject* const type = scaled ? nullptr : types.bf16;
+  if (!sizes_and_type(a[2], 3, type, k) || !sizes_and_type(a[3], 3, type, v) || !sizes_and_type(a[4], 3, types.i32, table)) return nullptr;
   const Ref ks(strides_of(a[2])), vs(ks.o ? strides_of(a[3]) : nullptr);
   if (!vs.o || !same(ks.o, vs.o) || !unit_stride(ks.o, 2) || !contiguous(a[4])) return nullptr;
   const int64_t D = c.format == S2_KV_MXFP4 ? 2 * k[2] : k[2];
@@ -430,7 +447,7 @@ PyObject* paged_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   if (!stride_at(ks.o, 0, c.page_stride) || !stride_at(ks.o, 1, c.tok_stride)) return nullptr;
   if (scaled) {
     int64_t sk[3], sv[3];
-    if (!sizes_and_element(a[5], 3, 1, sk) || !sizes_and_element(a[6], 3, 1, sv)) return nullptr;
+    if (!sizes_and_type(a[5], 3, nullptr, sk) || !sizes_and_type(a[6], 3, nullptr, sv)) return nullptr;
     const Ref sks(strides_of(a[5])), svs(sks.o ? strides_of(a[6]) : nullptr);
     if (!svs.o || !same(sks.o, svs.o) || !unit_stride(sks.o, 2)) return nullptr;
     for (int i = 0; i < 3; ++i)
@@ -464,7 +481,7 @@ bool cache_of(PyObject* o, s2_paged_cache& c) {
 // two bf16 tensors of the same strides, of `n` sizes, the last of them features side by side; their sizes and the strides of the first two
 bool pair_of(PyObject* a, PyObject* b, int n, int64_t* size, int64_t* stride) {
   int64_t other[4];
-  if (!sizes_and_element(a, n, 2, size) || !sizes_and_element(b, n, 2, other)) return false;
+  if (!sizes_and_type(a, n, types.bf16, size) || !sizes_and_type(b, n, types.bf16, other)) return false;
   for (int i = 0; i < n; ++i)
     if (size[i] != other[i]) return fail_assert();
   const Ref as(strides_of(a)), bs(as.o ? strides_of(b) : nullptr);
@@ -484,7 +501,7 @@ PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k 
     fail_assert();
     return nullptr;
   }
-  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_new) || !ints_of(a[4], c.nseq, d.start) || !as_i32(a[5], d.max_new) || !counter_of(a[7], d.skipped)) return nullptr;
+  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_new) || !ints_of(a[4], c.nseq, d.start) || !as_int(a[5], d.max_new) || !counter_of(a[7], d.skipped)) return nullptr;
   if (a[6] != Py_None) {
     const Ref count(PyObject_CallMethodNoArgs(a[6], names.numel));
     int64_t items;
@@ -513,7 +530,7 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k v 
     fail_assert();
     return nullptr;
   }
-  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_rows) || !ints_of(a[4], c.nseq, d.start) || !as_i32(a[5], d.max_rows) || !data_of(a[1], d.k) ||
+  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_rows) || !ints_of(a[4], c.nseq, d.start) || !as_int(a[5], d.max_rows) || !data_of(a[1], d.k) ||
       !data_of(a[2], d.v) || !as_address(a[6], stream))
     return nullptr;
   d.num_rows = (int32_t)size[1];
@@ -525,11 +542,7 @@ PyObject* kv_read(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k v 
 // fp32 [nseq, heads, ...] side by side, `count` of them, or None
 bool lse_of(PyObject* t, int64_t count, float*& at) {
   at = nullptr;
-  if (t == Py_None) return true;
-  const int32_t* words;
-  if (!ints_of(t, count, words)) return false;
-  at = reinterpret_cast<float*>(const_cast<int32_t*>(words));
-  return true;
+  return t == Py_None || row_of(t, types.f32, count, at);
 }
 
 // params or layout, cache, q seq_lens o lse, scale, workspace, missing, num_splits, stream
@@ -547,7 +560,7 @@ PyObject* over_cache(PyObject* const* a, Py_ssize_t n) {
     return nullptr;
   }
   if (!ints_of(a[3], c.nseq, d.seq_lens) || !lse_of(a[5], (int64_t)c.nseq * c.heads, d.lse) || !counter_of(a[8], d.missing) || !data_of(a[2], d.q) ||
-      !data_of(a[4], d.o) || !as_i32(a[9], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[6], scale) || !workspace_of(a[7], ws, bytes) ||
+      !data_of(a[4], d.o) || !as_int(a[9], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[6], scale) || !workspace_of(a[7], ws, bytes) ||
       !as_address(a[10], stream))
     return nullptr;
   d.q_stride_seq = stride[0];
@@ -583,7 +596,7 @@ PyObject* drafts(PyObject* const* a, Py_ssize_t n) {
   }
   if (!ints_of(a[5], c.nseq * size[2], d.parents) || !ints_of(a[6], c.nseq, d.seq_lens) ||
       !lse_of(a[8], (int64_t)c.nseq * c.heads * size[2], d.lse) || !counter_of(a[11], d.missing) || !data_of(a[2], d.q) || !data_of(a[3], d.k) ||
-      !data_of(a[4], d.v) || !data_of(a[7], d.o) || !as_i32(a[12], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[9], scale) ||
+      !data_of(a[4], d.v) || !data_of(a[7], d.o) || !as_int(a[12], d.num_splits) || !as_address(a[0], pattern) || !as_float(a[9], scale) ||
       !workspace_of(a[10], ws, bytes) || !as_address(a[13], stream))
     return nullptr;
   d.nodes = (int32_t)size[2];
@@ -614,7 +627,17 @@ PyObject* bind_to(void** to, Py_ssize_t count, PyObject* const* a, Py_ssize_t n)
   Py_RETURN_NONE;
 }
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) { return bind_to(api.at, kEntryPoints, a, n); }
-PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t n) { return bind_to(cache_api.at, kCacheEntryPoints, a, n); }
+PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+  const Ref torch(PyImport_ImportModule("torch"));
+  if (!torch.o) return nullptr;
+  const struct {
+    PyObject** at;
+    const char* name;
+  } all[] = {{&types.bf16, "bfloat16"}, {&types.i32, "int32"}, {&types.f32, "float32"}};
+  for (const auto& t : all)
+    if (!*t.at && !(*t.at = PyObject_GetAttrString(torch.o, t.name))) return nullptr;
+  return bind_to(cache_api.at, kCacheEntryPoints, a, n);
+}
 
 #define S2_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {S2_METHOD(bind),          S2_METHOD(fwd),          S2_METHOD(fwd_rows),      S2_METHOD(fwd_varlen),
@@ -633,7 +656,8 @@ PyMODINIT_FUNC PyInit__marshal(void) {
     PyObject** at;
     const char* text;
   } const all[] = {{&names.data_ptr, "data_ptr"}, {&names.stride, "stride"},   {&names.shape, "shape"}, {&names.is_contiguous, "is_contiguous"},
-                   {&names.numel, "numel"},       {&names.element_size, "element_size"}, {&names.value, "value"}};
+                   {&names.numel, "numel"},       {&names.element_size, "element_size"}, {&names.value, "value"},
+                   {&names.dtype, "dtype"}};
   for (const auto& n : all)
     if (!(*n.at = PyUnicode_InternFromString(n.text))) return nullptr;
   const Ref m(PyModule_Create(&module));
