@@ -428,6 +428,19 @@ bool counter_of(PyObject* t, int32_t*& at) {
   return t == Py_None || row_of(t, types.i32, 1, at);
 }
 
+// the strides of two tensors of the same n sizes, which are the same, features side by side; of a size of 1 any is (it is given as 0)
+bool strides_of_both(PyObject* a, PyObject* b, int n, const int64_t* size, int64_t* stride) {
+  const Ref as(strides_of(a)), bs(as.o ? strides_of(b) : nullptr);
+  if (!bs.o || !unit_stride(as.o, n - 1) || !unit_stride(bs.o, n - 1)) return false;
+  for (int i = 0; i < n - 1; ++i) {
+    int64_t other;
+    if (!stride_at(as.o, i, stride[i]) || !stride_at(bs.o, i, other)) return false;
+    if (size[i] == 1) stride[i] = 0;
+    else if (stride[i] != other) return fail_assert();
+  }
+  return true;
+}
+
 // format, block_size, k_pages, v_pages, block_table, k_scales, v_scales -> the bytes of an s2_paged_cache
 PyObject* paged_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   s2_paged_cache c{};
@@ -436,27 +449,27 @@ PyObject* paged_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
   int64_t k[3], v[3], table[3];
   PyObject* const type = scaled ? nullptr : types.bf16;
   if (!sizes_and_type(a[2], 3, type, k) || !sizes_and_type(a[3], 3, type, v) || !sizes_and_type(a[4], 3, types.i32, table)) return nullptr;
-  const Ref ks(strides_of(a[2])), vs(ks.o ? strides_of(a[3]) : nullptr);
-  if (!vs.o || !same(ks.o, vs.o) || !unit_stride(ks.o, 2) || !contiguous(a[4])) return nullptr;
+  int64_t stride[2];
+  if (!strides_of_both(a[2], a[3], 3, k, stride) || !contiguous(a[4])) return nullptr;
   const int64_t D = c.format == S2_KV_MXFP4 ? 2 * k[2] : k[2];
   if (k[0] != v[0] || k[1] != v[1] || k[2] != v[2] || k[1] != c.block_size || k[0] > INT32_MAX || table[0] > INT32_MAX || table[1] > INT32_MAX ||
       table[2] > INT32_MAX || D > INT32_MAX) {
     fail_assert();
     return nullptr;
   }
-  if (!stride_at(ks.o, 0, c.page_stride) || !stride_at(ks.o, 1, c.tok_stride)) return nullptr;
+  c.page_stride = stride[0];
+  c.tok_stride = stride[1];
   if (scaled) {
     int64_t sk[3], sv[3];
     if (!sizes_and_type(a[5], 3, nullptr, sk) || !sizes_and_type(a[6], 3, nullptr, sv)) return nullptr;
-    const Ref sks(strides_of(a[5])), svs(sks.o ? strides_of(a[6]) : nullptr);
-    if (!svs.o || !same(sks.o, svs.o) || !unit_stride(sks.o, 2)) return nullptr;
     for (int i = 0; i < 3; ++i)
       if (sk[i] != sv[i] || sk[i] != (i < 2 ? k[i] : D / 32)) {
         fail_assert();
         return nullptr;
       }
-    if (!data_of(a[5], c.k_scales) || !data_of(a[6], c.v_scales) || !stride_at(sks.o, 0, c.scale_page_stride) || !stride_at(sks.o, 1, c.scale_tok_stride))
-      return nullptr;
+    if (!strides_of_both(a[5], a[6], 3, sk, stride) || !data_of(a[5], c.k_scales) || !data_of(a[6], c.v_scales)) return nullptr;
+    c.scale_page_stride = stride[0];
+    c.scale_tok_stride = stride[1];
   } else if (a[5] != Py_None || a[6] != Py_None) {
     fail_assert();
     return nullptr;
@@ -478,17 +491,13 @@ bool cache_of(PyObject* o, s2_paged_cache& c) {
   return true;
 }
 
-// two bf16 tensors of the same strides, of `n` sizes, the last of them features side by side; their sizes and the strides of the first two
+// two bf16 tensors of the same strides, of `n` sizes, the last of them features side by side; their sizes and strides
 bool pair_of(PyObject* a, PyObject* b, int n, int64_t* size, int64_t* stride) {
   int64_t other[4];
   if (!sizes_and_type(a, n, types.bf16, size) || !sizes_and_type(b, n, types.bf16, other)) return false;
   for (int i = 0; i < n; ++i)
     if (size[i] != other[i]) return fail_assert();
-  const Ref as(strides_of(a)), bs(as.o ? strides_of(b) : nullptr);
-  if (!bs.o || !same(as.o, bs.o) || !unit_stride(as.o, n - 1)) return false;
-  for (int i = 0; i < n - 1; ++i)
-    if (!stride_at(as.o, i, stride[i])) return false;
-  return true;
+  return strides_of_both(a, b, n, size, stride);
 }
 
 PyObject* kv_append(PyObject*, PyObject* const* a, Py_ssize_t n) {  // cache, k v cu_new start, max_new, rows, skipped, stream

@@ -89,3 +89,28 @@ def test_a_format_is_not_taken_modulo_anything(value):
     k, v, ks, vs = _pools(B.KV_MXFP8)
     with pytest.raises(OverflowError):
         B.paged_cache(value, 64, k, v, torch.zeros(2, 3, 7, dtype=torch.int32), ks, vs)
+
+
+def test_strides_of_a_single_one_are_any(seen):  # noqa: F811
+    """One sequence of many, one head, one node, one page: the stride of a size of 1 is nothing that has to agree."""
+    k, v, ks, vs = _pools(B.KV_MXFP8)
+    one = lambda x, s: x.as_strided((1,) + x.shape[1:], (s,) + x.stride()[1:])  # noqa: E731
+    table = torch.zeros(1, 3, 7, dtype=torch.int32)
+    cache = B.paged_cache(B.KV_MXFP8, 64, one(k, 7), one(v, 99999), table, one(ks, 3), one(vs, 64))
+    q, o = torch.zeros(5, 3, D, dtype=torch.bfloat16)[2:3], torch.empty_strided((1, 3, D), (1, D, 1), dtype=torch.bfloat16)
+    lens, ws, par, st = torch.zeros(1, dtype=torch.int32), torch.zeros(64, dtype=torch.uint8), B.layout_params(3, 1, 64, 2, 4), Stream()
+    B.s2_attn_decode_paged_cache(par, cache, q, lens, o, None, 0.5, ws, stream=st)
+    assert seen[0][1][1]["page_stride"] == seen[0][1][1]["scale_page_stride"] == seen[0][1][2]["q_stride_seq"] == 0
+    assert seen[0][1][1]["tok_stride"] == k.stride(1) and seen[0][1][2]["q_stride_head"] == D
+    t = torch.zeros(1, 3, 4, 1, D, dtype=torch.bfloat16)
+    q = t[:, :, 2]
+    o = torch.empty_strided((1, 3, 1, D), (5, q.stride(1), 3, 1), dtype=torch.bfloat16)
+    parents = torch.zeros(1, 1, dtype=torch.int32)
+    B.s2_attn_tree_paged(par, cache, q, q, o, parents, lens, o, None, 0.5, ws, stream=st)
+    assert seen[1][1][2]["q_stride_node"] == seen[1][1][2]["kv_stride_node"] == 0 and seen[1][1][2]["q_stride_head"] == q.stride(1)
+    new = torch.zeros(1, 3, D, dtype=torch.bfloat16)
+    B.s2_kv_append_paged(cache, new, torch.empty_strided((1, 3, D), (3, D, 1), dtype=torch.bfloat16), torch.zeros(2, dtype=torch.int32), lens, 1, stream=st)
+    assert seen[2][1][1]["stride_row"] == 0 and seen[2][1][1]["stride_head"] == D
+    with pytest.raises(AssertionError):  # (of the others they do)
+        B.s2_attn_decode_paged_cache(par, cache, torch.zeros(1, 3, D, dtype=torch.bfloat16), lens, torch.zeros(1, 3, D + 8, dtype=torch.bfloat16)[..., :D], None, 0.5,
+                                     ws, stream=st)
