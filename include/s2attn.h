@@ -459,8 +459,9 @@ int s2_layout_resident_blocks(const s2_layout* layout, int32_t head, int32_t len
  * even; features that are not all finite and below 2^127 are written as scale byte 255, codes 0.  The result depends on
  * a row's values alone.  An item is left out for a head whose table does not hold its block (an evicted one), and
  * for all heads where its position is not in [0, max_blocks*block_size) or its row not in [0, num_rows); nothing but the rows of
- * the items written is touched.  Two items that name one position of one page leave either, but items may take the same row.
- * max_new is a limit, not a size: sequences of any lengths take the time of their rows.  (num_rows, or with rows num_items, + 64 * nseq) * heads
+ * the items written is touched.  Where two items name one position of one page (one that two heads or sequences share), a mixture of both is left, which is
+ * either only if their rows are the same; items may take the same row.
+ * max_new is a limit, not a size: sequences of any lengths take about the time of their rows.  (num_rows, or with rows num_items, + 64 * nseq) * heads
  * below 2^28 is always taken; SHAPE where a launch would be larger than the chip allows.
  * Errors: NULL, BAD_PARAM (format), SHAPE, ALIGN, HIP. */
 int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void* stream);
