@@ -850,10 +850,12 @@ int most_cache_splits(int64_t pairs, int64_t max_len) {
 // tokens (e4m3, D = 128, us: 8 heads of 47 units in 4 splits 13.2, 8 10.0, 16 9.0; 32 in 4 13.6, 8 11.2, 16 11.5; of 19 units in 4 10.1, 8 8.7, 16 10.3;
 // 64 of 31 to 46 units in 2 20.0, 4 15.3, 8 15.7), and else four workgroups of four to a compute unit where that leaves 24 units to each (512
 // of up to 46 units in one split 62.6, in two 65.6).
-// Trees of up to 32 nodes: a workgroup to a compute unit, and three units to it (it takes two at a time; bf16, D = 128, us: 32 pairs of 47 units in 4
-// splits 19.8, 8 16.3, 12 19.0, 16 16.6; e4m3: 8 of 47 in 6 13.2, 16 11.0, 32 11.6; 256 of 46 in one 38.5, in two 41.6).
+// Trees of up to 32 nodes: a workgroup to a compute unit, and three units to it (it takes two at a time; bf16, D = 128, 8 nodes, us: 32 pairs of 47 units in 4
+// splits 19.7, 8 16.3, 12 18.7, 16 16.5; e4m3: 8 of 47 in 6 13.5, 16 11.1, 32 11.4; 16 nodes, 256 of 46 in one 39.6, in two 41.7).  From 129 to 255 pairs that is
+// one split, which long rows over 8 bits would rather have in more: in 1, 2 and 3, 8 nodes, 160 pairs of 46 units bf16 50, 54, 48, e4m3 36, 32, 29; of 21 units 27, 31, 27
+// and 19, 20, 20; 224 of 46 58, 59, 63 and 38, 37, 38.
 // Larger ones, whose workgroups take a unit at a time between two barriers: two to a compute unit, and two units to each (64 nodes, bf16: 32 pairs of
-// 47 units in 4 27.4, 8 21.1, 16 22.0, 24 24.3; 40 nodes, e2m1: 4 of 47 in 12 15.0, 24 12.8, 32 13.6; 33 nodes, D = 64: 91 of 9 in 2 17.9, 6 15.9, 8 17.4).
+// 47 units in 4 31.6, 8 23.1, 16 22.8, 24 26.2; 40 nodes, e2m1: 4 of 47 in 12 15.1, 24 12.6, 32 13.5; 33 nodes, D = 64: 91 of 9 in 2 19.7, 6 16.6, 8 17.9).
 int choose_cache_splits(const s2_layout_params* lp, const s2_layout* layout, int nodes, int nseq, int heads, int max_len) {
   const int S = lp->block_size;
   const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / S, nullptr, 0);

@@ -6,9 +6,9 @@
 // fragments without bank conflicts); then each takes one tile of queries against the whole unit.  The next unit's bytes are on their way while this one
 // is worked on; two barriers a unit, whose waits other workgroups of the compute unit fill.
 //
-// 64 nodes of 16 sequences over bf16 (32 heads of 31 to 46 blocks of 64 tokens, D = 128) take 130 us, 4.8 TB/s.  Over 4 bits it is the compute unit: a unit is 32 KB
-// of LDS writes and 128 KB of reads, 1250 of the 1950 cycles that it takes, beside 960 of vector and 768 of matrix instructions a SIMD; 64 nodes of 64 sequences 293 us,
-// of which the bytes are 115 (with bank conflicts in the writes 10 more).  Loads two units ahead: 1 % faster for 64 sequences over bf16, else up to 13 % slower.
+// 64 nodes of 16 sequences over bf16 (32 heads of 31 to 46 blocks of 64 tokens, D = 128) take 130 us, 4.8 TB/s.  Over 4 bits it is the compute unit: vector
+// instructions take 53 % of a SIMD's cycles, matrix instructions 32 %, the LDS is busy 35 % of the time (a unit is 32 KB of writes and 128 KB of reads), in one chain a
+// unit; 64 nodes of 64 sequences 293 us, of which the bytes are 115 (with bank conflicts in the writes 10 more).  Loads two units ahead: 1 % faster for 64 sequences over bf16, else up to 13 % slower.
 #include <hip/hip_runtime.h>
 
 #include "cache_attn.h"

@@ -6,8 +6,8 @@
 // Scaling by a power of two is exact: the one rounding is that of the conversion instruction, and what is read back is exact in bf16.
 //
 // Both move bytes and nothing else; D/8 lanes take a row, 16 bytes of bf16 each.  A whole cache read back moves 5.0 TB/s (32 heads of 32768 x 128 over
-// e4m3, 162 us; a large copy reaches 4.9), prompts written 4.6 (8 of 1001 to 16384 tokens over e4m3, of which the mask keeps a few blocks in a
-// hundred, 50 us); the tokens of a decode step are a launch, 4 us.
+// e4m3, 162 us; a kernel that only streams, a byte read to two written, reaches 6.3 at this size), prompts written 4.6 (8 of 1001 to 16384 tokens over e4m3, of
+// which the mask keeps a few blocks in a hundred, 50 us; such a kernel 5.7); the tokens of a decode step are a launch, 4 us.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
