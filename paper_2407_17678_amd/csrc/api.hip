@@ -911,7 +911,7 @@ int decode_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_p
   if (c->format == S2_KV_BF16) {
     if (c->block_size != lp->block_size) return S2_ERR_SHAPE;
     if ((int64_t)c->nseq * c->heads > std::numeric_limits<int32_t>::max() / 64) return S2_ERR_SHAPE;
-    const int64_t ss = a->q_stride_seq, sh = a->q_stride_head;
+    const int64_t ss = c->nseq == 1 ? 0 : a->q_stride_seq, sh = c->heads == 1 ? 0 : a->q_stride_head;  // (of one there is no next)
     if (ss < 0 || (ss & 7) != 0 || sh < 0 || (sh & 7) != 0 || (reinterpret_cast<uintptr_t>(a->lse) & 3u) != 0) return S2_ERR_ALIGN;
     if (ss > (int64_t)1 << 40 || sh > (int64_t)1 << 40) return S2_ERR_SHAPE;
     s2_paged_decode_args d{};

@@ -25,3 +25,8 @@ def test_strides_that_are_refused(bad, status):
 
 def test_more_pairs_than_there_are_numbers():
     assert _decode(_cache(B.KV_BF16, nseq=1 << 16, heads=1 << 12), params=dict(PARAMS, num_heads=1 << 12), ws_bytes=1 << 60) == SHAPE
+
+
+def test_the_stride_of_one_sequence_or_head_is_not_looked_at():
+    assert _decode(_cache(B.KV_BF16, nseq=1), q_stride_seq=5, ws_bytes=100) == WORKSPACE
+    assert _decode(_cache(B.KV_BF16, heads=1), params=dict(PARAMS, num_heads=1), q_stride_head=-3, ws_bytes=100) == WORKSPACE
