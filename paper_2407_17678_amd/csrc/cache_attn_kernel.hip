@@ -9,7 +9,7 @@
 // formed as keys x queries: K comes from memory straight into the layout of the first operand (16 rows, four lanes to a row: CacheRows), a
 // lane of the result holds one query, and the probabilities are the second operand of the product with V as they stand.  V needs its tokens along the
 // contraction: its rows go through a piece of LDS that is the wavefront's own, written as they come and read by the transpose read.  (With K and V
-// shared by a workgroup in LDS, as for more queries, 24 nodes of 64 sequences over e4m3 took 251 us instead of 242, 20 of 8 sequences 27.4 instead of 23.1.)
+// shared by a workgroup in LDS, as for more queries, 24 nodes of 64 sequences over e4m3 took 251 us instead of 242, 20 of 8 sequences 27.4 instead of 23.1, P in one term.)
 //
 // A tree's nodes lie in up to five block rows (64 nodes, blocks of 16).  The blocks that any of them keeps are walked once: row by row,
 // each block in the first row that keeps it, with one bit to a row that does.

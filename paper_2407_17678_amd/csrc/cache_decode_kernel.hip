@@ -7,7 +7,7 @@
 // is: a lane accumulates its quarter of the features over the rows of its own, and rows are added up once at the end.  Probabilities stay in 32 bits.
 //
 // 64 x 32 heads of 8192 to 32768 x 128: e4m3 213 us (5.5 TB/s), e2m1 in blocks of 16 73 us (5.0 TB/s); one sequence of 32768 over e4m3 11.8 us with
-// its merge.  The matrix kernel of cache_attn_kernel.hip with one of its 16 columns in use, where a unit is a chain of LDS round trips (1250 cycles for its
+// its merge.  As matrix products, as in cache_attn_kernel.hip, with one of 16 columns in use, where a unit is a chain of LDS round trips (1250 cycles for its
 // scores, 2850 for its sums): 217, 119 and 16.7 us.
 #include <hip/hip_runtime.h>
 
