@@ -228,6 +228,69 @@ typedef struct {
   int64_t kv_stride_seq, kv_stride_head, kv_stride_node; /* elements, multiples of 8          */
 } s2_tree_args;
 
+/* Attention of a chunk of new tokens to each sequence over a paged cache that holds their keys and values already.  Row r of head h of q and o at
+ * base + r*q_stride_row + h*q_stride_head + d. */
+typedef struct {
+  const void* q;          /* DEVICE bf16, may be NULL when num_rows is 0                      */
+  const int32_t* cu_new;  /* DEVICE int32 [nseq + 1], ascending: sequence b's new tokens are rows
+                             cu_new[b] .. cu_new[b+1]-1                                       */
+  const int32_t* start;   /* DEVICE int32 [nseq]: position of the sequence's first new token  */
+  void* o;                /* DEVICE bf16, out                                                 */
+  float* lse;             /* DEVICE fp32 [heads, num_rows], out (may be NULL)                 */
+  int32_t* missing;       /* as in s2_paged_decode_args; a block that several rows keep counts once */
+  int32_t num_rows;       /* rows of q and o                                                  */
+  int32_t max_new;        /* no sequence has more new tokens (>= 0; what is beyond is not looked at) */
+  int32_t num_splits;     /* KV splits per (sequence, head); 0 = library chooses              */
+  int64_t q_stride_row, q_stride_head; /* elements, multiples of 8                            */
+} s2_chunk_args;
+
+/* The block tables of a paged cache before a step, from the lengths of the requests.  Pages that no table holds lie in a ring
+ * of num_pages entries: free_state[0] is where the first of them lies, free_state[1] how many there are. */
+typedef struct {
+  const int32_t* block_table; /* DEVICE int32 [nseq, heads, max_blocks], in                   */
+  const int32_t* lens;        /* DEVICE int32 [nseq]: tokens in the cache                     */
+  const int32_t* new_lens;    /* DEVICE int32 [nseq]: tokens that the step adds; negative: the sequence is over */
+  const int32_t* query_from;  /* DEVICE int32 [nseq] or NULL (lens): no query at an earlier position will read the cache */
+  const int32_t* free_pages;  /* DEVICE int32 [num_pages], in                                 */
+  const int32_t* free_state;  /* DEVICE int32 [2], in                                         */
+  int32_t* new_table;         /* DEVICE, out: block_table itself, or apart from it            */
+  int32_t* new_free_pages;    /* DEVICE, out: free_pages itself, or apart from it             */
+  int32_t* new_free_state;    /* DEVICE, out: free_state itself, or apart from it             */
+  int32_t* cu_new;            /* DEVICE int32 [nseq + 1] or NULL, out: row offsets of the new tokens */
+  int32_t* positions;         /* DEVICE int32 [num_rows] or NULL, out: position of each new row */
+  int32_t* seq_lens;          /* DEVICE int32 [nseq] or NULL, out: tokens in the cache after the step; may be lens or new_lens */
+  int32_t* short_of;          /* DEVICE int32[1] or NULL: the call ADDS the number of blocks that it had no page for */
+  int32_t nseq, heads;
+  int32_t max_blocks;         /* row length of block_table                                    */
+  int32_t num_pages;          /* pages in each pool                                           */
+  int32_t num_rows;           /* entries of positions (without it not looked at)              */
+} s2_kv_plan_args;
+
+/* Queries and keys on their way from a projection to attention: element (b,h,t,d) of q and k at b*in_stride_b + h*in_stride_h +
+ * t*in_stride_t + d, of q_out and k_out at the out_* strides; gradients of either at the strides of what they are the gradient of. */
+typedef struct {
+  const void* q;           /* DEVICE bf16, in; NULL: keys only (then k is given)              */
+  const void* k;           /* DEVICE bf16, in; NULL: queries only                             */
+  void* q_out;             /* DEVICE bf16, fwd out; may be q itself, with its strides         */
+  void* k_out;             /* DEVICE bf16, fwd out                                            */
+  const float* q_weight;   /* DEVICE fp32 [head_dim], or NULL: q is rotated only              */
+  const float* k_weight;   /* DEVICE fp32 [head_dim], or NULL: k is rotated only              */
+  const float* inv_freq;   /* DEVICE fp32 [rotary_dim / 2]: angle of a pair for one position  */
+  const int32_t* positions;/* DEVICE int32 [batch, seqlen], or NULL: row t is at position t   */
+  const void* d_q_out;     /* DEVICE bf16, bwd in                                             */
+  const void* d_k_out;     /* DEVICE bf16, bwd in                                             */
+  void* dq;                /* DEVICE bf16, bwd out                                            */
+  void* dk;                /* DEVICE bf16, bwd out                                            */
+  float* dq_weight;        /* DEVICE fp32 [head_dim], bwd out; needed where q_weight is given */
+  float* dk_weight;        /* DEVICE fp32 [head_dim], bwd out                                 */
+  int32_t batch, heads, seqlen, head_dim; /* head_dim 64 or 128                               */
+  int32_t rotary_dim;      /* features that are rotated, the first ones: a multiple of 16, 0 .. head_dim */
+  int32_t interleaved;     /* pair i is features 2i and 2i + 1 (1), or i and i + rotary_dim/2 (0) */
+  float eps;               /* >= 0                                                            */
+  int64_t in_stride_b, in_stride_h, in_stride_t;    /* elements, multiples of 8               */
+  int64_t out_stride_b, out_stride_h, out_stride_t;
+} s2_qk_norm_rope_args;
+
 /* ---- layout (section 4.2 mask -> compressed lists, section 3.2) ------------------------- */
 
 /* Builds the per-head lists of kept KV blocks from the closed form of the mask, on the host,
@@ -497,6 +560,54 @@ int s2_attn_tree_paged(const s2_layout_params* p, const s2_paged_cache* c, const
 int s2_attn_tree_paged_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_tree_args* a, float scale,
                               void* workspace, size_t workspace_bytes, void* stream);
 size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, int32_t head_dim, int32_t max_len, int32_t num_splits);
+
+/* Attention of a chunk of new tokens over the cache: row i of sequence b is the token at position start[b] + i; its own key and value and those of
+ * the new tokens before it are in the cache (s2_kv_append_paged before this call).  It attends the cached tokens up to its own position that block
+ * row (start[b] + i) div S of the mask keeps: a chunk gives what as many decode steps give.  A row whose position is outside [0,
+ * max_blocks*block_size) gets o = 0 and lse = -inf, and so does one all of whose kept blocks are not resident; such blocks contribute nothing and are counted.
+ * Rows that belong to no sequence are left as they were.  What a row does not attend stays out of its result whatever it holds; of what it attends, a V that
+ * is NaN, or infinities of both signs, give NaN in their feature.  With max_new (or num_rows) up to 64 probabilities go to V in 16 bits, as
+ * in a decode step, else rounded to bf16, as in s2_attn_fwd.  max_new is a limit, not a size.
+ * q and o may be the same tensor.
+ * workspace: s2_attn_chunk_workspace_bytes(..., max_blocks * block_size, num_splits) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit
+ * (with num_splits = 0 less will do, down to none at all for one split, with which nothing goes there: the call then takes fewer splits).  With a layout, it covers the cache.
+ * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
+int s2_attn_chunk_paged(const s2_layout_params* p, const s2_paged_cache* c, const s2_chunk_args* a, float scale,
+                        void* workspace, size_t workspace_bytes, void* stream);
+int s2_attn_chunk_paged_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_chunk_args* a, float scale,
+                               void* workspace, size_t workspace_bytes, void* stream);
+size_t s2_attn_chunk_workspace_bytes(int32_t nseq, int32_t heads, int32_t max_new, int32_t num_rows, int32_t head_dim, int32_t max_len, int32_t num_splits);
+
+/* The block tables for a step that adds new_lens[b] tokens to the lens[b] that sequence b has in the cache.  Afterwards a (sequence, head) holds, of
+ * the blocks with a token below lens + new_lens, those that some query at a position >= query_from can attend (the rule of s2_kv_resident_blocks with
+ * length query_from + 1: row query_from div S keeps the block, or the block is that row's or a later one), and no other: pages that it held of
+ * others go to the end of the ring of free pages, in ascending order of (sequence, head, block), and blocks that begin at or beyond lens
+ * and are not held take pages from its beginning, in the same order.  Pages that this call gives up are not taken before the next one, so that what runs
+ * beside it may still read them.  A block that there is no page for, and one that begins before lens and is not held, are not held (-1) or left as they are.  An entry that is negative or
+ * num_pages or more is not held; new entries that are not held and not to be held are -1.  A page is held by one entry at most.
+ * With new_lens < 0 nothing is held and the sequence counts as 0 new tokens and 0 tokens.  lens, new_lens and query_from are cut to what the table has room for;
+ * cu_new counts all of new_lens, positions are lens[b] + i for all of them, and entries of positions beyond the last row are left as they were.
+ * p->num_heads is heads, p->num_blocks is ignored; with a layout, it covers the cache.
+ * workspace: s2_kv_plan_workspace_bytes(nseq, heads) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit.
+ * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */
+int s2_kv_plan_paged(const s2_layout_params* p, const s2_kv_plan_args* a, void* workspace, size_t workspace_bytes, void* stream);
+int s2_kv_plan_paged_layout(const s2_layout* layout, const s2_kv_plan_args* a, void* workspace, size_t workspace_bytes, void* stream);
+size_t s2_kv_plan_workspace_bytes(int32_t nseq, int32_t heads);
+
+/* ---- queries and keys before attention: norm of each head's rows, rotation by position ------- */
+
+/* y = w * x / sqrt(mean(x^2) + eps) over the head_dim features of a row (with a weight; else y = x), then each pair of the first rotary_dim features turned by
+ * the angle position * inv_freq[pair]: (a, b) -> (a cos - b sin, b cos + a sin); from the strides of a projection to those of the attention calls (a packed batch,
+ * and the rows of s2_kv_append_paged and s2_attn_chunk_paged, are batch = 1).  All in 32 bits, angles in 64, one rounding to bf16.
+ * Outputs may be the inputs themselves, with the same strides.  Errors: NULL, BAD_PARAM (eps, interleaved), SHAPE, ALIGN, HIP. */
+int s2_qk_norm_rope_fwd(const s2_qk_norm_rope_args* a, void* stream);
+
+/* Its gradient: from q, k (as they went in) and d_q_out, d_k_out to dq, dk (bf16) and, where there is a weight, dq_weight, dk_weight (fp32, summed over
+ * batch, heads and rows in an order that the sizes alone decide).  dq may be q or d_q_out itself, with the same strides, and dk likewise.
+ * workspace: s2_qk_norm_rope_bwd_workspace_bytes(...) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit; none is needed without weights.
+ * Errors as above plus WORKSPACE. */
+int s2_qk_norm_rope_bwd(const s2_qk_norm_rope_args* a, void* workspace, size_t workspace_bytes, void* stream);
+size_t s2_qk_norm_rope_bwd_workspace_bytes(int32_t batch, int32_t heads, int32_t seqlen, int32_t head_dim);
 
 /* ---- ceiling probes (measurement only) ------------------------------------------------------ */
 

@@ -617,3 +617,98 @@ def tree_attention(q, k_cache, v_cache, k_draft, v_draft, parents, length, keeps
         v = np.concatenate([_f64(v_cache)[cached], _f64(v_draft)[nodes]])
         o[i], lse[i], weight[i] = attend(q[i], k, v, scale)
     return o, lse, weight
+
+
+# ---------------------------------------------------------------------------------------------
+# A step of serving around attention: block tables, queries and keys, a chunk of new tokens (sections 4.1 and 5.3)
+# ---------------------------------------------------------------------------------------------
+def chunk_attention(q, k_cache, v_cache, start, keeps, block_size, scale, max_len, resident=None):
+    """One head's chunk: q [T, D], row i the token at position start + i; k_cache, v_cache [>= start + T, D] hold the new tokens too.
+
+    keeps(row, col): whether block row `row` of the mask keeps block `col`.  Row i attends the cached tokens up to its own
+    position whose block its row keeps: by definition what a decode step at that position gives.  resident(col): whether
+    the cache holds the block.  Returns (o [T, D], lse [T], sum_j p_j |v_j| [T, D]), zeros and -inf for a row outside [0, max_len).
+    """
+    T, D = q.shape
+    o, lse, weight = np.zeros((T, D)), np.full(T, -np.inf), np.zeros((T, D))
+    for i in range(T):
+        at = start + i
+        if not 0 <= at < max_len:
+            continue
+        seen = [t for t in range(at + 1) if keeps(at // block_size, t // block_size) and (resident is None or resident(t // block_size))]
+        o[i], lse[i], weight[i] = attend(q[i], k_cache[seen], v_cache[seen], scale)
+    return o, lse, weight
+
+
+def plan_tables(table, lens, new_lens, free_pages, free_state, attended, block_size, query_from=None):
+    """Block tables for a step, an entry at a time, as a cache manager on the host would keep them.
+
+    table [nseq, heads, max_blocks]; attended(h, row, j): whether a query in block row `row` or a later one attends block j;
+    free_pages is a ring of which free_state = (first, count) names the free ones.  Returns a dict of what s2_kv_plan_paged writes
+    (positions of the new rows as a list, and of those before them; `short`: blocks without a page).
+    """
+    table, ring = np.array(table, copy=True), np.array(free_pages, copy=True)
+    old, P = np.array(free_pages), len(free_pages)
+    n, H, MB = table.shape
+    cap = MB * block_size
+    first = free_state[0] if 0 <= free_state[0] < P else 0
+    count = min(max(int(free_state[1]), 0), P)
+    taken, given, short = 0, 0, 0
+    cu, positions, seq_lens = [0], [], []
+    for b in range(n):
+        L = min(max(int(lens[b]), 0), cap)
+        over = new_lens[b] < 0
+        end = 0 if over else min(L + int(new_lens[b]), cap)
+        row = min(max(int(lens[b] if query_from is None else query_from[b]), 0), cap - 1) // block_size
+        for h in range(H):
+            for j in range(MB):
+                page = table[b, h, j]
+                held = 0 <= page < P
+                needed = j * block_size < end and attended(h, row, j)
+                if not needed:
+                    if held and given < P - count:
+                        ring[(first + count + given) % P] = page
+                        given += 1
+                    table[b, h, j] = -1
+                elif not held and j * block_size >= L:
+                    if taken < count:
+                        table[b, h, j] = old[(first + taken) % P]
+                        taken += 1
+                    else:
+                        table[b, h, j] = -1
+                        short += 1
+        positions += [L + i for i in range(max(int(new_lens[b]), 0))]
+        cu.append(len(positions))
+        seq_lens.append(end)
+    return dict(table=table, ring=ring, state=[(first + taken) % P, count - taken + given], cu_new=cu, positions=positions, seq_lens=seq_lens, short=short)
+
+
+def rotate_pairs(x, positions, inv_freq, interleaved, back=False):
+    """Turns the first 2 len(inv_freq) features of rows x [..., T, D] pair by pair: pair i by positions[t] * inv_freq[i] (back: the other way)."""
+    x = np.array(_f64(x), copy=True)
+    n = len(inv_freq)
+    angle = np.asarray(positions, dtype=np.float64)[..., None] * _f64(inv_freq)
+    turn = np.exp((-1j if back else 1j) * angle)
+    a, b = (slice(0, 2 * n, 2), slice(1, 2 * n, 2)) if interleaved else (slice(0, n), slice(n, 2 * n))
+    z = (x[..., a] + 1j * x[..., b]) * turn
+    x[..., a], x[..., b] = z.real, z.imag
+    return x
+
+
+def qk_norm_rope(x, weight, positions, inv_freq, eps, interleaved=False):
+    """Rows x [batch, heads, T, D] normalised (weight [D], or None: not) and rotated; positions [batch, T]."""
+    x = _f64(x)
+    if weight is not None:
+        x = _f64(weight) * x / np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    return rotate_pairs(x, np.asarray(positions)[:, None], inv_freq, interleaved)
+
+
+def qk_norm_rope_backward(x, weight, positions, inv_freq, eps, g, interleaved=False):
+    """Gradient of sum(g * qk_norm_rope(x)): (dx, dweight or None)."""
+    x, g = _f64(x), rotate_pairs(g, np.asarray(positions)[:, None], inv_freq, interleaved, back=True)
+    if weight is None:
+        return g, None
+    size = np.sqrt((x * x).mean(-1, keepdims=True) + eps)
+    unit = x / size
+    gw = g * _f64(weight)
+    return (gw - unit * (gw * unit).mean(-1, keepdims=True)) / size, (g * unit).sum((0, 1, 2))

@@ -113,6 +113,24 @@ class TreeArgs(C.Structure):
                 ("kv_stride_seq", C.c_int64), ("kv_stride_head", C.c_int64), ("kv_stride_node", C.c_int64)]
 
 
+class ChunkArgs(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("cu_new", C.c_void_p), ("start", C.c_void_p), ("o", C.c_void_p), ("lse", C.c_void_p), ("missing", C.c_void_p),
+                ("num_rows", C.c_int32), ("max_new", C.c_int32), ("num_splits", C.c_int32), ("q_stride_row", C.c_int64), ("q_stride_head", C.c_int64)]
+
+
+class KvPlanArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("block_table", "lens", "new_lens", "query_from", "free_pages", "free_state", "new_table", "new_free_pages",
+                                          "new_free_state", "cu_new", "positions", "seq_lens", "short_of")] + \
+               [(n, C.c_int32) for n in ("nseq", "heads", "max_blocks", "num_pages", "num_rows")]
+
+
+class QkNormRopeArgs(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out", "q_weight", "k_weight", "inv_freq", "positions", "d_q_out", "d_k_out", "dq", "dk",
+                                          "dq_weight", "dk_weight")] + \
+               [(n, C.c_int32) for n in ("batch", "heads", "seqlen", "head_dim", "rotary_dim", "interleaved")] + [("eps", C.c_float)] + \
+               [(n, C.c_int64) for n in ("in_stride_b", "in_stride_h", "in_stride_t", "out_stride_b", "out_stride_h", "out_stride_t")]
+
+
 EXPORTS = (
     "s2_layout_build", "s2_layout_from_csr", "s2_layout_destroy", "s2_layout_get", "s2_layout_get_tiles", "s2_layout_get_ds_units", "s2_attn_fwd", "s2_attn_fwd_rows", "s2_attn_fwd_varlen", "s2_attn_bwd_varlen",
     "s2_attn_bwd_varlen_workspace_bytes", "s2_attn_bwd",
@@ -121,6 +139,8 @@ EXPORTS = (
     "s2_kv_resident_blocks", "s2_attn_decode_layout", "s2_attn_decode_paged_layout",
     "s2_kv_append_paged", "s2_kv_read_paged", "s2_attn_decode_paged_cache", "s2_attn_decode_paged_cache_layout", "s2_attn_tree_paged",
     "s2_attn_tree_paged_layout", "s2_attn_tree_workspace_bytes",
+    "s2_attn_chunk_paged", "s2_attn_chunk_paged_layout", "s2_attn_chunk_workspace_bytes", "s2_kv_plan_paged", "s2_kv_plan_paged_layout",
+    "s2_kv_plan_workspace_bytes", "s2_qk_norm_rope_fwd", "s2_qk_norm_rope_bwd", "s2_qk_norm_rope_bwd_workspace_bytes",
     "s2_layout_resident_blocks", "s2_probe_scratch_bytes", "s2_probe_mfma", "s2_probe_read", "s2_probe_atomic_add", "s2_status_string",
     "s2_last_hip_error", "s2_version",
 )
@@ -132,6 +152,8 @@ _MARSHALLED = ("s2_attn_fwd", "s2_attn_fwd_rows", "s2_attn_fwd_varlen", "s2_attn
 # the same for those over a cache of any format (bind_cache())
 _CACHE_CALLS = ("s2_kv_append_paged", "s2_kv_read_paged", "s2_attn_decode_paged_cache", "s2_attn_decode_paged_cache_layout", "s2_attn_tree_paged",
                 "s2_attn_tree_paged_layout")
+# the same for what surrounds attention in a step (bind_step())
+_STEP_CALLS = ("s2_attn_chunk_paged", "s2_attn_chunk_paged_layout", "s2_kv_plan_paged", "s2_kv_plan_paged_layout", "s2_qk_norm_rope_fwd", "s2_qk_norm_rope_bwd")
 
 _lib = None
 _calls = None
@@ -146,10 +168,12 @@ def _marshal():
             from . import _marshal as calls
         except ImportError as e:
             raise ImportError("_marshal.so is not built: run `python -m paper_2407_17678_amd.build`") from e
-        if getattr(calls, "entry_points", None) != _MARSHALLED or getattr(calls, "cache_entry_points", None) != _CACHE_CALLS:
+        if (getattr(calls, "entry_points", None), getattr(calls, "cache_entry_points", None), getattr(calls, "step_entry_points", None)) != (
+                _MARSHALLED, _CACHE_CALLS, _STEP_CALLS):
             raise ImportError("_marshal.so is built from other sources: run `python -m paper_2407_17678_amd.build`")
         calls.bind(*(C.cast(getattr(L, name), C.c_void_p).value for name in _MARSHALLED))
         calls.bind_cache(*(C.cast(getattr(L, name), C.c_void_p).value for name in _CACHE_CALLS))
+        calls.bind_step(*(C.cast(getattr(L, name), C.c_void_p).value for name in _STEP_CALLS))
         _calls = calls
     return _calls
 
@@ -210,6 +234,17 @@ def lib():
     for pattern, suffix in ((C.POINTER(LayoutParams), ""), (C.c_void_p, "_layout")):
         for name, args in (("s2_attn_decode_paged_cache", CacheDecodeArgs), ("s2_attn_tree_paged", TreeArgs)):
             getattr(L, name + suffix).argtypes = [pattern, C.POINTER(PagedCacheStruct), C.POINTER(args), C.c_float, C.c_void_p, C.c_size_t, C.c_void_p]
+        getattr(L, "s2_attn_chunk_paged" + suffix).argtypes = [pattern, C.POINTER(PagedCacheStruct), C.POINTER(ChunkArgs), C.c_float, C.c_void_p, C.c_size_t,
+                                                               C.c_void_p]
+        getattr(L, "s2_kv_plan_paged" + suffix).argtypes = [pattern, C.POINTER(KvPlanArgs), C.c_void_p, C.c_size_t, C.c_void_p]
+    L.s2_attn_chunk_workspace_bytes.argtypes = [C.c_int32] * 7
+    L.s2_attn_chunk_workspace_bytes.restype = C.c_size_t
+    L.s2_kv_plan_workspace_bytes.argtypes = [C.c_int32] * 2
+    L.s2_kv_plan_workspace_bytes.restype = C.c_size_t
+    L.s2_qk_norm_rope_fwd.argtypes = [C.POINTER(QkNormRopeArgs), C.c_void_p]
+    L.s2_qk_norm_rope_bwd.argtypes = [C.POINTER(QkNormRopeArgs), C.c_void_p, C.c_size_t, C.c_void_p]
+    L.s2_qk_norm_rope_bwd_workspace_bytes.argtypes = [C.c_int32] * 4
+    L.s2_qk_norm_rope_bwd_workspace_bytes.restype = C.c_size_t
     L.s2_attn_tree_workspace_bytes.argtypes = [C.c_int32] * 6
     L.s2_attn_tree_workspace_bytes.restype = C.c_size_t
     L.s2_probe_scratch_bytes.restype = C.c_size_t
@@ -521,6 +556,58 @@ def s2_attn_tree_paged_layout(layout, cache, q, k_draft, v_draft, parents, seq_l
     """s2_attn_tree_paged following the rows of a Layout (any pattern) instead of the closed form."""
     _check(_marshal().tree_layout(layout.handle, cache.raw, q, k_draft, v_draft, parents, seq_lens, o, lse, scale, workspace, missing, num_splits,
                                   _stream(stream)), "s2_attn_tree_paged_layout")
+
+
+def s2_attn_chunk_workspace_bytes(nseq, heads, max_new, num_rows, head_dim, max_len, num_splits=0):
+    return lib().s2_attn_chunk_workspace_bytes(nseq, heads, max_new, num_rows, head_dim, max_len, num_splits)
+
+
+def s2_attn_chunk_paged(params, cache, q, cu_new, start, o, lse, scale, workspace, max_new, missing=None, num_splits=0, stream=None):
+    """q, o: bf16 [rows, heads, D] of the same strides; cu_new: device int32 [nseq + 1]; start: [nseq]; lse: [heads, rows] or None; workspace: None for one split."""
+    _check(_marshal().chunk(_params_ptr(params), cache.raw, q, cu_new, start, o, lse, scale, workspace, max_new, missing, num_splits, _stream(stream)),
+           "s2_attn_chunk_paged")
+
+
+def s2_attn_chunk_paged_layout(layout, cache, q, cu_new, start, o, lse, scale, workspace, max_new, missing=None, num_splits=0, stream=None):
+    """s2_attn_chunk_paged following the rows of a Layout (any pattern) instead of the closed form."""
+    _check(_marshal().chunk_layout(layout.handle, cache.raw, q, cu_new, start, o, lse, scale, workspace, max_new, missing, num_splits, _stream(stream)),
+           "s2_attn_chunk_paged_layout")
+
+
+def s2_kv_plan_workspace_bytes(nseq, heads):
+    return lib().s2_kv_plan_workspace_bytes(nseq, heads)
+
+
+def s2_kv_plan_paged(params, block_table, lens, new_lens, free_pages, free_state, new_table, new_free_pages, new_free_state, workspace, cu_new=None,
+                     positions=None, seq_lens=None, query_from=None, short=None, stream=None):
+    """All int32 on the device: tables [nseq, heads, max_blocks]; lens, new_lens, seq_lens, query_from [nseq]; free_pages [num_pages]; free_state [2] (where the first
+    free page lies, how many there are); cu_new [nseq + 1]; positions [rows]; short [1].  The new ones may be the old ones (in place)."""
+    _check(_marshal().plan(_params_ptr(params), block_table, lens, new_lens, free_pages, free_state, new_table, new_free_pages, new_free_state, workspace,
+                           cu_new, positions, seq_lens, query_from, short, _stream(stream)), "s2_kv_plan_paged")
+
+
+def s2_kv_plan_paged_layout(layout, block_table, lens, new_lens, free_pages, free_state, new_table, new_free_pages, new_free_state, workspace, cu_new=None,
+                            positions=None, seq_lens=None, query_from=None, short=None, stream=None):
+    """s2_kv_plan_paged following the rows of a Layout (any pattern) instead of the closed form."""
+    _check(_marshal().plan_layout(layout.handle, block_table, lens, new_lens, free_pages, free_state, new_table, new_free_pages, new_free_state, workspace,
+                                  cu_new, positions, seq_lens, query_from, short, _stream(stream)), "s2_kv_plan_paged_layout")
+
+
+def s2_qk_norm_rope_fwd(q, k, q_out, k_out, q_weight, k_weight, inv_freq, eps, positions=None, interleaved=False, stream=None):
+    """q, k and q_out, k_out: bf16 [batch, heads, seqlen, D], each two of the same strides (q_out may be q); weights: float32 [D], None: rotated only; inv_freq:
+    float32 [rotary_dim / 2] (None: no rotation); positions: int32 [batch, seqlen], None: row t is at t.  q (and q_out) or k (and k_out) may be None."""
+    _check(_marshal().rope_fwd(q, k, q_out, k_out, q_weight, k_weight, inv_freq, eps, positions, interleaved, _stream(stream)), "s2_qk_norm_rope_fwd")
+
+
+def s2_qk_norm_rope_bwd_workspace_bytes(batch, heads, seqlen, head_dim):
+    return lib().s2_qk_norm_rope_bwd_workspace_bytes(batch, heads, seqlen, head_dim)
+
+
+def s2_qk_norm_rope_bwd(q, k, d_q_out, d_k_out, dq, dk, q_weight, k_weight, dq_weight, dk_weight, inv_freq, eps, workspace, positions=None, interleaved=False,
+                        stream=None):
+    """Gradient of s2_qk_norm_rope_fwd (q, k as they went in); dq, dk: strides of q, k; dq_weight, dk_weight: float32 [D], written (None without that weight)."""
+    _check(_marshal().rope_bwd(q, k, d_q_out, d_k_out, dq, dk, q_weight, k_weight, dq_weight, dk_weight, inv_freq, eps, workspace, positions, interleaved,
+                               _stream(stream)), "s2_qk_norm_rope_bwd")
 
 
 def s2_kv_resident_blocks(params, head, length):

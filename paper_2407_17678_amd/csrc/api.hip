@@ -48,9 +48,10 @@ void free_device_copies(s2_layout* L) {
   free_tiles(L->kv_tiles);
   if (L->d_row_ptr) (void)hipFree(L->d_row_ptr);
   if (L->d_col_idx) (void)hipFree(L->d_col_idx);
+  if (L->d_last_row) (void)hipFree(L->d_last_row);
   if (L->d_dq_units) (void)hipFree(L->d_dq_units);
   if (L->d_kv_split_codes) (void)hipFree(L->d_kv_split_codes);
-  L->d_row_ptr = L->d_col_idx = L->d_dq_units = L->d_kv_split_codes = nullptr;
+  L->d_row_ptr = L->d_col_idx = L->d_last_row = L->d_dq_units = L->d_kv_split_codes = nullptr;
 }
 
 s2::DevTiles dev_tiles(const s2::TileList& t) {
@@ -179,8 +180,11 @@ namespace {
 // Tile lists for the three passes, then the device copy when a GPU is visible.  Takes ownership
 // of L: on failure it is deleted.
 int finish_layout(s2_layout* L, int st, s2_layout** out) {
+  std::vector<int32_t> last_row;
   if (st == S2_OK) {
     try {
+      last_row.resize(L->col_ptr.size() - 1);
+      for (size_t j = 0; j < last_row.size(); ++j) last_row[j] = L->col_ptr[j + 1] > L->col_ptr[j] ? L->row_idx[(size_t)L->col_ptr[j + 1] - 1] : -1;
       const int S = L->p.block_size;
       static_assert(s2::kFwdBM == s2::kBwdBM, "forward and dQ walk the same lists");
       s2::build_tiles(*L, s2::kBwdBM / S, false, L->q_tiles);
@@ -199,7 +203,7 @@ int finish_layout(s2_layout* L, int st, s2_layout** out) {
   if (hipGetDeviceCount(&ndev) == hipSuccess && ndev > 0) {
     int dev = 0;
     bool ok = hip_ok(hipGetDevice(&dev)) && upload_tiles(L->q_tiles) && upload_tiles(L->kv_tiles) && upload(L->row_ptr, &L->d_row_ptr) &&
-              upload(L->col_idx, &L->d_col_idx) && upload(L->dq_units, &L->d_dq_units) &&
+              upload(L->col_idx, &L->d_col_idx) && upload(last_row, &L->d_last_row) && upload(L->dq_units, &L->d_dq_units) &&
               upload(L->kv_split_codes, &L->d_kv_split_codes);
     if (!ok) {
       free_device_copies(L);
@@ -673,6 +677,21 @@ void set_pattern(PARAMS& p, const s2_layout_params* lp, const s2_layout* layout)
   }
 }
 
+// Where the arrays of a plan lie in its workspace: the new tokens of 256 sequences each come first.
+struct PlanWorkspace {
+  size_t seq, pair, group, state, bytes;
+};
+PlanWorkspace plan_workspace(const s2::KvPlanParams& p) {
+  PlanWorkspace w;
+  auto after = [](size_t at, size_t bytes) { return (at + bytes + 255) / 256 * 256; };
+  w.seq = after(0, ((size_t)p.nseq + 255) / 256 * sizeof(int64_t));
+  w.pair = after(w.seq, (size_t)p.nseq * 4 * sizeof(int32_t));
+  w.group = after(w.pair, (size_t)p.pairs * 2 * sizeof(int32_t));
+  w.state = after(w.group, (size_t)p.groups * 2 * sizeof(int32_t));
+  w.bytes = after(w.state, 2 * sizeof(int32_t));
+  return w;
+}
+
 int decode_contiguous(const s2_layout_params* lp, const s2_layout* layout, const s2_decode_args* a, float scale,
                       void* workspace, size_t workspace_bytes, void* stream) {
   if (!a->q || !a->k_cache || !a->v_cache || !a->seq_lens || !a->o) return S2_ERR_NULL;
@@ -976,7 +995,254 @@ int tree_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_pag
   return attend_cache(lp, layout, c, p, scale, a->num_splits, workspace, workspace_bytes, stream);
 }
 
+// The most splits that the library takes for a chunk: two workgroups to a compute unit, two units of 64 tokens to each.
+int most_chunk_splits(int64_t groups, int64_t max_len) {
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, (512 + groups - 1) / groups, (max_len + 127) / 128}));
+}
+
+// (the fields that decide the launch's size)
+s2::CacheChunkParams chunk_sizes(int nseq, int heads, int max_new, int num_rows) {
+  s2::CacheChunkParams p{};
+  p.nseq = nseq;
+  p.heads = heads;
+  p.num_rows = num_rows;
+  p.max_new = std::min(max_new, num_rows);
+  return p;
+}
+
+int chunk_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_paged_cache* c, const s2_chunk_args* a, float scale, void* workspace,
+                size_t workspace_bytes, void* stream) {
+  if (!a->cu_new || !a->start) return S2_ERR_NULL;
+  if (!(scale > 0.f) || !std::isfinite(scale)) return S2_ERR_BAD_PARAM;
+  s2::CacheRef cache;
+  int st = check_cache(c, cache);
+  if (st != S2_OK) return st;
+  if (lp->block_size != c->block_size) return S2_ERR_SHAPE;
+  const int max_len = c->max_blocks * c->block_size;
+  st = check_pattern(lp, layout, c->heads, max_len);
+  if (st != S2_OK) return st;
+  if (a->num_splits < 0 || a->num_splits > 64) return S2_ERR_BAD_PARAM;
+  if (a->num_rows < 0 || a->max_new < 0) return S2_ERR_SHAPE;
+  if (a->num_rows > 0 && (!a->q || !a->o)) return S2_ERR_NULL;
+  for (int64_t s : {a->q_stride_row, a->q_stride_head}) {
+    if (s < 0 || (s & 7) != 0) return S2_ERR_ALIGN;
+    if (s > (int64_t)1 << 40) return S2_ERR_SHAPE;
+  }
+  if (!aligned16(a->q) || !aligned16(a->o)) return S2_ERR_ALIGN;
+  for (const void* x : {(const void*)a->cu_new, (const void*)a->start, (const void*)a->lse, (const void*)a->missing})
+    if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return S2_ERR_ALIGN;
+  s2::CacheChunkParams p = chunk_sizes(c->nseq, c->heads, a->max_new, a->num_rows);
+  if (p.max_new == 0) return S2_OK;
+  const int64_t groups = s2::chunk_tiles(p) * c->heads;
+  if (groups > s2::kMostGroups) return S2_ERR_SHAPE;
+  const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / c->block_size, nullptr, 0);
+  const int64_t units = (blocks * c->block_size + 63) / 64;
+  int splits = a->num_splits > 0 ? a->num_splits : (int)std::max<int64_t>(1, std::min<int64_t>(most_chunk_splits(groups, max_len), units / 2));
+  auto bytes = [&](int n) { return n == 1 ? 0 : s2_attn_chunk_workspace_bytes(c->nseq, c->heads, a->max_new, a->num_rows, c->head_dim, max_len, n); };
+  // (a smaller workspace is for fewer splits, where the caller has not asked for a number)
+  while (a->num_splits == 0 && splits > 1 && (!workspace || bytes(splits) > workspace_bytes)) --splits;
+  if (splits > 1 && (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < bytes(splits))) return S2_ERR_WORKSPACE;
+  const int64_t rows = (int64_t)c->nseq * c->heads * p.max_new;
+  if (groups * splits > s2::kMostGroups || (splits > 1 && (rows + 3) / 4 > s2::kMostGroups)) return S2_ERR_SHAPE;
+  p.c = cache;
+  p.q = static_cast<const uint16_t*>(a->q);
+  p.cu = a->cu_new;
+  p.start = a->start;
+  p.o = static_cast<uint16_t*>(a->o);
+  p.lse = a->lse;
+  p.missing = a->missing;
+  p.part_acc = static_cast<float*>(workspace);
+  p.part_ml = splits > 1 ? p.part_acc + (size_t)rows * splits * c->head_dim : nullptr;
+  p.max_len = max_len;
+  p.num_splits = splits;
+  p.q_sr = a->q_stride_row;
+  p.q_sh = a->q_stride_head;
+  p.scale = scale;
+  p.scale_log2e = scale * 1.4426950408889634f;
+  set_pattern(p, lp, layout);
+  return hip_ok(s2::launch_cache_chunk(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+int kv_plan(const s2_layout_params* lp, const s2_layout* layout, const s2_kv_plan_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!a->block_table || !a->lens || !a->new_lens || !a->free_pages || !a->free_state || !a->new_table || !a->new_free_pages || !a->new_free_state)
+    return S2_ERR_NULL;
+  if (!good_block_size(lp->block_size)) return S2_ERR_BAD_PARAM;
+  if (a->nseq < 1 || a->heads < 1 || a->max_blocks < 1 || a->num_pages < 1) return S2_ERR_SHAPE;
+  if (a->positions && a->num_rows < 0) return S2_ERR_SHAPE;
+  const int64_t pairs = (int64_t)a->nseq * a->heads, max_len = (int64_t)a->max_blocks * lp->block_size;
+  if (pairs > std::numeric_limits<int32_t>::max() / 64 || max_len > std::numeric_limits<int32_t>::max() - 64) return S2_ERR_SHAPE;
+  const int st = check_pattern(lp, layout, a->heads, max_len);
+  if (st != S2_OK) return st;
+  for (const void* x : {(const void*)a->block_table, (const void*)a->lens, (const void*)a->new_lens, (const void*)a->query_from, (const void*)a->free_pages,
+                        (const void*)a->free_state, (const void*)a->new_table, (const void*)a->new_free_pages, (const void*)a->new_free_state,
+                        (const void*)a->cu_new, (const void*)a->positions, (const void*)a->seq_lens, (const void*)a->short_of})
+    if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return S2_ERR_ALIGN;
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 || workspace_bytes < s2_kv_plan_workspace_bytes(a->nseq, a->heads))
+    return S2_ERR_WORKSPACE;
+  s2::KvPlanParams p{};
+  p.table = a->block_table;
+  p.lens = a->lens;
+  p.new_lens = a->new_lens;
+  p.query_from = a->query_from;
+  p.ring = a->free_pages;
+  p.free_state = a->free_state;
+  p.new_table = a->new_table;
+  p.new_ring = a->new_free_pages;
+  p.new_state = a->new_free_state;
+  p.cu_new = a->cu_new;
+  p.positions = a->positions;
+  p.seq_lens = a->seq_lens;
+  p.short_of = a->short_of;
+  p.pairs = pairs;
+  p.nseq = a->nseq;
+  p.heads = a->heads;
+  p.max_blocks = a->max_blocks;
+  p.max_len = (int)max_len;
+  p.num_pages = a->num_pages;
+  p.num_rows = a->num_rows;
+  p.block_shift = 31 - __builtin_clz((unsigned)lp->block_size);
+  p.apart = a->new_table != a->block_table;
+  set_pattern(p, lp, layout);
+  if (layout) p.last_row = layout->d_last_row;
+  s2::plan_groups(p);
+  if (p.groups + (int64_t)a->nseq + a->num_pages / s2::kRingEach + 1 > s2::kMostGroups) return S2_ERR_SHAPE;
+  const PlanWorkspace w = plan_workspace(p);
+  char* const at = static_cast<char*>(workspace);
+  p.ws_fresh = reinterpret_cast<int64_t*>(at);
+  p.ws_seq = reinterpret_cast<int32_t*>(at + w.seq);
+  p.ws_pair = reinterpret_cast<int32_t*>(at + w.pair);
+  p.ws_group = reinterpret_cast<int32_t*>(at + w.group);
+  p.ws_state = reinterpret_cast<int32_t*>(at + w.state);
+  return hip_ok(s2::launch_kv_plan(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+// What s2_qk_norm_rope_fwd and _bwd have in common.
+int qk_rope(const s2_qk_norm_rope_args* a, bool bwd, s2::QkRopeParams& p) {
+  if (!a->q && !a->k) return S2_ERR_NULL;
+  const void* const x[2] = {a->q, a->k};
+  void* const out[2] = {bwd ? a->dq : a->q_out, bwd ? a->dk : a->k_out};
+  const void* const g[2] = {a->d_q_out, a->d_k_out};
+  const float* const weight[2] = {a->q_weight, a->k_weight};
+  float* const d_weight[2] = {a->dq_weight, a->dk_weight};
+  for (int i = 0; i < 2; ++i)
+    if (x[i] && (!out[i] || (bwd && (!g[i] || (weight[i] && !d_weight[i]))))) return S2_ERR_NULL;
+  if (a->rotary_dim > 0 && !a->inv_freq) return S2_ERR_NULL;
+  if (!(a->eps >= 0.f) || !std::isfinite(a->eps) || (a->interleaved != 0 && a->interleaved != 1)) return S2_ERR_BAD_PARAM;
+  if (a->batch < 1 || a->heads < 1 || a->seqlen < 0) return S2_ERR_SHAPE;
+  if (a->head_dim != 64 && a->head_dim != 128) return S2_ERR_SHAPE;
+  if (a->rotary_dim < 0 || a->rotary_dim > a->head_dim || a->rotary_dim % 16 != 0) return S2_ERR_SHAPE;
+  const int64_t rows = (int64_t)a->batch * a->seqlen;
+  if (rows > s2::kMostGroups || rows * a->heads > std::numeric_limits<int32_t>::max()) return S2_ERR_SHAPE;
+  for (int64_t s : {a->in_stride_b, a->in_stride_h, a->in_stride_t, a->out_stride_b, a->out_stride_h, a->out_stride_t}) {
+    if (s < 0 || (s & 7) != 0) return S2_ERR_ALIGN;
+    if (s > (int64_t)1 << 40) return S2_ERR_SHAPE;
+  }
+  const bool alike = (a->batch == 1 || a->in_stride_b == a->out_stride_b) && (a->heads == 1 || a->in_stride_h == a->out_stride_h) &&
+                     (a->seqlen <= 1 || a->in_stride_t == a->out_stride_t);
+  for (int i = 0; i < 2; ++i) {
+    if (!x[i]) continue;
+    for (const void* y : {x[i], (const void*)out[i], bwd ? g[i] : nullptr, (const void*)weight[i]})
+      if (!aligned16(y)) return S2_ERR_ALIGN;
+    if (bwd && (reinterpret_cast<uintptr_t>(d_weight[i]) & 3u) != 0) return S2_ERR_ALIGN;
+    // (in place a row goes where it came from)
+    if (!alike && out[i] == (bwd ? g[i] : x[i])) return S2_ERR_SHAPE;
+    p.x[i] = static_cast<const uint16_t*>(x[i]);
+    p.y[i] = static_cast<uint16_t*>(out[i]);
+    p.g[i] = static_cast<const uint16_t*>(g[i]);
+    p.weight[i] = weight[i];
+    p.d_weight[i] = d_weight[i];
+  }
+  if ((reinterpret_cast<uintptr_t>(a->inv_freq) & 3u) != 0 || (reinterpret_cast<uintptr_t>(a->positions) & 3u) != 0) return S2_ERR_ALIGN;
+  p.inv_freq = a->inv_freq;
+  p.positions = a->positions;
+  p.batch = a->batch;
+  p.heads = a->heads;
+  p.seqlen = a->seqlen;
+  p.head_dim = a->head_dim;
+  p.rotary_dim = a->rotary_dim;
+  p.interleaved = a->interleaved;
+  p.eps = a->eps;
+  p.x_sb = a->in_stride_b;
+  p.x_sh = a->in_stride_h;
+  p.x_st = a->in_stride_t;
+  p.y_sb = a->out_stride_b;
+  p.y_sh = a->out_stride_h;
+  p.y_st = a->out_stride_t;
+  p.rows = (int)rows;
+  return S2_OK;
+}
+
 }  // namespace
+
+int s2_attn_chunk_paged(const s2_layout_params* lp, const s2_paged_cache* c, const s2_chunk_args* a, float scale, void* workspace,
+                        size_t workspace_bytes, void* stream) {
+  if (!lp || !c || !a) return S2_ERR_NULL;
+  return chunk_cache(lp, nullptr, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+int s2_attn_chunk_paged_layout(const s2_layout* layout, const s2_paged_cache* c, const s2_chunk_args* a, float scale, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  if (!layout || !c || !a) return S2_ERR_NULL;
+  return chunk_cache(&layout->p, layout, c, a, scale, workspace, workspace_bytes, stream);
+}
+
+size_t s2_attn_chunk_workspace_bytes(int32_t nseq, int32_t heads, int32_t max_new, int32_t num_rows, int32_t head_dim, int32_t max_len, int32_t num_splits) {
+  if (nseq < 1 || heads < 1 || max_new < 1 || num_rows < 1 || head_dim < 1) return 0;
+  s2::CacheChunkParams p = chunk_sizes(nseq, heads, max_new, num_rows);
+  if (num_splits <= 0) num_splits = most_chunk_splits(s2::chunk_tiles(p) * heads, max_len);
+  if (num_splits == 1) return 0;
+  const size_t items = (size_t)nseq * heads * p.max_new * num_splits;
+  return ((items * (head_dim + 2) * sizeof(float) + 255) / 256) * 256;
+}
+
+int s2_kv_plan_paged(const s2_layout_params* lp, const s2_kv_plan_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!lp || !a) return S2_ERR_NULL;
+  return kv_plan(lp, nullptr, a, workspace, workspace_bytes, stream);
+}
+
+int s2_kv_plan_paged_layout(const s2_layout* layout, const s2_kv_plan_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!layout || !a) return S2_ERR_NULL;
+  return kv_plan(&layout->p, layout, a, workspace, workspace_bytes, stream);
+}
+
+size_t s2_kv_plan_workspace_bytes(int32_t nseq, int32_t heads) {
+  if (nseq < 1 || heads < 1) return 0;
+  s2::KvPlanParams p{};
+  p.nseq = nseq;
+  p.pairs = (int64_t)nseq * heads;
+  s2::plan_groups(p);
+  return plan_workspace(p).bytes;
+}
+
+int s2_qk_norm_rope_fwd(const s2_qk_norm_rope_args* a, void* stream) {
+  if (!a) return S2_ERR_NULL;
+  s2::QkRopeParams p{};
+  const int st = qk_rope(a, false, p);
+  if (st != S2_OK || p.rows == 0) return st;
+  if (s2::qk_rope_groups(p) > s2::kMostGroups) return S2_ERR_SHAPE;
+  return hip_ok(s2::launch_qk_rope(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+int s2_qk_norm_rope_bwd(const s2_qk_norm_rope_args* a, void* workspace, size_t workspace_bytes, void* stream) {
+  if (!a) return S2_ERR_NULL;
+  s2::QkRopeParams p{};
+  const int st = qk_rope(a, true, p);
+  if (st != S2_OK) return st;
+  if ((a->q && a->q_weight) || (a->k && a->k_weight)) {
+    if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) != 0 ||
+        workspace_bytes < s2_qk_norm_rope_bwd_workspace_bytes(a->batch, a->heads, a->seqlen, a->head_dim))
+      return S2_ERR_WORKSPACE;
+    p.part = static_cast<float*>(workspace);
+  }
+  if (p.rows == 0 && !p.part) return S2_OK;
+  return hip_ok(s2::launch_qk_rope_bwd(p, static_cast<hipStream_t>(stream))) ? S2_OK : S2_ERR_HIP;
+}
+
+size_t s2_qk_norm_rope_bwd_workspace_bytes(int32_t batch, int32_t heads, int32_t seqlen, int32_t head_dim) {
+  if (batch < 1 || heads < 1 || seqlen < 0 || (head_dim != 64 && head_dim != 128)) return 0;
+  const int64_t rows = std::min<int64_t>((int64_t)batch * seqlen, s2::kMostGroups);
+  return ((size_t)std::max(1, s2::qk_rope_parts((int)rows, heads, head_dim)) * 2 * head_dim * sizeof(float) + 255) / 256 * 256;
+}
 
 int s2_kv_append_paged(const s2_paged_cache* c, const s2_kv_append_args* a, void* stream) {
   if (!c || !a) return S2_ERR_NULL;

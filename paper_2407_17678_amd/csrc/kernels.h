@@ -181,6 +181,87 @@ struct CacheAttnParams {
   FastDiv by_heads, by_splits, by_stride;  // set by launch_cache_attn
 };
 
+// Block tables for a step (s2_kv_plan_args).
+constexpr int kRingEach = 4096;  // entries of the ring to a workgroup
+struct KvPlanParams {
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* new_lens;
+  const int32_t* query_from;  // nullptr: lens
+  const int32_t* ring;
+  const int32_t* free_state;
+  int32_t* new_table;
+  int32_t* new_ring;
+  int32_t* new_state;
+  int32_t* cu_new;
+  int32_t* positions;
+  int32_t* seq_lens;
+  int32_t* short_of;
+  // workspace: of a sequence its tokens before and after, the row of its first query and its new tokens; of a (sequence, head), and of a workgroup's, the pages that
+  // are given up and taken; the state of the ring; new tokens of 256 sequences each
+  int32_t* ws_seq;
+  int32_t* ws_pair;
+  int32_t* ws_group;
+  int32_t* ws_state;
+  int64_t* ws_fresh;
+  int64_t pairs;
+  int nseq, heads, max_blocks, max_len, num_pages, num_rows, block_shift;
+  bool apart;                 // the new table is not the old one
+  int pairs_each, groups;     // (sequence, head) pairs to a wavefront, workgroups over the tables (set by plan_groups)
+  // the pattern, as in DecodeParams
+  int block_size, local_blocks, stride, window_blocks, dense, head_index_base;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  int num_blocks;
+  const int32_t* last_row;    // with a layout: the last row that keeps a block, [heads, num_blocks]
+  FastDiv by_heads, by_stride;  // set by launch_kv_plan
+};
+
+// Norm and rotation of queries and keys (s2_qk_norm_rope_args): [0] of q, [1] of k.
+struct QkRopeParams {
+  const uint16_t* x[2];
+  uint16_t* y[2];              // fwd: results; bwd: gradients of x
+  const uint16_t* g[2];        // bwd: gradients of the results
+  const float* weight[2];
+  float* d_weight[2];
+  float* part;                 // bwd: [part][2][head_dim] sums of the weights' gradients
+  const float* inv_freq;
+  const int32_t* positions;
+  int batch, heads, seqlen, head_dim, rotary_dim, interleaved;
+  float eps;
+  int64_t x_sb, x_sh, x_st;    // of x (and of its gradients)
+  int64_t y_sb, y_sh, y_st;    // of the results
+  // set by the launch: a wavefront's heads, wavefronts to a row, rows to a wavefront (bwd)
+  int rows;
+  int heads_each, head_groups, parts;
+  FastDiv by_groups, by_seqlen;
+};
+
+// Attention of a chunk of new tokens over a paged cache (s2_chunk_args).
+struct CacheChunkParams {
+  CacheRef c;
+  const uint16_t* q;
+  const int32_t* cu;
+  const int32_t* start;
+  uint16_t* o;
+  float* lse;       // [heads, num_rows]
+  float* part_acc;  // [nseq * heads * max_new][split][head_dim]
+  float* part_ml;   // [nseq * heads * max_new][split][2]  (max, sum)
+  int32_t* missing;
+  int nseq, heads, num_rows, max_new, max_len, num_splits;
+  int64_t q_sr, q_sh;
+  float scale, scale_log2e;
+  // the pattern, as in DecodeParams
+  int block_size, local_blocks, stride, window_blocks, dense, head_index_base;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  int num_blocks;
+  // set by chunk_tiles: rows of a tile (1 << tile_shift), tiles of the launch; seq_tiles of them to a sequence, or (packed) to all
+  int tile_shift, seq_tiles, num_tiles;
+  bool packed;
+  FastDiv by_heads, by_splits, by_stride, by_tiles;  // set by launch_cache_chunk
+};
+
 // Each returns the hipError_t of the launch (hipGetLastError after the launch).
 hipError_t launch_fwd(const AttnParams& p, bool dense, hipStream_t stream);
 // The launch of it for mask blocks of 16 and 32 tokens (row_map set).
@@ -215,5 +296,19 @@ hipError_t launch_kv_rows(const KvRowsParams& p, hipStream_t stream);
 // Up to so many workgroups a decode step over 8 or 4 bits takes eight wavefronts to each instead of four.
 constexpr int kCacheWideGroups = 256;
 hipError_t launch_cache_attn(const CacheAttnParams& p, hipStream_t stream);
+// Rows up to which a chunk is one tile wherever its positions lie.
+constexpr int kChunkFew = 64;
+// The tiles of a launch over chunks (sets the tile fields), and the launch.
+int64_t chunk_tiles(CacheChunkParams& p);
+hipError_t launch_cache_chunk(const CacheChunkParams& p, hipStream_t stream);
+// The workgroups over the tables (sets the group fields), and the launch.
+void plan_groups(KvPlanParams& p);
+hipError_t launch_kv_plan(const KvPlanParams& p, hipStream_t stream);
+// The workgroups of the forward, and its launch.
+int64_t qk_rope_groups(const QkRopeParams& p);
+hipError_t launch_qk_rope(const QkRopeParams& p, hipStream_t stream);
+// Workgroups that leave sums of the weights' gradients, and the launch of the backward.
+int qk_rope_parts(int rows, int heads, int head_dim);
+hipError_t launch_qk_rope_bwd(const QkRopeParams& p, hipStream_t stream);
 
 }  // namespace s2

@@ -57,6 +57,7 @@ struct s2_layout {
   int device = -1;
   int32_t* d_row_ptr = nullptr;  // device copies of the compressed rows (decode reads one row of them)
   int32_t* d_col_idx = nullptr;
+  int32_t* d_last_row = nullptr;  // [H*B]: the last row that keeps a block (block tables are planned by it)
   s2::TileList q_tiles;   // row groups  -> kept KV blocks   (forward, dQ pass)
   s2::TileList kv_tiles;  // column groups -> attending Q blocks (dK/dV pass)
   // Of the key tiles the kernels walk: the ways to cut them, and what choosing one takes

@@ -47,10 +47,25 @@ union {
 } cache_api;
 constexpr Py_ssize_t kCacheEntryPoints = sizeof(CacheApi) / sizeof(void*);
 
+// The entry points of what surrounds attention in a step, in the order bind_step() is given their addresses (_STEP_CALLS in binding.py).
+#define S2_STEP_ENTRY_POINTS(X) \
+  X(s2_attn_chunk_paged, chunk) X(s2_attn_chunk_paged_layout, chunk_layout) X(s2_kv_plan_paged, plan) X(s2_kv_plan_paged_layout, plan_layout) \
+  X(s2_qk_norm_rope_fwd, rope_fwd) X(s2_qk_norm_rope_bwd, rope_bwd)
+struct StepApi {
+#define X(entry, name) decltype(&entry) name;
+  S2_STEP_ENTRY_POINTS(X)
+#undef X
+};
+union {
+  StepApi f;
+  void* at[sizeof(StepApi) / sizeof(void*)];
+} step_api;
+constexpr Py_ssize_t kStepEntryPoints = sizeof(StepApi) / sizeof(void*);
+
 struct Names {
   PyObject *data_ptr, *stride, *shape, *is_contiguous, *numel, *element_size, *value, *dtype;
 } names;
-// torch's objects for the types of elements, for as long as the process lives (set by bind_cache())
+// torch's objects for the types of elements, for as long as the process lives (set by bind_cache() and bind_step())
 struct Types {
   PyObject *bf16, *i32, *f32;
 } types;
@@ -625,6 +640,199 @@ PyObject* drafts(PyObject* const* a, Py_ssize_t n) {
 PyObject* tree(PyObject*, PyObject* const* a, Py_ssize_t n) { return drafts<false>(a, n); }
 PyObject* tree_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return drafts<true>(a, n); }
 
+// params or layout, cache, q cu_new start o lse, scale, workspace, max_new, missing, num_splits, stream
+template <bool LAYOUT>
+PyObject* chunk_call(PyObject* const* a, Py_ssize_t n) {
+  s2_paged_cache c;
+  s2_chunk_args d{};
+  float scale;
+  void *pattern, *stream, *ws = nullptr;
+  size_t bytes = 0;
+  int64_t size[3], stride[2];
+  if (!count_is(n, 13) || !cache_of(a[1], c) || !pair_of(a[2], a[5], 3, size, stride)) return nullptr;
+  if (size[1] != c.heads || size[2] != c.head_dim || size[0] > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  if (!ints_of(a[3], (int64_t)c.nseq + 1, d.cu_new) || !ints_of(a[4], c.nseq, d.start) || !lse_of(a[6], (int64_t)c.heads * size[0], d.lse) ||
+      !counter_of(a[10], d.missing) || !data_of(a[2], d.q) || !data_of(a[5], d.o) || !as_int(a[9], d.max_new) || !as_int(a[11], d.num_splits) ||
+      !as_address(a[0], pattern) || !as_float(a[7], scale) || (a[8] != Py_None && !workspace_of(a[8], ws, bytes)) || !as_address(a[12], stream))
+    return nullptr;
+  d.num_rows = (int32_t)size[0];
+  d.q_stride_row = stride[0];
+  d.q_stride_head = stride[1];
+  return status_of([&] {
+    if constexpr (LAYOUT)
+      return step_api.f.chunk_layout(static_cast<s2_layout*>(pattern), &c, &d, scale, ws, bytes, stream);
+    else
+      return step_api.f.chunk(static_cast<s2_layout_params*>(pattern), &c, &d, scale, ws, bytes, stream);
+  });
+}
+PyObject* chunk(PyObject*, PyObject* const* a, Py_ssize_t n) { return chunk_call<false>(a, n); }
+PyObject* chunk_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return chunk_call<true>(a, n); }
+
+// int32, side by side, `count` of them, or None
+bool ints_or_none(PyObject* t, int64_t count, const int32_t*& at) {
+  at = nullptr;
+  return t == Py_None || ints_of(t, count, at);
+}
+bool out_ints(PyObject* t, int64_t count, int32_t*& at) { return row_of(t, types.i32, count, at); }
+bool out_ints_or_none(PyObject* t, int64_t count, int32_t*& at) {
+  at = nullptr;
+  return t == Py_None || out_ints(t, count, at);
+}
+
+// params or layout, block_table lens new_lens free_pages free_state new_table new_free_pages new_free_state, workspace, cu_new positions seq_lens query_from short_of,
+// stream
+template <bool LAYOUT>
+PyObject* plan_call(PyObject* const* a, Py_ssize_t n) {
+  s2_kv_plan_args d{};
+  void *pattern, *stream, *ws;
+  size_t bytes;
+  int64_t table[3], other[3], pages[1], rows = 0;
+  if (!count_is(n, 16) || !sizes_and_type(a[1], 3, types.i32, table) || !sizes_and_type(a[6], 3, types.i32, other) || !sizes_and_type(a[4], 1, types.i32, pages))
+    return nullptr;
+  for (int i = 0; i < 3; ++i)
+    if (table[i] != other[i] || table[i] > INT32_MAX) {
+      fail_assert();
+      return nullptr;
+    }
+  if (pages[0] > INT32_MAX) {
+    fail_assert();
+    return nullptr;
+  }
+  const int64_t entries = table[0] * table[1] * table[2];
+  if (a[11] != Py_None) {
+    const Ref count(PyObject_CallMethodNoArgs(a[11], names.numel));
+    if (!count.o || !as_i64(count.o, rows)) return nullptr;
+    if (rows > INT32_MAX) {
+      fail_assert();
+      return nullptr;
+    }
+  }
+  if (!ints_of(a[1], entries, d.block_table) || !ints_of(a[2], table[0], d.lens) || !ints_of(a[3], table[0], d.new_lens) ||
+      !ints_of(a[4], pages[0], d.free_pages) || !ints_of(a[5], 2, d.free_state) || !out_ints(a[6], entries, d.new_table) ||
+      !out_ints(a[7], pages[0], d.new_free_pages) || !out_ints(a[8], 2, d.new_free_state) || !workspace_of(a[9], ws, bytes) ||
+      !out_ints_or_none(a[10], table[0] + 1, d.cu_new) || !out_ints_or_none(a[11], rows, d.positions) || !out_ints_or_none(a[12], table[0], d.seq_lens) ||
+      !ints_or_none(a[13], table[0], d.query_from) || !counter_of(a[14], d.short_of) || !as_address(a[0], pattern) || !as_address(a[15], stream))
+    return nullptr;
+  d.nseq = (int32_t)table[0];
+  d.heads = (int32_t)table[1];
+  d.max_blocks = (int32_t)table[2];
+  d.num_pages = (int32_t)pages[0];
+  d.num_rows = (int32_t)rows;
+  return status_of([&] {
+    if constexpr (LAYOUT)
+      return step_api.f.plan_layout(static_cast<s2_layout*>(pattern), &d, ws, bytes, stream);
+    else
+      return step_api.f.plan(static_cast<s2_layout_params*>(pattern), &d, ws, bytes, stream);
+  });
+}
+PyObject* plan(PyObject*, PyObject* const* a, Py_ssize_t n) { return plan_call<false>(a, n); }
+PyObject* plan_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return plan_call<true>(a, n); }
+
+// Tensors [batch, heads, seqlen, head_dim] of one call that have the same sizes, and in a family (q and k as they go in, or as they come out) the same strides; None
+// where there is none.
+struct Family {
+  bool any = false;
+  PyObject* like = nullptr;
+  int64_t stride[3] = {0, 0, 0};
+};
+alignas(16) char nothing[16];  // where a tensor without elements lies (which has no address of its own): nothing is read or written there
+bool member_of(PyObject* t, Family& f, int64_t* size, bool& sized, void*& at) {
+  at = nullptr;
+  if (t == Py_None) return true;
+  int64_t mine[4], stride[3];
+  if (!sizes_and_type(t, 4, types.bf16, mine)) return false;
+  for (int i = 0; i < 4; ++i) {
+    if ((sized && mine[i] != size[i]) || mine[i] > INT32_MAX) return fail_assert();
+    size[i] = mine[i];
+  }
+  sized = true;
+  if (!strides_of_both(f.any ? f.like : t, t, 4, mine, stride)) return false;
+  for (int i = 0; i < 3; ++i) f.stride[i] = stride[i];
+  f.any = true;
+  f.like = t;
+  if (!data_of(t, at)) return false;
+  if (!at && mine[0] * mine[2] == 0) at = nothing;
+  return true;
+}
+bool weight_of(PyObject* t, int64_t count, float*& at) {
+  at = nullptr;
+  return t == Py_None || row_of(t, types.f32, count, at);
+}
+
+// q k, (backward: d_q_out d_k_out dq dk, else q_out k_out), q_weight k_weight, (backward: dq_weight dk_weight), inv_freq, eps, (backward: workspace), positions,
+// interleaved, stream
+template <bool BWD>
+PyObject* rope_call(PyObject* const* a, Py_ssize_t n) {
+  s2_qk_norm_rope_args d{};
+  constexpr int W = BWD ? 6 : 4, F = BWD ? 10 : 6, P = BWD ? 13 : 8;
+  if (!count_is(n, P + 3)) return nullptr;
+  Family in, out;
+  int64_t size[4] = {0, 0, 0, 0};
+  bool sized = false;
+  void *q, *k, *to[4] = {nullptr, nullptr, nullptr, nullptr}, *ws = nullptr, *stream;
+  size_t bytes = 0;
+  if (!member_of(a[0], in, size, sized, q) || !member_of(a[1], in, size, sized, k)) return nullptr;
+  for (int i = 2; i < W; ++i)
+    if (!member_of(a[i], BWD && i >= 4 ? in : out, size, sized, to[i - 2])) return nullptr;
+  float *weight[2], *d_weight[2] = {nullptr, nullptr};
+  for (int i = 0; i < 2; ++i)
+    if (!weight_of(a[W + i], size[3], weight[i]) || (BWD && !weight_of(a[W + 2 + i], size[3], d_weight[i]))) return nullptr;
+  float* freq = nullptr;
+  int64_t pairs = 0;
+  if (a[F] != Py_None) {
+    const Ref count(PyObject_CallMethodNoArgs(a[F], names.numel));
+    if (!count.o || !as_i64(count.o, pairs) || !row_of(a[F], types.f32, pairs, freq)) return nullptr;
+    if (pairs > INT32_MAX / 2) {
+      fail_assert();
+      return nullptr;
+    }
+  }
+  const int at_eps = F + 1;
+  if (!as_float(a[at_eps], d.eps) || (BWD && a[at_eps + 1] != Py_None && !workspace_of(a[at_eps + 1], ws, bytes))) return nullptr;
+  if (!ints_or_none(a[P], size[0] * size[2], d.positions)) return nullptr;
+  const int interleaved = PyObject_IsTrue(a[P + 1]);
+  if (interleaved < 0 || !as_address(a[P + 2], stream)) return nullptr;
+  d.q = q;
+  d.k = k;
+  if (BWD) {
+    d.d_q_out = to[0];
+    d.d_k_out = to[1];
+    d.dq = to[2];
+    d.dk = to[3];
+  } else {
+    d.q_out = to[0];
+    d.k_out = to[1];
+  }
+  d.q_weight = weight[0];
+  d.k_weight = weight[1];
+  d.dq_weight = d_weight[0];
+  d.dk_weight = d_weight[1];
+  d.inv_freq = freq;
+  d.batch = (int32_t)size[0];
+  d.heads = (int32_t)size[1];
+  d.seqlen = (int32_t)size[2];
+  d.head_dim = (int32_t)size[3];
+  d.rotary_dim = (int32_t)(2 * pairs);
+  d.interleaved = interleaved;
+  d.in_stride_b = in.stride[0];
+  d.in_stride_h = in.stride[1];
+  d.in_stride_t = in.stride[2];
+  d.out_stride_b = out.stride[0];
+  d.out_stride_h = out.stride[1];
+  d.out_stride_t = out.stride[2];
+  return status_of([&] {
+    if constexpr (BWD)
+      return step_api.f.rope_bwd(&d, ws, bytes, stream);
+    else
+      return step_api.f.rope_fwd(&d, stream);
+  });
+}
+PyObject* rope_fwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return rope_call<false>(a, n); }
+PyObject* rope_bwd(PyObject*, PyObject* const* a, Py_ssize_t n) { return rope_call<true>(a, n); }
+
 PyObject* bind_to(void** to, Py_ssize_t count, PyObject* const* a, Py_ssize_t n) {
   if (!count_is(n, count)) return nullptr;
   for (Py_ssize_t i = 0; i < n; ++i)
@@ -636,17 +844,19 @@ PyObject* bind_to(void** to, Py_ssize_t count, PyObject* const* a, Py_ssize_t n)
   Py_RETURN_NONE;
 }
 PyObject* bind(PyObject*, PyObject* const* a, Py_ssize_t n) { return bind_to(api.at, kEntryPoints, a, n); }
-PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t n) {
+bool find_types() {
   const Ref torch(PyImport_ImportModule("torch"));
-  if (!torch.o) return nullptr;
+  if (!torch.o) return false;
   const struct {
     PyObject** at;
     const char* name;
   } all[] = {{&types.bf16, "bfloat16"}, {&types.i32, "int32"}, {&types.f32, "float32"}};
   for (const auto& t : all)
-    if (!*t.at && !(*t.at = PyObject_GetAttrString(torch.o, t.name))) return nullptr;
-  return bind_to(cache_api.at, kCacheEntryPoints, a, n);
+    if (!*t.at && !(*t.at = PyObject_GetAttrString(torch.o, t.name))) return false;
+  return true;
 }
+PyObject* bind_cache(PyObject*, PyObject* const* a, Py_ssize_t n) { return find_types() ? bind_to(cache_api.at, kCacheEntryPoints, a, n) : nullptr; }
+PyObject* bind_step(PyObject*, PyObject* const* a, Py_ssize_t n) { return find_types() ? bind_to(step_api.at, kStepEntryPoints, a, n) : nullptr; }
 
 #define S2_METHOD(name) {#name, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(name)), METH_FASTCALL, nullptr}
 PyMethodDef methods[] = {S2_METHOD(bind),          S2_METHOD(fwd),          S2_METHOD(fwd_rows),      S2_METHOD(fwd_varlen),
@@ -654,7 +864,9 @@ PyMethodDef methods[] = {S2_METHOD(bind),          S2_METHOD(fwd),          S2_M
                          S2_METHOD(decode),        S2_METHOD(decode_static), S2_METHOD(decode_layout), S2_METHOD(decode_paged),
                          S2_METHOD(decode_paged_layout), S2_METHOD(bind_cache), S2_METHOD(paged_cache), S2_METHOD(kv_append),
                          S2_METHOD(kv_read),       S2_METHOD(decode_cache), S2_METHOD(decode_cache_layout), S2_METHOD(tree),
-                         S2_METHOD(tree_layout),   {nullptr, nullptr, 0, nullptr}};
+                         S2_METHOD(tree_layout),   S2_METHOD(bind_step),    S2_METHOD(chunk),         S2_METHOD(chunk_layout),
+                         S2_METHOD(plan),          S2_METHOD(plan_layout),  S2_METHOD(rope_fwd),      S2_METHOD(rope_bwd),
+                         {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_marshal", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 
@@ -674,12 +886,13 @@ PyMODINIT_FUNC PyInit__marshal(void) {
 #define X(entry, name) #entry,
   const char* const entries[] = {S2_ENTRY_POINTS(X)};
   const char* const cache_entries[] = {S2_CACHE_ENTRY_POINTS(X)};
+  const char* const step_entries[] = {S2_STEP_ENTRY_POINTS(X)};
 #undef X
   const struct {
     const char* attribute;
     const char* const* entry;
     Py_ssize_t count;
-  } orders[] = {{"entry_points", entries, kEntryPoints}, {"cache_entry_points", cache_entries, kCacheEntryPoints}};
+  } orders[] = {{"entry_points", entries, kEntryPoints}, {"cache_entry_points", cache_entries, kCacheEntryPoints}, {"step_entry_points", step_entries, kStepEntryPoints}};
   for (const auto& of : orders) {
     const Ref order(PyTuple_New(of.count));
     if (!order.o) return nullptr;
