@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libs2attn.so")
 MARSHAL = os.path.join(HERE, "_marshal.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
-SOURCES = ["api.hip", "layout.cpp", "fwd_pipe_kernel.hip", "fwd_gather_kernel.hip", "bwd_kernel.hip", "bwd_merged_kernel.hip", "dq_pipe_kernel.hip", "dq_gemm_kernel.hip", "decode_kernel.hip", "cache_attn_kernel.hip", "cache_attn_shared_kernel.hip", "cache_decode_kernel.hip", "kv_cache_kernel.hip", "cache_chunk_kernel.hip", "kv_plan_kernel.hip", "qk_rope_kernel.hip", "probe_kernel.hip"]
+SOURCES = ["api.hip", "layout.cpp", "fwd_pipe_kernel.hip", "fwd_gather_kernel.hip", "bwd_kernel.hip", "bwd_merged_kernel.hip", "dq_pipe_kernel.hip", "dq_gemm_kernel.hip", "decode_kernel.hip", "cache_attn_kernel.hip", "cache_attn_shared_kernel.hip", "cache_decode_kernel.hip", "kv_cache_kernel.hip", "cache_chunk_kernel.hip", "cache_chunk_wide_kernel.hip", "kv_plan_kernel.hip", "qk_rope_kernel.hip", "probe_kernel.hip"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-Wno-unused-function"]
 # gfx950 only.  Packed-fp32 VALU forms are switched off for the device pass (the host pass

@@ -117,6 +117,23 @@ struct CacheRows {
       }
   }
 
+  // Operand kk as operands() gives it, or (8 or 4 bits, where `turned` is all ones instead of 0) the one beside it in its pair.
+  __device__ static __forceinline__ u32x4 operand(const Part& p, int g, int kk, uint32_t turned) {
+    auto of = [&](int i, int j) __attribute__((always_inline)) { return (p.x[i] & ~turned) | (p.x[j] & turned); };
+    if constexpr (FMT == S2_KV_BF16) {
+      return u32x4{p.x[4 * kk], p.x[4 * kk + 1], p.x[4 * kk + 2], p.x[4 * kk + 3]};
+    } else if constexpr (FMT == S2_KV_MXFP8) {
+      const float s = scale_of((p.scales >> (8 * (g >> 1)) >> (16 * (kk >> 1))) & 255);
+      uint32_t lo[2], hi[2];
+      values8(of(2 * kk, 2 * (kk ^ 1)), s, lo);
+      values8(of(2 * kk + 1, 2 * (kk ^ 1) + 1), s, hi);
+      return u32x4{lo[0], lo[1], hi[0], hi[1]};
+    } else {
+      const float s = scale_of((p.scales >> (8 * (D == 128 ? g : g >> 1))) & 255);
+      return values4(of(kk, kk ^ 1), s);
+    }
+  }
+
   // acc[8 * kk + e] += pr * (feature e of operand kk), in 32 bits
   __device__ static __forceinline__ void add_times(const Part& p, int g, float pr, float (&acc)[D / 4]) {
     static_assert(kScaled, "");
