@@ -75,6 +75,17 @@ __device__ __forceinline__ const CacheChunkParams& chunk_params() {
   return *(const CacheChunkParams*)at;
 }
 
+// (loaded as a whole: word by word, where each is used, they are a dozen trips to memory one after the other)
+__device__ __forceinline__ ChunkLookUp chunk_look_up() {
+  typedef uint32_t u32x16 __attribute__((ext_vector_type(16)));
+  const char* const at = reinterpret_cast<const char*>(&chunk_params().look_up);
+  struct {
+    u32x16 a, b;
+  } w = {load_const<u32x16>(at), load_const<u32x16>(at + 64)};
+  asm volatile("" : "+s"(w.a), "+s"(w.b));
+  return __builtin_bit_cast(ChunkLookUp, w);
+}
+
 // Positions [lo, hi) of a tile that the table has room for, and the block rows they lie in (eight at most).
 struct ChunkRows {
   int lo, hi, row0, n_rows;
@@ -103,7 +114,8 @@ __device__ __forceinline__ ChunkQuery chunk_query(const CacheChunkParams& p, con
 
 // 64 tokens: of one block, or (SMALL) four pieces of 16 of the list's blocks, as a wavefront holds them.  What masks need of its pieces lies in LDS, for the last four units.
 struct ChunkUnit {
-  int page, info, at;        // of the wavefront's own piece: page, tokens to read | block rows that keep them << 8, position of the first
+  int64_t off, scale_off;    // where the wavefront's own piece begins, its scales (bytes in either pool)
+  int rows;                  // tokens to read of it
   int flags;
   __device__ __forceinline__ bool on(int half) const { return flags >> half & 1; }  // some query of the wavefront attends some token of the half
   __device__ __forceinline__ bool some() const { return flags >> 2 & 1; }           // some query of the workgroup may not attend some token
@@ -154,7 +166,8 @@ struct ChunkWalk {
   uint32_t ring;                     // where the pieces lie
   int n_missing = 0;
   int turn = -1, u_now = 0, u_end = 0;
-  int page = 0, info = 0, at = 0;    // of this lane's unit (piece)
+  int info = 0, at = 0;              // of this lane's unit (piece): tokens to read | block rows that keep them << 8, position of the first
+  uint32_t off[2] = {0, 0}, scale_off[2] = {0, 0};
   uint64_t live = 0, some = 0, on[2] = {0, 0};
 
   // (scope_: in LDS, filled for the workgroup; ring_: room for kRing pairs of words there; q0, q1: a lane's first query and its last)
@@ -178,7 +191,7 @@ struct ChunkWalk {
     return (pieces | pieces >> 2) & 0x1111111111111111ull;
   }
 
-  __device__ __forceinline__ static RowBlocks blocks_of(const CacheChunkParams& p, const ChunkScope& s, int turn_) {
+  __device__ __forceinline__ static RowBlocks blocks_of(const ChunkLookUp& p, const ChunkScope& s, int turn_) {
     RowBlocks rb = row_blocks(p, s.h, s.r.row0 + turn_);
     if (!p.row_ptr) rb.count = rb.n_stripe + (s.r.row0 + s.r.n_rows - rb.local_lo);
     return rb;
@@ -186,10 +199,10 @@ struct ChunkWalk {
 
   // Looks up the next units that there are; false: there are none.
   __device__ __forceinline__ bool look_up() {
-    const CacheChunkParams& p = chunk_params();
+    const ChunkLookUp p = chunk_look_up();
     const ChunkScope s = scope_now(scope);
     const ChunkRows& r = s.r;
-    const int sh = p.c.block_shift, S = 1 << sh, turns = p.row_ptr ? r.n_rows : 1;
+    const int sh = p.block_shift, S = 1 << sh, turns = p.row_ptr ? r.n_rows : 1;
     RowBlocks rb;
     if (u_now < u_end) rb = blocks_of(p, s, turn);
     while (u_now >= u_end) {
@@ -217,8 +230,8 @@ struct ChunkWalk {
       }
     }
     if (bits == 0) rows = 0;
-    page = rows > 0 ? p.c.table[((int64_t)s.b * p.heads + s.h) * p.c.max_blocks + blk] : 0;
-    const bool held = page >= 0 && page < p.c.num_pages;
+    int page = rows > 0 ? p.table[((int64_t)s.b * p.heads + s.h) * p.max_blocks + blk] : 0;
+    const bool held = page >= 0 && page < p.num_pages;
     if (__any(rows > 0 && !held) && p.missing) {
       // a block counts once: in the tile of the first of the chunk's rows that keeps it (in closed form no row drops a block and keeps it later)
       bool counts = rows > 0 && !held && skip == 0;
@@ -237,6 +250,11 @@ struct ChunkWalk {
     }
     if (!held) page = rows = 0;
     info = rows | bits << 8;
+    const int64_t o = page * p.page + skip * p.tok, so = page * p.scale_page + skip * p.scale_tok;
+    off[0] = (uint32_t)o;
+    off[1] = (uint32_t)(o >> 32);
+    scale_off[0] = (uint32_t)so;
+    scale_off[1] = (uint32_t)(so >> 32);
     const int all = (1 << r.n_rows) - 1;
     live = of_units(__ballot(rows > 0));
     some = of_units(__ballot(rows < kTokens || bits != all || at + rows - 1 > r.lo));
@@ -257,7 +275,7 @@ struct ChunkWalk {
   __device__ __forceinline__ bool next(int n, ChunkUnit& w) {
     while (live == 0)
       if (!look_up()) {
-        w.page = w.info = w.at = w.flags = 0;  // (no rows: loading it fetches nothing)
+        w.off = w.scale_off = w.rows = w.flags = 0;  // (no rows: loading it fetches nothing)
         return false;
       }
     const int i = __builtin_ctzll(live);
@@ -267,9 +285,12 @@ struct ChunkWalk {
       *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(ring + 8 * ((n & 3) * NB + mine)) = u32x2{(uint32_t)info, (uint32_t)at};
     w.flags = (int)(on[0] >> i & 1) | (int)(on[1] >> i & 1) << 1 | (int)(some >> i & 1) << 2;
     const int own = SMALL ? i + piece : i;
-    w.page = __builtin_amdgcn_readlane(page, own);
-    w.info = __builtin_amdgcn_readlane(info, own);
-    w.at = __builtin_amdgcn_readlane(at, own);
+    auto both = [&](const uint32_t (&x)[2]) __attribute__((always_inline)) {
+      return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x[1], own) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x[0], own));
+    };
+    w.off = both(off);
+    w.scale_off = both(scale_off);
+    w.rows = __builtin_amdgcn_readlane(info, own) & 255;
     return true;
   }
 };

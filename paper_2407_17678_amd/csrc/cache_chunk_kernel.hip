@@ -74,10 +74,9 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_chunk_kernel(const
   typename Rows::Part kr, vr;
   auto load = [&](auto is_v, const ChunkUnit& w, typename Rows::Part& to) __attribute__((always_inline)) {
     constexpr bool V = decltype(is_v)::value;
-    const int skip = w.at & (p.block_size - 1);
-    const uint8_t* const at = (V ? p.c.v : p.c.k) + w.page * p.c.page + skip * p.c.tok;
-    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + w.page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
-    Rows::load(to, at, scale_at, w.info & 255, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, gw);
+    const uint8_t* const at = (V ? p.c.v : p.c.k) + w.off;
+    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + w.scale_off : nullptr;
+    Rows::load(to, at, scale_at, w.rows, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + c, gw);
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};
@@ -305,6 +304,28 @@ hipError_t launch_cache_chunk(const CacheChunkParams& params, hipStream_t stream
   p.by_splits = fast_div(p.num_splits);
   p.by_stride = fast_div(p.stride > 0 ? p.stride : 1);
   p.by_tiles = fast_div(p.seq_tiles);
+  ChunkLookUp& l = p.look_up;
+  l.table = p.c.table;
+  l.page = p.c.page;
+  l.scale_page = p.c.scale_page;
+  l.row_ptr = p.row_ptr;
+  l.col_idx = p.col_idx;
+  l.missing = p.missing;
+  l.tok = p.c.tok;
+  l.scale_tok = p.c.scale_tok;
+  l.max_blocks = p.c.max_blocks;
+  l.num_pages = p.c.num_pages;
+  l.block_shift = p.c.block_shift;
+  l.heads = p.heads;
+  l.num_splits = p.num_splits;
+  l.local_blocks = p.local_blocks;
+  l.stride = p.stride;
+  l.window_blocks = p.window_blocks;
+  l.dense = p.dense;
+  l.head_index_base = p.head_index_base;
+  l.num_blocks = p.num_blocks;
+  l.by_splits = p.by_splits;
+  l.by_stride = p.by_stride;
   return p.c.head_dim == 128 ? launch_dim<128>(p, stream) : launch_dim<64>(p, stream);
 }
 

@@ -6,8 +6,9 @@
 // matrix instruction to each.  V lags behind K by a unit, so that both tiles of a trip are used up in it and one barrier a trip is enough: meanwhile each
 // wavefront brings its 16 rows of the next unit's K, and of this one's V, from registers to bf16 in the other stage, and asks for those after them.
 //
-// The running maximum is exact, by halves.  Where it moves, the accumulators lack the half whose probabilities were formed against the old one: they
-// are scaled a half step later, when it has been added.
+// The reference maximum of a query moves only where a score exceeds it by more than 2^8 (a probability is then up to 2^8, rounded as any other): one of 32 queries has a
+// new maximum in nearly every half step of the first hundred.  Where it moves, the accumulators lack the half whose probabilities were formed against the
+// old one: they are scaled a half step later, when it has been added.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -68,27 +69,27 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
 #pragma unroll
   for (int dt = 0; dt < DT; ++dt) acc[dt] = f32x16{};
   float m_run = kNegInf, mc = 0.f, l_run = 0.f, alpha = 1.f;  // mc: the maximum as exponents have it, 0 while nothing was seen
+  // how far a score may exceed it (finite, also where 2^8 is out of reach of any score: the first has to move it from -inf)
+  const float tau = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(__builtin_bit_cast(int, fminf(8.f / cl, 3.4e38f))));
   bool scaled = false;                                        // whether alpha is to be applied to the accumulators
 
-  const uint32_t write = lds_addr(sh_kv) + (16 * wave + (lane & 15)) * RB;
+  const uint32_t write = lds_addr(sh_kv) + (16 * wave + (lane & 15)) * RB + 2 * Rows::feature(0, lane >> 4);  // (feature(kk, g) is feature(kk, 0) further on)
   const uint32_t k_read = lds_addr(sh_kv) + l32 * RB + 16 * half, v_read = lds_addr(sh_kv) + 2 * Tile::tr_base(lane);
   constexpr int kV0 = 2 * Tile::kBytes;
 
   typename Rows::Part kr, vr;
   auto load = [&](auto is_v, const ChunkUnit& w, typename Rows::Part& to) S2_INLINE {
     constexpr bool V = decltype(is_v)::value;
-    const int skip = w.at & (p.block_size - 1);
-    const uint8_t* const at = (V ? p.c.v : p.c.k) + w.page * p.c.page + skip * p.c.tok;
-    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + w.page * p.c.scale_page + skip * p.c.scale_tok : nullptr;
+    const uint8_t* const at = (V ? p.c.v : p.c.k) + w.off;
+    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + w.scale_off : nullptr;
     const int ln = lane_now();
-    Rows::load(to, at, scale_at, w.info & 255, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + (ln & 15), ln >> 4);
+    Rows::load(to, at, scale_at, w.rows, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + (ln & 15), ln >> 4);
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};
   // operand kk of my row of 16 into a stage
-  auto put = [&](const typename Rows::Part& part, int kk, uint32_t to) S2_INLINE {
-    const int g = lane_now() >> 4;
-    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + 2 * Rows::feature(kk, g)) = Rows::operand(part, g, kk, 0);
+  auto put = [&](const typename Rows::Part& part, int g, int kk, uint32_t to) S2_INLINE {
+    *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(to + 2 * Rows::feature(kk, 0)) = Rows::operand(part, g, kk, 0);
   };
   // (what it has asked of the LDS is done before a wavefront is past it; loads from memory stay on their way)
   auto barrier = [&]() S2_INLINE {
@@ -104,7 +105,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
 
   // Half step H of trip t: scores of half H of unit t (sn), probabilities of the half before it (sc, pc), the product of half H of unit t - 1 (pp) with V.  on_n, on_s, on_p:
   // whether these are mine; some_n, some_p: whether a token of their units is not attended by some query.
-  auto half_step = [&](auto hc, int t, bool on_n, bool on_s, bool on_p, bool some_n, bool some_p, f32x16& sn, f32x16& sc, u32x4 (&pc)[2], u32x4 (&pp)[2],
+  auto half_step = [&](auto busy, auto hc, int t, bool on_n, bool on_s, bool on_p, bool some_n, bool some_p, f32x16& sn, f32x16& sc, u32x4 (&pc)[2], u32x4 (&pp)[2],
                        auto&& beside) S2_INLINE {
     constexpr int H = decltype(hc)::value;
     const uint32_t stage = (t & 1) * (uint32_t)Tile::kBytes;
@@ -113,7 +114,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
       // queries that attend them here, and taken out of V.
       const uint32_t seen = on_p ? seen_of(t - 1, H) : 0;
 #pragma unroll 1
-      for (int i = 0; i < 32; ++i) {
+      for (int i = 0; decltype(busy)::value && i < 32; ++i) {
         const uint32_t row = lds_addr(sh_kv) + kV0 + stage + (32 * H + i) * RB + 8 * half;
 #pragma unroll
         for (int dt = 0; dt < DT; ++dt)
@@ -130,6 +131,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
       barrier();
       clean_words(reinterpret_cast<uint32_t*>(sh_kv[2 + (t & 1)]) + (32 * H + 8 * wave) * RB / 4, 8 * RB / 4, lane);
       barrier();
+    }
+    if constexpr (!decltype(busy)::value) {
+      static_for<NS>([&](auto sl) S2_INLINE { beside(sl); });
+      return;
     }
     uint32_t ks = k_read + stage, vs = v_read + stage;
     float mc_use = on_s ? mc : __builtin_inff();  // (not mine: its scores are zeros, its probabilities 0)
@@ -195,12 +200,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
         }
       }
       // (a lane's own scores are enough to see whether any of a query's is above its maximum)
-      if (__any(mx > m_run)) {
-        const float m_new = fmaxf(m_run, max_halves(mx));
-        mc = m_new == kNegInf ? 0.f : m_new * cl;
-        alpha = m_new > m_run ? fast_exp2(m_run * cl - mc) : 1.f;  // (see cache_attn_kernel.hip)
+      if (__any(mx - m_run > tau)) {  // (-inf minus itself is not a number, and no reason to move)
+        const float top = max_halves(mx);
+        const bool moves = top - m_run > tau;
+        alpha = moves ? fast_exp2(m_run * cl - top * cl) : 1.f;  // (what another query's maximum does leaves this one's result as it is)
+        m_run = moves ? top : m_run;
+        mc = m_run == kNegInf ? 0.f : m_run * cl;
         l_run *= alpha;
-        m_run = m_new;
         scaled = true;
       }
     } else {
@@ -208,17 +214,18 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
     }
   };
 
-  {
+  // (a wavefront without a query fetches its rows of K and V for the others and nothing else)
+  auto trips = [&](auto busy) S2_INLINE {
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
     constexpr int kPut = NS / KO;  // slots to an operand that is put
     ChunkUnit prev{}, cur, next;
     bool more = walk.next(0, cur), had = false;
     load(kK, cur, kr);
-    static_for<KO>([&](auto kk) S2_INLINE { put(kr, decltype(kk)::value, write); });
+    static_for<KO>([&](auto kk) S2_INLINE { put(kr, lane >> 4, decltype(kk)::value, write); });
     // (no V before the first: zeros)
     static_for<KO>([&](auto kk) S2_INLINE {
-      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(write + kV0 + 2 * Rows::feature(decltype(kk)::value, lane >> 4)) = u32x4{};
+      *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(write + kV0 + 2 * Rows::feature(decltype(kk)::value, 0)) = u32x4{};
     });
     bool more_next = more && walk.next(1, next);
     if (!more) next = cur;
@@ -229,20 +236,21 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
       const uint32_t to = ((t + 1) & 1) * (uint32_t)Tile::kBytes;
       ChunkUnit then{};
       const bool more_then = more_next && walk.next(t + 2, then);
+      const int g = lane_now() >> 4;
       if (tid < 2) sh_v_odd[(t + 3) & 3][tid] = 0;  // (read a trip ago, written a trip from now)
-      half_step(first, t, cur.on(0), prev.on(1), prev.on(0), cur.some(), prev.some(), s0, s1, pb1, pb0, [&](auto slc) S2_INLINE {
+      half_step(busy, first, t, cur.on(0), prev.on(1), prev.on(0), cur.some(), prev.some(), s0, s1, pb1, pb0, [&](auto slc) S2_INLINE {
         constexpr int sl = decltype(slc)::value;
-        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(kr, sl / kPut, write + to);
+        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(kr, g, sl / kPut, write + to);
         if constexpr (sl == NS - 1) load(kK, then, kr);
       });
-      half_step(second, t, cur.on(1), cur.on(0), prev.on(1), cur.some(), prev.some(), s1, s0, pb0, pb1, [&](auto slc) S2_INLINE {
+      half_step(busy, second, t, cur.on(1), cur.on(0), prev.on(1), cur.some(), prev.some(), s1, s0, pb0, pb1, [&](auto slc) S2_INLINE {
         constexpr int sl = decltype(slc)::value;
-        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(vr, sl / kPut, write + kV0 + to);
+        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(vr, g, sl / kPut, write + kV0 + to);
         if constexpr (sl == NS - 1) load(kV, next, vr);
       });
       if (cur.some()) {  // whether my rows of its V are all finite
         u32x4 v[KO];
-        static_for<KO>([&](auto kk) S2_INLINE { v[decltype(kk)::value] = lds_read16(write + kV0 + to + D / 2 * (lane_now() >> 4), 16 * decltype(kk)::value); });
+        static_for<KO>([&](auto kk) S2_INLINE { v[decltype(kk)::value] = lds_read16(write + kV0 + to, 2 * Rows::feature(decltype(kk)::value, 0)); });
         if (odd_bits(v)) sh_v_odd[(t + 1) & 3][wave >> 1] = 1;
       }
       barrier();
@@ -253,7 +261,11 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
       cur = next;
       next = then;
     }
-  }
+  };
+  if (__any(q0.there))
+    trips(std::true_type{});
+  else
+    trips(std::false_type{});
   const CacheChunkParams& pe = chunk_params();
   if (pe.missing && tid == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 

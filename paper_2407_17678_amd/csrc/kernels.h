@@ -237,6 +237,19 @@ struct QkRopeParams {
   FastDiv by_groups, by_seqlen;
 };
 
+// What a look-up of the blocks that a tile of a chunk attends takes of the parameters below, side by side: 32 words, in two loads.
+struct ChunkLookUp {
+  const int32_t* table;
+  int64_t page, scale_page;
+  const int32_t* row_ptr;
+  const int32_t* col_idx;
+  int32_t* missing;
+  int tok, scale_tok, max_blocks, num_pages, block_shift, heads, num_splits;
+  int local_blocks, stride, window_blocks, dense, head_index_base, num_blocks, none;
+  FastDiv by_splits, by_stride;
+  int rest[2];
+};
+static_assert(sizeof(ChunkLookUp) == 128, "two loads of 16 words");
 // Attention of a chunk of new tokens over a paged cache (s2_chunk_args).
 struct CacheChunkParams {
   CacheRef c;
@@ -260,6 +273,7 @@ struct CacheChunkParams {
   int tile_shift, seq_tiles, num_tiles;
   bool packed;
   FastDiv by_heads, by_splits, by_stride, by_tiles;  // set by launch_cache_chunk
+  ChunkLookUp look_up;                               // likewise
 };
 
 // Each returns the hipError_t of the launch (hipGetLastError after the launch).
