@@ -118,6 +118,7 @@ struct ChunkUnit {
   int rows;                  // tokens to read of it
   int flags;
   __device__ __forceinline__ bool on(int half) const { return flags >> half & 1; }  // some query of the wavefront attends some token of the half
+  __device__ __forceinline__ bool there() const { return flags >> 3 & 1; }          // (there is no unit of no tokens)
   __device__ __forceinline__ bool some() const { return flags >> 2 & 1; }           // some query of the workgroup may not attend some token
 };
 
@@ -271,19 +272,20 @@ struct ChunkWalk {
     return true;
   }
 
-  // Unit n, the next one with a token to read (SMALL: the units of a look-up are NB lanes apart).
-  __device__ __forceinline__ bool next(int n, ChunkUnit& w) {
+  // Whether a unit with a token to read is looked up.
+  __device__ __forceinline__ bool find() {
     while (live == 0)
-      if (!look_up()) {
-        w.off = w.scale_off = w.rows = w.flags = 0;  // (no rows: loading it fetches nothing)
-        return false;
-      }
+      if (!look_up()) return false;
+    return true;
+  }
+  // The next one of those, as unit n (SMALL: the units of a look-up are NB lanes apart).
+  __device__ __forceinline__ void take(int n, ChunkUnit& w) {
     const int i = __builtin_ctzll(live);
     live &= live - 1;
     const int mine = lane_now() - i;
     if (mine >= 0 && mine < NB)
       *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(ring + 8 * ((n & 3) * NB + mine)) = u32x2{(uint32_t)info, (uint32_t)at};
-    w.flags = (int)(on[0] >> i & 1) | (int)(on[1] >> i & 1) << 1 | (int)(some >> i & 1) << 2;
+    w.flags = (int)(on[0] >> i & 1) | (int)(on[1] >> i & 1) << 1 | (int)(some >> i & 1) << 2 | 8;
     const int own = SMALL ? i + piece : i;
     auto both = [&](const uint32_t (&x)[2]) __attribute__((always_inline)) {
       return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x[1], own) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x[0], own));
@@ -291,7 +293,14 @@ struct ChunkWalk {
     w.off = both(off);
     w.scale_off = both(scale_off);
     w.rows = __builtin_amdgcn_readlane(info, own) & 255;
-    return true;
+  }
+  __device__ __forceinline__ bool next(int n, ChunkUnit& w) {
+    if (find()) {
+      take(n, w);
+      return true;
+    }
+    w = ChunkUnit{};  // (no rows: loading it fetches nothing)
+    return false;
   }
 };
 

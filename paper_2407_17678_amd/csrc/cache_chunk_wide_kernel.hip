@@ -28,7 +28,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
   constexpr int W = 4, MW = 32, KK = D / 16, DT = D / 32, KO = D / 32;  // KO: operands of eight features to a lane's part of a row
   constexpr int NS = 2 * KK;                                            // slots: KK of the scores, 2 * DT of the product with V
   constexpr int RB = Tile::kStride * 2;
-  constexpr int kLead = 3, kRing = kLead + 1;  // fragments are asked for so many slots ahead
+  constexpr int kLead = D == 128 ? 5 : 3, kRing = kLead + 1;  // fragments are asked for so many slots ahead
   constexpr int RS = D + 4;                    // floats to a row where results are turned
   static_assert(2 * DT == KK && W * MW * RS * 4 <= 4 * Tile::kBytes, "the wavefronts' sums fit where K and V were");
 
@@ -62,7 +62,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
   // what my query attends of half H of unit u, bits
   auto seen_of = [&](int u, int H) S2_INLINE {
     const ChunkQuery q = chunk_query(chunk_params(), sh_tile, sh_scope.r, MW * wave + (lane_now() & 31) - sh_tile.skipped);
-    return (uint32_t)(chunk_seen<SMALL>(walk, u, q.rel, q.pos) >> (32 * H));
+    return chunk_seen<SMALL>(walk, u, q.rel, q.pos) >> (32 * H);
   };
 
   f32x16 acc[DT];
@@ -77,13 +77,16 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
   const uint32_t k_read = lds_addr(sh_kv) + l32 * RB + 16 * half, v_read = lds_addr(sh_kv) + 2 * Tile::tr_base(lane);
   constexpr int kV0 = 2 * Tile::kBytes;
 
+  // (kept in registers: left to itself the compiler fetches them where they are used, and waits for the LDS as well)
+  const uint8_t *k_pool = p.c.k, *v_pool = p.c.v, *k_scales = p.c.ks, *v_scales = p.c.vs;
+  int tok = p.c.tok, scale_tok = p.c.scale_tok;
+  asm volatile("" : "+s"(k_pool), "+s"(v_pool), "+s"(tok));
+  if constexpr (Rows::kScaled) asm volatile("" : "+s"(k_scales), "+s"(v_scales), "+s"(scale_tok));
+  const int my_row = (SMALL ? 0 : 16 * wave) + (lane & 15), lane_at = my_row * tok + Rows::kLoadBytes * (lane >> 4), scale_at = my_row * scale_tok;
   typename Rows::Part kr, vr;
   auto load = [&](auto is_v, const ChunkUnit& w, typename Rows::Part& to) S2_INLINE {
     constexpr bool V = decltype(is_v)::value;
-    const uint8_t* const at = (V ? p.c.v : p.c.k) + w.off;
-    const uint8_t* const scale_at = Rows::kScaled ? (V ? p.c.vs : p.c.ks) + w.scale_off : nullptr;
-    const int ln = lane_now();
-    Rows::load(to, at, scale_at, w.rows, p.c.tok, p.c.scale_tok, (SMALL ? 0 : 16 * wave) + (ln & 15), ln >> 4);
+    Rows::load_at(to, (V ? v_pool : k_pool) + w.off, Rows::kScaled ? (V ? v_scales : k_scales) + w.scale_off : nullptr, w.rows, tok, scale_tok, lane_at, scale_at);
   };
   constexpr std::false_type kK{};
   constexpr std::true_type kV{};
@@ -103,63 +106,40 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
   // the same as operands: rounded to bf16, as in the forward of a whole sequence: off by up to 2^-8 of a probability
   u32x4 pb0[2] = {u32x4{}, u32x4{}}, pb1[2] = {u32x4{}, u32x4{}};
 
-  // Half step H of trip t: scores of half H of unit t (sn), probabilities of the half before it (sc, pc), the product of half H of unit t - 1 (pp) with V.  on_n, on_s, on_p:
-  // whether these are mine; some_n, some_p: whether a token of their units is not attended by some query.
-  auto half_step = [&](auto busy, auto hc, int t, bool on_n, bool on_s, bool on_p, bool some_n, bool some_p, f32x16& sn, f32x16& sc, u32x4 (&pc)[2], u32x4 (&pp)[2],
+  // The fragments of a trip, in one ring through both of its half steps: of half f / NS the rows of K, then those of V, transposed.
+  bf16x8 fr[kRing];
+  uint32_t ks = 0, vs = 0;
+  auto frag_load = [&](auto fc) S2_INLINE {
+    constexpr int f = decltype(fc)::value % NS, H = decltype(fc)::value / NS;
+    if constexpr (f < KK)
+      fr[decltype(fc)::value % kRing] = __builtin_bit_cast(bf16x8, lds_read16(ks, 32 * H * RB + 32 * f));
+    else
+      fr[decltype(fc)::value % kRing] = __builtin_bit_cast(bf16x8, lds_read_tr(vs, kV0 + (32 * H + 16 * ((f - KK) / DT)) * RB + 64 * ((f - KK) % DT), RB));
+  };
+  static_assert(kLead <= KK, "of the second half no V is asked for in the first");
+  auto first_frags = [&]() S2_INLINE { static_for<kLead>([&](auto fc) S2_INLINE { frag_load(fc); }); };
+
+  // Half step H of trip t: scores of half H of unit t (sn), probabilities of the half before it (sc, pc), the product of half H of unit t - 1 (pp) with V.  on_n, on_s:
+  // whether the first two are mine; some_n: whether a token of the unit is not attended by some query.  Where nothing is mine it all runs the same, with zeros: a
+  // branch around it has the compiler move the accumulators between registers.
+  auto half_step = [&](auto hc, int t, bool on_n, bool on_s, bool some_n, f32x16& sn, f32x16& sc, u32x4 (&pc)[2], u32x4 (&pp)[2],
                        auto&& beside) S2_INLINE {
     constexpr int H = decltype(hc)::value;
-    const uint32_t stage = (t & 1) * (uint32_t)Tile::kBytes;
-    if (some_p && sh_v_odd[t & 3][H]) {  // (the same for all wavefronts)
-      // What a query does not attend stays out of its result whatever it holds, but 0 times an infinity or NaN is none: such values of V are added to the sums of the
-      // queries that attend them here, and taken out of V.
-      const uint32_t seen = on_p ? seen_of(t - 1, H) : 0;
-#pragma unroll 1
-      for (int i = 0; decltype(busy)::value && i < 32; ++i) {
-        const uint32_t row = lds_addr(sh_kv) + kV0 + stage + (32 * H + i) * RB + 8 * half;
-#pragma unroll
-        for (int dt = 0; dt < DT; ++dt)
-#pragma unroll
-          for (int g = 0; g < 4; ++g) {
-            const u32x2 v = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)(row + 64 * dt + 16 * g);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const uint32_t bits = e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
-              acc[dt][4 * g + e] += (seen >> i & 1) && (bits & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, bits) : 0.f;
-            }
-          }
-      }
-      barrier();
-      clean_words(reinterpret_cast<uint32_t*>(sh_kv[2 + (t & 1)]) + (32 * H + 8 * wave) * RB / 4, 8 * RB / 4, lane);
-      barrier();
-    }
-    if constexpr (!decltype(busy)::value) {
-      static_for<NS>([&](auto sl) S2_INLINE { beside(sl); });
-      return;
-    }
-    uint32_t ks = k_read + stage, vs = v_read + stage;
     float mc_use = on_s ? mc : __builtin_inff();  // (not mine: its scores are zeros, its probabilities 0)
-    asm volatile("" : "+v"(ks), "+v"(vs), "+v"(mc_use));
-    bf16x8 fr[kRing];
-    auto frag_load = [&](auto fc) S2_INLINE {
-      constexpr int f = decltype(fc)::value;
-      if constexpr (f < KK)
-        fr[f % kRing] = __builtin_bit_cast(bf16x8, lds_read16(ks, 32 * H * RB + 32 * f));
-      else
-        fr[f % kRing] = __builtin_bit_cast(bf16x8, lds_read_tr(vs, kV0 + (32 * H + 16 * ((f - KK) / DT)) * RB + 64 * ((f - KK) % DT), RB));
-    };
+    asm volatile("" : "+v"(mc_use));
     float mx = kNegInf;
     // 16 scores in three stages - scale and shift, exponential, sum and pack - each a slot behind the one before it
     constexpr auto upto = [](int sl) { return std::max(0, std::min(16, (16 * (sl + 1) + NS - 3) / (NS - 2))); };
     static_assert(upto(NS - 3) >= 16, "packed in time");
-    static_for<kLead>([&](auto fc) S2_INLINE { frag_load(fc); });
+    if constexpr (H == 0) first_frags();
     S2_FENCE();
     static_for<NS>([&](auto slc) S2_INLINE {
       constexpr int sl = decltype(slc)::value;
-      if constexpr (sl + kLead < NS) frag_load(std::integral_constant<int, sl + kLead>{});
+      if constexpr (H * NS + sl + kLead < 2 * NS) frag_load(std::integral_constant<int, H * NS + sl + kLead>{});
       if constexpr (sl < KK)
-        sn = mfma32(fr[sl % kRing], qf[sl], sl == 0 ? f32x16{} : sn);
+        sn = mfma32(fr[(H * NS + sl) % kRing], qf[sl], sl == 0 ? f32x16{} : sn);
       else
-        acc[(sl - KK) % DT] = mfma32(fr[sl % kRing], __builtin_bit_cast(bf16x8, pp[(sl - KK) / DT]), acc[(sl - KK) % DT]);
+        acc[(sl - KK) % DT] = mfma32(fr[(H * NS + sl) % kRing], __builtin_bit_cast(bf16x8, pp[(sl - KK) / DT]), acc[(sl - KK) % DT]);
 #pragma unroll
       for (int e = upto(sl - 1); e < upto(sl); ++e) sc[e] = __builtin_fmaf(sc[e], cl, -mc_use);
 #pragma unroll
@@ -167,7 +147,10 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
 #pragma unroll
       for (int e = upto(sl - 3); e < upto(sl - 2); ++e) {
         l_run += sc[e];
-        if (e & 1) pc[e >> 3][(e & 7) >> 1] = pack2(sc[e - 1], sc[e]);
+        if (e & 1) {
+          pc[e >> 3][(e & 7) >> 1] = pack2(sc[e - 1], sc[e]);
+          asm volatile("" : "+v"(pc[e >> 3][(e & 7) >> 1]));  // (here, not where it is used, half a trip on)
+        }
       }
       // maximum of the new scores, once their products are done
       constexpr int M0 = KK + 2, kMax = D == 128 ? 4 : 8;
@@ -191,7 +174,7 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
     }
     if (on_n) {
       if (some_n) {
-        const uint32_t seen = seen_of(t, H) >> (4 * (lane_now() >> 5));
+        const uint32_t seen = (uint32_t)seen_of(t, H) >> (4 * (lane_now() >> 5));
         mx = kNegInf;
 #pragma unroll
         for (int r = 0; r < 16; ++r) {
@@ -214,39 +197,64 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
     }
   };
 
-  // (a wavefront without a query fetches its rows of K and V for the others and nothing else)
-  auto trips = [&](auto busy) S2_INLINE {
+  {
     constexpr std::integral_constant<int, 0> first{};
     constexpr std::integral_constant<int, 1> second{};
-    constexpr int kPut = NS / KO;  // slots to an operand that is put
-    ChunkUnit prev{}, cur, next;
-    bool more = walk.next(0, cur), had = false;
+    ChunkUnit prev{}, cur{}, next{};
+    // (the second unit is one of the first look-up's or none: an empty one among the others changes nothing, and one place less looks up)
+    bool more = walk.find();  // whether there may be more units
+    if (more) walk.take(0, cur);
+    if (more && walk.live != 0) walk.take(1, next);
     load(kK, cur, kr);
     static_for<KO>([&](auto kk) S2_INLINE { put(kr, lane >> 4, decltype(kk)::value, write); });
-    // (no V before the first: zeros)
-    static_for<KO>([&](auto kk) S2_INLINE {
+    static_for<KO>([&](auto kk) S2_INLINE {  // (no V before the first: zeros, which a probability of 0 leaves)
       *(__attribute__((address_space(3))) u32x4*)(uintptr_t)(write + kV0 + 2 * Rows::feature(decltype(kk)::value, 0)) = u32x4{};
     });
-    bool more_next = more && walk.next(1, next);
-    if (!more) next = cur;
     load(kK, next, kr);
     load(kV, cur, vr);
     barrier();
-    for (int t = 0; more || had; ++t) {
+    for (int t = 0;; ++t) {
       const uint32_t to = ((t + 1) & 1) * (uint32_t)Tile::kBytes;
-      ChunkUnit then{};
-      const bool more_then = more_next && walk.next(t + 2, then);
+      ChunkUnit then;
+      more = more && walk.next(t + 2, then);
+      if (!more) then = ChunkUnit{};
       const int g = lane_now() >> 4;
       if (tid < 2) sh_v_odd[(t + 3) & 3][tid] = 0;  // (read a trip ago, written a trip from now)
-      half_step(busy, first, t, cur.on(0), prev.on(1), prev.on(0), cur.some(), prev.some(), s0, s1, pb1, pb0, [&](auto slc) S2_INLINE {
+      if (prev.some() && (sh_v_odd[t & 3][0] | sh_v_odd[t & 3][1])) {  // (the same for all wavefronts)
+        // What a query does not attend stays out of its result whatever it holds, but 0 times an infinity or NaN is none: such values of V are added to the sums of
+        // the queries that attend them here, and taken out of V.
+        const uint64_t seen = seen_of(t - 1, 0);
+#pragma unroll 1
+        for (int i = 0; i < 64; ++i) {
+          const uint32_t row = lds_addr(sh_kv) + kV0 + (t & 1) * (uint32_t)Tile::kBytes + i * RB + 8 * half;
+#pragma unroll
+          for (int dt = 0; dt < DT; ++dt)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const u32x2 v = *(const __attribute__((address_space(3))) u32x2*)(uintptr_t)(row + 64 * dt + 16 * q);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) {
+                const uint32_t bits = e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16;
+                acc[dt][4 * q + e] += (seen >> i & 1) && (bits & 0x7f800000u) == 0x7f800000u ? __builtin_bit_cast(float, bits) : 0.f;
+              }
+            }
+        }
+        barrier();
+        clean_words(reinterpret_cast<uint32_t*>(sh_kv[2 + (t & 1)]) + 16 * wave * RB / 4, 16 * RB / 4, lane);
+        barrier();
+      }
+      ks = k_read + (t & 1) * (uint32_t)Tile::kBytes;
+      vs = v_read + (t & 1) * (uint32_t)Tile::kBytes;
+      asm volatile("" : "+v"(ks), "+v"(vs));
+      half_step(first, t, cur.on(0), prev.on(1), cur.some(), s0, s1, pb1, pb0, [&](auto slc) S2_INLINE {
         constexpr int sl = decltype(slc)::value;
-        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(kr, g, sl / kPut, write + to);
-        if constexpr (sl == NS - 1) load(kK, then, kr);
+        if constexpr (sl < KO) put(kr, g, sl, write + to);
+        if constexpr (sl == KO) load(kK, then, kr);
       });
-      half_step(busy, second, t, cur.on(1), cur.on(0), prev.on(1), cur.some(), prev.some(), s1, s0, pb0, pb1, [&](auto slc) S2_INLINE {
+      half_step(second, t, cur.on(1), cur.on(0), cur.some(), s1, s0, pb0, pb1, [&](auto slc) S2_INLINE {
         constexpr int sl = decltype(slc)::value;
-        if constexpr (sl % kPut == 0 && sl / kPut < KO) put(vr, g, sl / kPut, write + kV0 + to);
-        if constexpr (sl == NS - 1) load(kV, next, vr);
+        if constexpr (sl < KO) put(vr, g, sl, write + kV0 + to);
+        if constexpr (sl == KO) load(kV, next, vr);
       });
       if (cur.some()) {  // whether my rows of its V are all finite
         u32x4 v[KO];
@@ -254,18 +262,13 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
         if (odd_bits(v)) sh_v_odd[(t + 1) & 3][wave >> 1] = 1;
       }
       barrier();
-      had = more;
-      more = more_next;
-      more_next = more_then;
+      // (the last unit's probabilities meet its V in the trip after its own)
+      if (!more && !cur.there() && !next.there()) break;
       prev = cur;
       cur = next;
       next = then;
     }
-  };
-  if (__any(q0.there))
-    trips(std::true_type{});
-  else
-    trips(std::false_type{});
+  }
   const CacheChunkParams& pe = chunk_params();
   if (pe.missing && tid == 0 && walk.n_missing > 0) atomicAdd(pe.missing, walk.n_missing);
 

@@ -63,23 +63,27 @@ struct CacheRows {
 
   // rows 0 .. 15 from `at`, of which `rows` exist: the others read as zeros and are not fetched
   __device__ static __forceinline__ void load(Part& p, const uint8_t* at, const uint8_t* scales_at, int rows, int tok, int scale_tok, int r, int g) {
+    load_at(p, at, scales_at, rows, tok, scale_tok, r * tok + kLoadBytes * g, r * scale_tok);
+  }
+  // the same, a lane's bytes beginning at lane_at and its scales at scale_at
+  __device__ static __forceinline__ void load_at(Part& p, const uint8_t* at, const uint8_t* scales_at, int rows, int tok, int scale_tok, int lane_at, int scale_at) {
     const auto buf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(at), 0, rows * tok, 0x00020000);
 #pragma unroll
     for (int j = 0; j < kLoads; ++j) {
       if constexpr (kLoadBytes == 16) {
-        const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, r * tok + 64 * j + 16 * g, 0, 0));
+        const u32x4 w = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(buf, lane_at + 64 * j, 0, 0));
 #pragma unroll
         for (int e = 0; e < 4; ++e) p.x[4 * j + e] = w[e];
       } else {
-        const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buf, r * tok + 8 * g, 0, 0));
+        const u32x2 w = __builtin_bit_cast(u32x2, __builtin_amdgcn_raw_buffer_load_b64(buf, lane_at, 0, 0));
         p.x[0] = w[0];
         p.x[1] = w[1];
       }
     }
     if constexpr (kScaled) {
       const auto sbuf = __builtin_amdgcn_make_buffer_rsrc(const_cast<uint8_t*>(scales_at), 0, rows * scale_tok, 0x00020000);
-      p.scales = D == 128 ? __builtin_amdgcn_raw_buffer_load_b32(sbuf, r * scale_tok, 0, 0)
-                          : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(sbuf, r * scale_tok, 0, 0);
+      p.scales = D == 128 ? __builtin_amdgcn_raw_buffer_load_b32(sbuf, scale_at, 0, 0)
+                          : (uint32_t)__builtin_amdgcn_raw_buffer_load_b16(sbuf, scale_at, 0, 0);
     }
   }
 
