@@ -163,7 +163,7 @@ struct ChunkWalk {
   static constexpr int NB = SMALL ? 4 : 1, kTokens = 64 / NB, kUnits = 64 / NB;
   static constexpr int kRing = 4 * NB;  // pieces in LDS (a wavefront's own)
   const ChunkScope& scope;
-  int piece;
+  int wave, first, step;             // whose queries and pieces these are; unit `first` of the split, and every step-th
   uint32_t ring;                     // where the pieces lie
   int n_missing = 0;
   int turn = -1, u_now = 0, u_end = 0;
@@ -172,8 +172,9 @@ struct ChunkWalk {
   uint64_t live = 0, some = 0, on[2] = {0, 0};
 
   // (scope_: in LDS, filled for the workgroup; ring_: room for kRing pairs of words there; q0, q1: a lane's first query and its last)
-  __device__ __forceinline__ ChunkWalk(ChunkScope& scope_, int n_rows, int piece_, const void* ring_, const ChunkQuery& q0, const ChunkQuery& q1)
-      : scope(scope_), piece(piece_), ring(lds_addr(ring_)) {
+  __device__ __forceinline__ ChunkWalk(ChunkScope& scope_, int n_rows, int wave_, const void* ring_, const ChunkQuery& q0, const ChunkQuery& q1, int first_ = 0,
+                                       int step_ = 1)
+      : scope(scope_), wave(wave_), first(first_), step(step_), ring(lds_addr(ring_)) {
     if (n_rows == 0) turn = 1 << 20;  // (nothing to look up)
     int my_bits = 0;
 #pragma unroll 1
@@ -182,8 +183,8 @@ struct ChunkWalk {
 #pragma unroll
     for (int i = 1; i < 64; i *= 2) last = max(last, __shfl_xor(last, i, 64));
     // (read again by the wavefront itself)
-    scope_.bits[piece] = my_bits;
-    scope_.last[piece] = last;
+    scope_.bits[wave] = my_bits;
+    scope_.last[wave] = last;
   }
 
   __device__ static uint64_t of_units(uint64_t pieces) {
@@ -212,12 +213,12 @@ struct ChunkWalk {
       rb = blocks_of(p, s, turn);
       const int units = (int)((((int64_t)rb.count << sh) + 63) >> 6);
       const int even = units / p.by_splits, rest = units - even * p.num_splits;
-      u_now = even * s.split + rest * s.split / p.by_splits;
+      u_now = even * s.split + rest * s.split / p.by_splits + first;
       u_end = even * (s.split + 1) + rest * (s.split + 1) / p.by_splits;
     }
     const int lane = lane_now();
-    const int u = u_now + lane / NB, l = 64 * u + 16 * (lane % NB), n = l >> sh, skip = l & (S - 1);
-    u_now += kUnits;
+    const int u = u_now + step * (lane / NB), l = 64 * u + 16 * (lane % NB), n = l >> sh, skip = l & (S - 1);
+    u_now += step * kUnits;
     const bool inside = u < u_end && n < rb.count;
     const int blk = inside ? rb.block_of_lane(n) : 0;
     at = blk * S + skip;
@@ -259,8 +260,8 @@ struct ChunkWalk {
     const int all = (1 << r.n_rows) - 1;
     live = of_units(__ballot(rows > 0));
     some = of_units(__ballot(rows < kTokens || bits != all || at + rows - 1 > r.lo));
-    const bool mine = (bits & scope_word(scope.bits[piece])) != 0;
-    const int my_last = scope_word(scope.last[piece]);
+    const bool mine = (bits & scope_word(scope.bits[wave])) != 0;
+    const int my_last = scope_word(scope.last[wave]);
     if (SMALL) {
       const uint64_t x = __ballot(mine && rows > 0 && at <= my_last);
       on[0] = (x | x >> 1) & 0x1111111111111111ull;
@@ -278,21 +279,26 @@ struct ChunkWalk {
       if (!look_up()) return false;
     return true;
   }
-  // The next one of those, as unit n (SMALL: the units of a look-up are NB lanes apart).
-  __device__ __forceinline__ void take(int n, ChunkUnit& w) {
+  // The next one of those, as unit n (SMALL: the units of a look-up are NB lanes apart): N pieces of 16 tokens from `piece` on.
+  __device__ __forceinline__ void take(int n, ChunkUnit& w) { take(n, wave, &w); }
+  template <int N = 1>
+  __device__ __forceinline__ void take(int n, int piece, ChunkUnit* w) {
     const int i = __builtin_ctzll(live);
     live &= live - 1;
     const int mine = lane_now() - i;
     if (mine >= 0 && mine < NB)
       *(__attribute__((address_space(3))) u32x2*)(uintptr_t)(ring + 8 * ((n & 3) * NB + mine)) = u32x2{(uint32_t)info, (uint32_t)at};
-    w.flags = (int)(on[0] >> i & 1) | (int)(on[1] >> i & 1) << 1 | (int)(some >> i & 1) << 2 | 8;
-    const int own = SMALL ? i + piece : i;
-    auto both = [&](const uint32_t (&x)[2]) __attribute__((always_inline)) {
-      return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x[1], own) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x[0], own));
-    };
-    w.off = both(off);
-    w.scale_off = both(scale_off);
-    w.rows = __builtin_amdgcn_readlane(info, own) & 255;
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      const int own = SMALL ? i + piece + t : i;
+      auto both = [&](const uint32_t (&x)[2]) __attribute__((always_inline)) {
+        return (int64_t)((uint64_t)(uint32_t)__builtin_amdgcn_readlane((int)x[1], own) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)x[0], own));
+      };
+      w[t].flags = (int)(on[0] >> i & 1) | (int)(on[1] >> i & 1) << 1 | (int)(some >> i & 1) << 2 | 8;
+      w[t].off = both(off);
+      w[t].scale_off = both(scale_off);
+      w[t].rows = __builtin_amdgcn_readlane(info, own) & 255;
+    }
   }
   __device__ __forceinline__ bool next(int n, ChunkUnit& w) {
     if (find()) {
