@@ -995,9 +995,15 @@ int tree_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_pag
   return attend_cache(lp, layout, c, p, scale, a->num_splits, workspace, workspace_bytes, stream);
 }
 
-// The most splits that the library takes for a chunk: two workgroups to a compute unit, two units of 64 tokens to each.
-int most_chunk_splits(int64_t groups, int64_t max_len) {
-  return (int)std::max<int64_t>(1, std::min<int64_t>({64, (512 + groups - 1) / groups, (max_len + 127) / 128}));
+// The most splits that the library takes for a chunk: units of 64 tokens go two to a split, and the workgroups of the tiles that sequences fill a workgroup to a
+// compute unit, or two of the kernel for 33 to 64 rows, whose wavefronts wait for each other.  bf16, head_dim 128, 44 units for a query, us by splits:
+//   256 rows, 32 heads (64 tiles)    1: 73  2: 49  4: 36  6: 39  8: 38  16: 52      4 x 256 rows, 32 heads (256)   1: 76  2: 79  4: 89
+//   16 rows, 32 heads                1: 30  4: 17  8: 13.9  12: 15.1  16: 15.3      48 rows, 32 heads              1: 74  8: 21.4  16: 21.0  24: 21.7
+//   4 x 48 rows, 32 heads            1: 74  2: 48  4: 37  6: 36  8: 41              and 12 units, 16 rows, 8 heads 1: 12.6  4: 11.8  6: 10.7  12: 11.2
+int most_chunk_splits(const s2::CacheChunkParams& p, int64_t max_len) {
+  const int64_t rows = (int64_t)1 << p.tile_shift, fill = p.max_new > 32 && p.max_new <= s2::kChunkFew ? 512 : 256;
+  const int64_t groups = p.heads * std::min((p.max_new + rows - 1) / rows * p.nseq, p.num_rows / rows + p.nseq);
+  return (int)std::max<int64_t>(1, std::min<int64_t>({64, (fill + groups / 2) / groups, (max_len + 127) / 128}));
 }
 
 // (the fields that decide the launch's size)
@@ -1037,7 +1043,7 @@ int chunk_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_pa
   if (groups > s2::kMostGroups) return S2_ERR_SHAPE;
   const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / c->block_size, nullptr, 0);
   const int64_t units = (blocks * c->block_size + 63) / 64;
-  int splits = a->num_splits > 0 ? a->num_splits : (int)std::max<int64_t>(1, std::min<int64_t>(most_chunk_splits(groups, max_len), units / 2));
+  int splits = a->num_splits > 0 ? a->num_splits : (int)std::max<int64_t>(1, std::min<int64_t>(most_chunk_splits(p, max_len), (units + 1) / 2));
   auto bytes = [&](int n) { return n == 1 ? 0 : s2_attn_chunk_workspace_bytes(c->nseq, c->heads, a->max_new, a->num_rows, c->head_dim, max_len, n); };
   // (a smaller workspace is for fewer splits, where the caller has not asked for a number)
   while (a->num_splits == 0 && splits > 1 && (!workspace || bytes(splits) > workspace_bytes)) --splits;
@@ -1189,7 +1195,10 @@ int s2_attn_chunk_paged_layout(const s2_layout* layout, const s2_paged_cache* c,
 size_t s2_attn_chunk_workspace_bytes(int32_t nseq, int32_t heads, int32_t max_new, int32_t num_rows, int32_t head_dim, int32_t max_len, int32_t num_splits) {
   if (nseq < 1 || heads < 1 || max_new < 1 || num_rows < 1 || head_dim < 1) return 0;
   s2::CacheChunkParams p = chunk_sizes(nseq, heads, max_new, num_rows);
-  if (num_splits <= 0) num_splits = most_chunk_splits(s2::chunk_tiles(p) * heads, max_len);
+  if (num_splits <= 0) {
+    s2::chunk_tiles(p);
+    num_splits = most_chunk_splits(p, max_len);
+  }
   if (num_splits == 1) return 0;
   const size_t items = (size_t)nseq * heads * p.max_new * num_splits;
   return ((items * (head_dim + 2) * sizeof(float) + 255) / 256) * 256;

@@ -15,7 +15,8 @@ struct ChunkTileAt {
   int64_t pos, start;
 };
 // Tiles of up to kChunkFew rows begin at a sequence's first new token, larger ones at multiples of their rows in its positions, so that a tile lies in as few
-// block rows as it can.  Either every sequence has as many as the longest may need, or (packed) there are those of the rows that there are: sequence
+// block rows as it can.  Either every sequence has as many as the longest may need (the last ones, which few need, behind all others: between them they left
+// compute units idle that got two of them, 4 sequences of 256 rows with 1024 + 2048 tokens each to attend 97 us, so 76), or (packed) there are those of the rows that there are: sequence
 // b, whose rows begin at lo, has the tiles from lo / rows + 2 b on, as many at least as it needs, and the last one that begins at or before a tile is found 64
 // sequences at a time.
 // (a sequence's rows in the tensors)
@@ -27,8 +28,9 @@ __device__ __forceinline__ ChunkTileAt chunk_tile_at(const CacheChunkParams& p, 
   ChunkTileAt x;
   int tile, lo, hi, start;
   if (!p.packed) {
-    x.b = t / p.by_tiles;
-    tile = t - x.b * p.seq_tiles;
+    const int begun = p.seq_tiles - 1, last = t - p.nseq * begun;
+    x.b = last < 0 ? t / p.by_tiles : last;
+    tile = last < 0 ? t - x.b * begun : begun;
     lo = load_const<int32_t>(p.cu + x.b);
     hi = load_const<int32_t>(p.cu + x.b + 1);
     start = load_const<int32_t>(p.start + x.b);

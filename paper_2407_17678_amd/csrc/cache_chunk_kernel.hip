@@ -441,6 +441,14 @@ __global__ __launch_bounds__(256) void cache_chunk_merge_kernel(const CacheChunk
   const float* const ml = p.part_ml + item * n * 2;
   const f32x4* const part = reinterpret_cast<const f32x4*>(p.part_acc) + item * n * LPR + c;
   const float ms = lane < n ? ml[2 * lane] : kNegInf, ls = lane < n ? ml[2 * lane + 1] : 0.f;
+  // (kEach loads on their way at a time, the first ones along with the statistics)
+  constexpr int kEach = 4;
+  f32x4 y[kEach];
+  auto load = [&](int s0) __attribute__((always_inline)) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) y[k] = part[(int64_t)min(s0 + k * NG + g, n - 1) * LPR];
+  };
+  load(0);
   float m = ms;
   m = fmaxf(m, of_neighbour<1>(m));
   m = fmaxf(m, of_neighbour<2>(m));
@@ -454,16 +462,21 @@ __global__ __launch_bounds__(256) void cache_chunk_merge_kernel(const CacheChunk
   l += of_neighbour<8>(l);
   l = sum_halves(sum_rows(l));
   f32x4 a = f32x4{};
-  for (int s0 = 0; s0 < n; s0 += NG) {
-    const int s = s0 + g;
-    const float of = __shfl(weight, s & 63, 64);
-    if (s < n) a += part[(int64_t)s * LPR] * of;
+  for (int s0 = 0;;) {
+#pragma unroll
+    for (int k = 0; k < kEach; ++k) {
+      const int s = s0 + k * NG + g;
+      const float of = __shfl(weight, s & 63, 64);
+      if (s < n) a += y[k] * of;
+    }
+    s0 += kEach * NG;
+    if (s0 >= n) break;
+    load(s0);
   }
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    float y = a[e];
-    if (LPR == 16) y = sum_rows(y);
-    a[e] = sum_halves(y);
+    if (LPR == 16) a[e] = sum_rows(a[e]);
+    a[e] = sum_halves(a[e]);
   }
   if (lane >= LPR) return;
   bf16x4 out;
@@ -534,7 +547,7 @@ hipError_t launch_cache_chunk(const CacheChunkParams& params, hipStream_t stream
   p.by_heads = fast_div(p.heads);
   p.by_splits = fast_div(p.num_splits);
   p.by_stride = fast_div(p.stride > 0 ? p.stride : 1);
-  p.by_tiles = fast_div(p.seq_tiles);
+  p.by_tiles = fast_div(std::max(p.seq_tiles - 1, 1));
   ChunkLookUp& l = p.look_up;
   l.table = p.c.table;
   l.page = p.c.page;
