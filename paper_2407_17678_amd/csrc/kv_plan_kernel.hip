@@ -22,6 +22,9 @@ namespace s2 {
 
 namespace {
 
+using i32x2 = __attribute__((ext_vector_type(2))) int;
+using i32x4 = __attribute__((ext_vector_type(4))) int;
+
 constexpr int kThreadsPlan = 256, kWaves = kThreadsPlan / 64;
 constexpr int kGroups = 1024;  // workgroups over the tables, about: so many counts are added up by each of them
 
@@ -42,14 +45,15 @@ struct Fate {
   bool held, needed, taken;  // it has a page; it is to have one; it is to take one
 };
 __device__ __forceinline__ Fate fate_of(const KvPlanParams& p, const Seq& s, const RowBlocks& rb, int h, int j, int page) {
+  const int S = 1 << p.block_shift;
   Fate f;
   f.held = page >= 0 && page < p.num_pages;
-  f.needed = ((int64_t)j << p.block_shift) < s.end;
+  f.needed = j < (s.end + S - 1) >> p.block_shift;  // (max_len is below 2^31 - S)
   if (p.last_row)
     f.needed = f.needed && p.last_row[(int64_t)h * p.num_blocks + j] >= s.row;
   else
     f.needed = f.needed && (j >= s.row || row_keeps(p, rb, h, s.row, j, 0));
-  f.taken = f.needed && !f.held && ((int64_t)j << p.block_shift) >= s.len;
+  f.taken = f.needed && !f.held && j >= (s.len + S - 1) >> p.block_shift;
   return f;
 }
 
@@ -58,27 +62,42 @@ __device__ __forceinline__ int wave_sum(int x) {
   for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i, 64);
   return x;
 }
-// The sum of x over a workgroup (to all its threads).
-template <class T>
-__device__ __forceinline__ T group_sum(T x, T* parts) {
+// The sums of N numbers over a workgroup (to all its threads).
+template <int N>
+__device__ __forceinline__ void group_sums(int64_t (&x)[N], int64_t (*parts)[kWaves]) {
 #pragma unroll
-  for (int i = 1; i < 64; i *= 2) x += __shfl_xor(x, i, 64);
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) parts[threadIdx.x >> 6] = x;
-  __syncthreads();
-  T sum = 0;
+  for (int k = 0; k < N; ++k) {
 #pragma unroll
-  for (int i = 0; i < kWaves; ++i) sum += parts[i];
-  return sum;
+    for (int i = 1; i < 64; i *= 2) x[k] += __shfl_xor(x[k], i, 64);
+    if ((threadIdx.x & 63) == 0) parts[k][threadIdx.x >> 6] = x[k];
+  }
+  __syncthreads();
+#pragma unroll
+  for (int k = 0; k < N; ++k) {
+    x[k] = 0;
+#pragma unroll
+    for (int i = 0; i < kWaves; ++i) x[k] += parts[k][i];
+  }
+}
+
+// kAtOnce times 64 entries of a line from j0 on, a lane's; -1 behind the line's end.  (One load after the other costs its latency 8 times in a line of 512.)
+constexpr int kAtOnce = 8;
+__device__ __forceinline__ void load_entries(const int32_t* line, int j0, int max_blocks, int lane, int (&to)[kAtOnce]) {
+#pragma unroll
+  for (int k = 0; k < kAtOnce; ++k) {
+    const int j = j0 + 64 * k + lane;
+    to[k] = line[min(j, max_blocks - 1)];
+    if (j >= max_blocks) to[k] = -1;
+  }
 }
 
 __global__ __launch_bounds__(kThreadsPlan) void kv_plan_count_kernel(const KvPlanParams p) {
-  __shared__ int64_t parts[kWaves];
+  __shared__ int64_t parts[1][kWaves];
   __shared__ int counts[kWaves][2];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   if ((int)blockIdx.x >= p.groups) {  // 256 sequences
     const int block = blockIdx.x - p.groups, b = block * kThreadsPlan + tid;
-    int64_t fresh = 0;
+    int64_t fresh[1] = {0};
     if (b < p.nseq) {
       const int len = p.lens[b], n = p.new_lens[b];
       const Seq s = seq_of(len, n, p.query_from ? p.query_from[b] : len, p);
@@ -87,10 +106,10 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_count_kernel(const KvPla
       to[1] = s.end;
       to[2] = s.row;
       to[3] = max(n, 0);
-      fresh = max(n, 0);
+      fresh[0] = max(n, 0);
     }
-    fresh = group_sum(fresh, parts);
-    if (tid == 0) p.ws_fresh[block] = fresh;
+    group_sums(fresh, parts);
+    if (tid == 0) p.ws_fresh[block] = fresh[0];
     if (block == 0 && tid == 0) {
       const int first = p.free_state[0], count = min(max(p.free_state[1], 0), p.num_pages);
       p.ws_state[0] = first >= 0 && first < p.num_pages ? first : 0;
@@ -102,18 +121,27 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_count_kernel(const KvPla
   for (int i = 0; i < p.pairs_each; ++i) {
     const int64_t pair = ((int64_t)blockIdx.x * kWaves + wave) * p.pairs_each + i;
     if (pair >= p.pairs) break;
+    const int32_t* const line = p.table + pair * p.max_blocks;
+    int page[kAtOnce];
+    load_entries(line, 0, p.max_blocks, lane, page);
     const int b = (int)pair / p.by_heads, h = (int)pair - b * p.heads;
     const int len = load_const<int32_t>(p.lens + b);
     const Seq s = seq_of(len, load_const<int32_t>(p.new_lens + b), p.query_from ? load_const<int32_t>(p.query_from + b) : len, p);
     const RowBlocks rb{};
-    const int32_t* const line = p.table + pair * p.max_blocks;
     int f0 = 0, t0 = 0;
-    for (int j0 = 0; j0 < p.max_blocks; j0 += 64) {
-      const int j = j0 + lane;
-      const bool is = j < p.max_blocks;
-      const Fate f = fate_of(p, s, rb, h, is ? j : 0, is ? line[j] : -1);
-      f0 += __popcll(__ballot(is && f.held && !f.needed));
-      t0 += __popcll(__ballot(is && f.taken));
+    for (int j0 = 0;;) {
+#pragma unroll
+      for (int k = 0; k < kAtOnce; ++k) {
+        if (j0 + 64 * k >= p.max_blocks) break;
+        const int j = j0 + 64 * k + lane;
+        const bool is = j < p.max_blocks;
+        const Fate f = fate_of(p, s, rb, h, is ? j : 0, page[k]);
+        f0 += __popcll(__ballot(is && f.held && !f.needed));
+        t0 += __popcll(__ballot(is && f.taken));
+      }
+      j0 += 64 * kAtOnce;
+      if (j0 >= p.max_blocks) break;
+      load_entries(line, j0, p.max_blocks, lane, page);
     }
     if (lane == 0) {
       p.ws_pair[2 * pair] = f0;
@@ -136,18 +164,21 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_count_kernel(const KvPla
 }
 
 // What all groups before `group` give up and take.
-__device__ __forceinline__ void before_group(const KvPlanParams& p, int group, int64_t* parts, int64_t& freed, int64_t& taken) {
-  freed = taken = 0;
+__device__ __forceinline__ void before_group(const KvPlanParams& p, int group, int64_t (*parts)[kWaves], int64_t& freed, int64_t& taken) {
+  int64_t sums[2] = {0, 0};
+#pragma unroll 4
   for (int i = threadIdx.x; i < group; i += kThreadsPlan) {
-    freed += p.ws_group[2 * i];
-    taken += p.ws_group[2 * i + 1];
+    const i32x2 of = reinterpret_cast<const i32x2*>(p.ws_group)[i];
+    sums[0] += of[0];
+    sums[1] += of[1];
   }
-  freed = group_sum(freed, parts);
-  taken = group_sum(taken, parts);
+  group_sums(sums, parts);
+  freed = sums[0];
+  taken = sums[1];
 }
 
 __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlanParams p) {
-  __shared__ int64_t parts[kWaves];
+  __shared__ int64_t parts[2][kWaves];
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int first = p.ws_state[0], count = p.ws_state[1];
   const int room = p.num_pages - count;  // pages that the ring has room for (more than are held only if an entry names a page twice)
@@ -156,18 +187,23 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
     return at >= p.num_pages ? at - p.num_pages : at;
   };
   if (item < p.groups) {
+    const int64_t pair0 = (int64_t)item * kWaves * p.pairs_each, mine = pair0 + (int64_t)wave * p.pairs_each;
+    int page[kAtOnce];
+    load_entries(p.table + min(mine, p.pairs - 1) * p.max_blocks, 0, p.max_blocks, lane, page);
+    // (all of these loads before the wavefronts wait for each other)
+    int f0 = 0, t0 = 0;  // of the wavefronts before mine
+    for (int64_t i = pair0 + lane; i < min(mine, (int64_t)p.pairs); i += 64) {
+      const i32x2 of = reinterpret_cast<const i32x2*>(p.ws_pair)[i];
+      f0 += of[0];
+      t0 += of[1];
+    }
+    i32x4 seq = reinterpret_cast<const i32x4*>(p.ws_seq)[(int)min(mine, p.pairs - 1) / p.by_heads];
     int64_t freed, taken;
     before_group(p, item, parts, freed, taken);
     if (item == p.groups - 1 && tid == 0) {
       const int64_t f = min(freed + p.ws_group[2 * item], (int64_t)room), t = min(taken + p.ws_group[2 * item + 1], (int64_t)count);
       p.new_state[0] = (int)slot(first + t);
       p.new_state[1] = (int)(count - t + f);
-    }
-    const int64_t pair0 = (int64_t)item * kWaves * p.pairs_each, mine = pair0 + (int64_t)wave * p.pairs_each;
-    int f0 = 0, t0 = 0;  // of the wavefronts before mine
-    for (int64_t i = pair0 + lane; i < min(mine, (int64_t)p.pairs); i += 64) {
-      f0 += p.ws_pair[2 * i];
-      t0 += p.ws_pair[2 * i + 1];
     }
     freed += wave_sum(f0);
     taken += wave_sum(t0);
@@ -176,30 +212,38 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
       const int64_t pair = mine + i;
       if (pair >= p.pairs) break;
       const int b = (int)pair / p.by_heads, h = (int)pair - b * p.heads;
-      const Seq s{p.ws_seq[4 * (int64_t)b], p.ws_seq[4 * (int64_t)b + 1], p.ws_seq[4 * (int64_t)b + 2]};
+      if (i > 0) seq = reinterpret_cast<const i32x4*>(p.ws_seq)[b];
+      const Seq s{seq[0], seq[1], seq[2]};
       const RowBlocks rb{};
       const int32_t* const line = p.table + pair * p.max_blocks;
       int32_t* const to = p.new_table + pair * p.max_blocks;
-      for (int j0 = 0; j0 < p.max_blocks; j0 += 64) {
-        const int j = j0 + lane;
-        const bool is = j < p.max_blocks;
-        const int page = is ? line[j] : -1;
-        const Fate f = fate_of(p, s, rb, h, is ? j : 0, page);
-        const uint64_t gives = __ballot(is && f.held && !f.needed), takes = __ballot(is && f.taken);
-        const uint64_t below = ((uint64_t)1 << lane) - 1;
-        int now = f.needed ? page : -1;
-        if (gives >> lane & 1) {
-          const int64_t at = freed + __popcll(gives & below);
-          if (at < room) p.new_ring[slot((int64_t)first + count + at)] = page;
+      if (i > 0) load_entries(line, 0, p.max_blocks, lane, page);
+      for (int j0 = 0;;) {
+#pragma unroll
+        for (int k = 0; k < kAtOnce; ++k) {
+          if (j0 + 64 * k >= p.max_blocks) break;
+          const int j = j0 + 64 * k + lane;
+          const bool is = j < p.max_blocks;
+          const Fate f = fate_of(p, s, rb, h, is ? j : 0, page[k]);
+          const uint64_t gives = __ballot(is && f.held && !f.needed), takes = __ballot(is && f.taken);
+          const uint64_t below = ((uint64_t)1 << lane) - 1;
+          int now = f.needed ? page[k] : -1;
+          if (gives >> lane & 1) {
+            const int64_t at = freed + __popcll(gives & below);
+            if (at < room) p.new_ring[slot((int64_t)first + count + at)] = page[k];
+          }
+          if (takes >> lane & 1) {
+            const int64_t at = taken + __popcll(takes & below);
+            now = at < count ? p.ring[slot(first + at)] : -1;
+          }
+          without += __popcll(__ballot((takes >> lane & 1) && taken + __popcll(takes & below) >= count));
+          if (is && (p.apart || now != page[k])) to[j] = now;
+          freed += __popcll(gives);
+          taken += __popcll(takes);
         }
-        if (takes >> lane & 1) {
-          const int64_t at = taken + __popcll(takes & below);
-          now = at < count ? p.ring[slot(first + at)] : -1;
-        }
-        without += __popcll(__ballot((takes >> lane & 1) && taken + __popcll(takes & below) >= count));
-        if (is && (p.apart || now != page)) to[j] = now;
-        freed += __popcll(gives);
-        taken += __popcll(takes);
+        j0 += 64 * kAtOnce;
+        if (j0 >= p.max_blocks) break;
+        load_entries(line, j0, p.max_blocks, lane, page);
       }
     }
     if (p.short_of && lane == 0 && without > 0) atomicAdd(p.short_of, without);
@@ -208,11 +252,12 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
   item -= p.groups;
   if (item < p.nseq) {  // a sequence's rows
     if (!p.cu_new && !p.positions && !p.seq_lens) return;
-    int64_t before = 0;
-    for (int i = tid; i < item / kThreadsPlan; i += kThreadsPlan) before += p.ws_fresh[i];
+    int64_t sums[1] = {0};
+    for (int i = tid; i < item / kThreadsPlan; i += kThreadsPlan) sums[0] += p.ws_fresh[i];
     const int in_block = item / kThreadsPlan * kThreadsPlan + tid;
-    if (in_block < item) before += p.ws_seq[4 * (int64_t)in_block + 3];
-    before = group_sum(before, parts);
+    if (in_block < item) sums[0] += p.ws_seq[4 * (int64_t)in_block + 3];
+    group_sums(sums, parts);
+    const int64_t before = sums[0];
     const int len = p.ws_seq[4 * (int64_t)item], end = p.ws_seq[4 * (int64_t)item + 1], fresh = p.ws_seq[4 * (int64_t)item + 3];
     if (tid == 0) {
       constexpr int64_t kMost = 0x7fffffff;
