@@ -537,6 +537,7 @@ int64_t chunk_tiles(CacheChunkParams& p) {
   const int64_t of_rows = p.num_rows / BM + 2 * (int64_t)p.nseq;
   p.packed = of_rows < each * p.nseq;
   const int64_t tiles = p.packed ? of_rows : each * p.nseq;
+  p.sorted = p.nseq > 1 && p.nseq <= 64;
   p.seq_tiles = (int)each;
   p.num_tiles = (int)std::min<int64_t>(tiles, kMostGroups + 1);
   return tiles;

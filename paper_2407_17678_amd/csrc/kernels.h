@@ -269,9 +269,10 @@ struct CacheChunkParams {
   const int32_t* row_ptr;
   const int32_t* col_idx;
   int num_blocks;
-  // set by chunk_tiles: rows of a tile (1 << tile_shift), tiles of the launch; seq_tiles of them to a sequence, or (packed) to all
+  // set by chunk_tiles: rows of a tile (1 << tile_shift), tiles of the launch; seq_tiles of them to a sequence, or (packed) to all, or in the order
+  // of the sequences' ends (sorted)
   int tile_shift, seq_tiles, num_tiles;
-  bool packed;
+  bool packed, sorted;
   FastDiv by_heads, by_splits, by_stride, by_tiles;  // set by launch_cache_chunk
   ChunkLookUp look_up;                               // likewise
 };
