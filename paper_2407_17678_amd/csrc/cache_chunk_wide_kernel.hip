@@ -14,6 +14,7 @@
 #include <algorithm>
 
 #include "cache_chunk.h"
+#include "cache_chunk_few.h"
 #include "config.h"
 
 namespace s2 {
@@ -47,6 +48,14 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
   const ChunkTileAt x0 = chunk_tile_at(p, tile);
   if (x0.rows <= 0) return;
   const ChunkRows r0 = chunk_block_rows(p, x0);
+  // A tile of few rows (a short chunk among long ones, the end of one) would leave wavefronts without a query: theirs take tokens of their own instead (12 chunks of up to
+  // 1024 rows over e4m3 105 us to 95, 40 of up to 300 226 to 191, 4 of 2048 as before).  Expected not to be: else the loop below goes without registers that this one takes.
+  if (__builtin_expect(__builtin_amdgcn_readfirstlane(x0.rows) <= 32, 0)) {
+    using Few = ChunkFewShared<D, 2, SMALL>;
+    static_assert(sizeof(Few) <= sizeof(sh_kv), "it fits where K and V are otherwise");
+    chunk_few<D, FMT, 2, SMALL>(p, x0, r0, h, split, *reinterpret_cast<Few*>(sh_kv));
+    return;
+  }
   const ChunkQuery q0 = chunk_query(p, x0, r0, MW * wave + l32 - x0.skipped);
   bf16x8 qf[KK];
 #pragma unroll
