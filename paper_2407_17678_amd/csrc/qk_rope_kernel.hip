@@ -33,9 +33,18 @@ __device__ __forceinline__ float lower(uint32_t x) { return __builtin_bit_cast(f
 __device__ __forceinline__ float upper(uint32_t x) { return __builtin_bit_cast(float, x & 0xffff0000u); }
 __device__ __forceinline__ float feature_of(const u32x4& x, int e) { return e & 1 ? upper(x[e >> 1]) : lower(x[e >> 1]); }
 
-// A row's part that nothing here reads again.  (Forward of 32 heads, 32768 tokens: 225 us with ordinary loads and stores, 222 with these loads, 210 with
-// such stores as well; of 4 x 16 heads, 8192 tokens, backward: 168 and 157, with such stores 161: they go where the same lines were read.)
+// A row's part that nothing here reads again.  (Of 32 heads, 32768 tokens, forward: 225 us with ordinary loads and stores, 222 with these loads, 208 with such stores as
+// well; of 4 x 16 heads, 8192 tokens, backward: 169 with these loads, 158 with such stores, 155 with the next heads' loads before this one's sums.)
 __device__ __forceinline__ u32x4 load_once(const uint16_t* at) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at)); }
+
+// A row's part of the results; FAR: of more than the caches hold.
+template <bool FAR>
+__device__ __forceinline__ void store(uint16_t* at, const u32x4& x) {
+  if (FAR)
+    __builtin_nontemporal_store(x, reinterpret_cast<u32x4*>(at));
+  else
+    *reinterpret_cast<u32x4*>(at) = x;
+}
 
 // sum over the D / 8 lanes of a row
 template <int D>
@@ -104,7 +113,6 @@ __device__ __forceinline__ void weights(const float* w, int from, float (&to)[8]
   }
 }
 
-// FAR: more results than the caches hold.
 template <int D, bool FAR>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_kernel(const QkRopeParams p) {
   constexpr int LPR = D / 8, HPW = 64 / LPR;
@@ -161,16 +169,12 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_kernel(const QkRopePa
         const float z = __builtin_fmaf(feature_of(vo, 2 * i + 1), other[2 * i + 1], feature_of(v, 2 * i + 1) * own[2 * i + 1]);
         out[i] = pack2(a * r, z * r);
       }
-      if (!is) continue;
-      if (FAR)
-        __builtin_nontemporal_store(out, reinterpret_cast<u32x4*>(y + h * p.y_sh));
-      else
-        *reinterpret_cast<u32x4*>(y + h * p.y_sh) = out;
+      if (is) store<FAR>(y + h * p.y_sh, out);
     }
   }
 }
 
-template <int D>
+template <int D, bool FAR>
 __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_bwd_kernel(const QkRopeParams p) {
   constexpr int LPR = D / 8, HPW = 64 / LPR;
   __shared__ float2 cs[kRopeWaves][64];
@@ -197,10 +201,16 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_bwd_kernel(const QkRo
       const bool norm = p.weight[which] != nullptr;
       float w[8];
       if (norm) weights(p.weight[which], 8 * c, w);
+      u32x4 g_next{}, x_next{};
+      auto load = [&](int h) __attribute__((always_inline)) {
+        g_next = h < h1 ? load_once(p.g[which] + at_y + h * p.y_sh) : u32x4{};
+        x_next = h < h1 ? load_once(p.x[which] + at_x + h * p.x_sh) : u32x4{};
+      };
+      load(h0 + mine);
       for (int h = h0 + mine; h - mine < h1; h += HPW) {
         const bool is = h < h1;
-        const u32x4 gv = is ? load_once(p.g[which] + at_y + h * p.y_sh) : u32x4{};
-        const u32x4 v = is ? load_once(p.x[which] + at_x + h * p.x_sh) : u32x4{};
+        const u32x4 gv = g_next, v = x_next;
+        load(h + HPW);
         const u32x4 go = partners(gv, turn);
         float g[8];
 #pragma unroll
@@ -224,7 +234,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_bwd_kernel(const QkRo
         }
 #pragma unroll
         for (int i = 0; i < 4; ++i) out[i] = pack2(g[2 * i], g[2 * i + 1]);
-        if (is) *reinterpret_cast<u32x4*>(p.y[which] + at_x + h * p.x_sh) = out;
+        if (is) store<FAR>(p.y[which] + at_x + h * p.x_sh, out);
       }
     }
   }
@@ -285,6 +295,8 @@ constexpr int64_t kFwdWaves = 8192;
 constexpr int64_t kFarBytes = 32 << 20;
 constexpr int kBwdParts = 1024;
 
+bool is_far(const QkRopeParams& p) { return (int64_t)p.rows * p.heads * p.head_dim * 2 * ((p.x[0] != nullptr) + (p.x[1] != nullptr)) > kFarBytes; }
+
 }  // namespace
 
 int64_t qk_rope_groups(const QkRopeParams& params) {
@@ -296,7 +308,7 @@ int64_t qk_rope_groups(const QkRopeParams& params) {
 hipError_t launch_qk_rope(const QkRopeParams& params, hipStream_t stream) {
   QkRopeParams p = params;
   head_groups(p, kFwdWaves);
-  const bool far = (int64_t)p.rows * p.heads * p.head_dim * 2 * ((p.x[0] != nullptr) + (p.x[1] != nullptr)) > kFarBytes;
+  const bool far = is_far(p);
   const dim3 grid((p.rows * p.head_groups + kRopeWaves - 1) / kRopeWaves), block(64 * kRopeWaves);
   if (p.head_dim == 128) {
     if (far)
@@ -326,11 +338,19 @@ hipError_t launch_qk_rope_bwd(const QkRopeParams& params, hipStream_t stream) {
   QkRopeParams p = params;
   head_groups(p, (int64_t)kBwdParts * kRopeWaves);
   p.parts = qk_rope_parts(p.rows, p.heads, p.head_dim);
-  const dim3 block(64 * kRopeWaves);
-  if (p.head_dim == 128)
-    hipLaunchKernelGGL(qk_rope_bwd_kernel<128>, dim3(p.parts), block, 0, stream, p);
-  else
-    hipLaunchKernelGGL(qk_rope_bwd_kernel<64>, dim3(p.parts), block, 0, stream, p);
+  const dim3 grid(p.parts), block(64 * kRopeWaves);
+  const bool far = is_far(p);
+  if (p.head_dim == 128) {
+    if (far)
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<128, true>), grid, block, 0, stream, p);
+    else
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<128, false>), grid, block, 0, stream, p);
+  } else {
+    if (far)
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<64, true>), grid, block, 0, stream, p);
+    else
+      hipLaunchKernelGGL((qk_rope_bwd_kernel<64, false>), grid, block, 0, stream, p);
+  }
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || !p.part) return e;
   if (p.head_dim == 128)
