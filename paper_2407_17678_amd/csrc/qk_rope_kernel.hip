@@ -4,12 +4,12 @@
 // Each feature of y is a sum of two, x_f (w_f cos) and its partner's x_p (w_p (-+ sin)), both times r: the factors are the same for all heads of a row.
 // Backward: with xh = x r and g' = R_t^T g, dw = sum g' xh and dx = r (w g' - xh mean(w g' xh)); r is formed again from x, which dw needs anyway.
 //
-// It moves bytes: D / 8 lanes take a row of D features, 16 bytes each, a wavefront 512 / D heads of one token at a time.  The angles of a token are formed once
+// It moves bytes, and they bound it where there are many rows; a decode step's (64 x 32 heads 5.4 us) is the launch and two trips to memory.  D / 8 lanes take a row of D features, 16 bytes each, a wavefront 512 / D heads of one token at a time.  The angles of a token are formed once
 // for its heads, a pair to a lane, and go through LDS: position times frequency and the whole turns that it holds in 64 bits (a far position's angle has no
 // digits left for its fraction in 32), sine and cosine of what is left in 32.
 //
 // The weights' gradients are summed in registers over what a wavefront takes, over the wavefronts of a workgroup through LDS, and over workgroups by a
-// second launch, in an order that the sizes alone decide.
+// second launch, in an order that the sizes alone decide (1024 parts of 2 x 128 sums 4.6 us; with eight groups of threads to 32 features instead of 64 to 16, 7.5).
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -34,7 +34,8 @@ __device__ __forceinline__ float upper(uint32_t x) { return __builtin_bit_cast(f
 __device__ __forceinline__ float feature_of(const u32x4& x, int e) { return e & 1 ? upper(x[e >> 1]) : lower(x[e >> 1]); }
 
 // A row's part that nothing here reads again.  (Of 32 heads, 32768 tokens, forward: 225 us with ordinary loads and stores, 222 with these loads, 208 with such stores as
-// well; of 4 x 16 heads, 8192 tokens, backward: 169 with these loads, 158 with such stores, 155 with the next heads' loads before this one's sums.)
+// well, 202 with the next heads' loads before these heads' sums, 5.3 TB/s, a large copy's rate; without the arithmetic 200.  Of 4 x 16 heads, 8192 tokens, backward: 169
+// with these loads, 158 with such stores, 155 with the next heads' loads first, 5.2 TB/s.)
 __device__ __forceinline__ u32x4 load_once(const uint16_t* at) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at)); }
 
 // A row's part of the results; FAR: of more than the caches hold.
@@ -151,9 +152,12 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_kernel(const QkRopePa
         other[e] *= turn.swapped ? wo[e ^ 1] : wo[e];
       }
     }
+    auto load = [&](int h) __attribute__((always_inline)) { return h < h1 ? load_once(x + h * p.x_sh) : u32x4{}; };
+    u32x4 next = load(h0 + mine);
     for (int h = h0 + mine; h - mine < h1; h += HPW) {
       const bool is = h < h1;
-      const u32x4 v = is ? load_once(x + h * p.x_sh) : u32x4{};
+      const u32x4 v = next;
+      next = load(h + HPW);
       const u32x4 vo = partners(v, turn);
       float r = 1.f;
       if (norm) {
