@@ -566,8 +566,10 @@ size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, 
  * row (start[b] + i) div S of the mask keeps: a chunk gives what as many decode steps give.  A row whose position is outside [0,
  * max_blocks*block_size) gets o = 0 and lse = -inf, and so does one all of whose kept blocks are not resident; such blocks contribute nothing and are counted.
  * Rows that belong to no sequence are left as they were.  What a row does not attend stays out of its result whatever it holds; of what it attends, a V that
- * is NaN, or infinities of both signs, give NaN in their feature.  With max_new (or num_rows) up to 64 probabilities go to V in 16 bits, as
- * in a decode step, else rounded to bf16, as in s2_attn_fwd.  max_new is a limit, not a size.
+ * is NaN, or infinities of both signs, give NaN in their feature, and an infinity an infinity of its sign, however small its token's probability (or NaN, where
+ * that is 0).  With max_new (or num_rows) up to 64 probabilities go to V in 16 bits, as in a decode step, else those of 128 rows at a time that lie in
+ * the same 128 positions rounded to bf16, as in s2_attn_fwd, or in 16 bits if they are 32 or fewer; each relative to a power of two of up to 2^8 (the sum is not).
+ * max_new is a limit, not a size: the tokens of a sequence beyond it are rows of nobody.  Offsets of cu_new outside [0, num_rows] are cut to it.
  * q and o may be the same tensor.
  * workspace: s2_attn_chunk_workspace_bytes(..., max_blocks * block_size, num_splits) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit
  * (with num_splits = 0 less will do, down to none at all for one split, with which nothing goes there: the call then takes fewer splits).  With a layout, it covers the cache.
@@ -585,8 +587,10 @@ size_t s2_attn_chunk_workspace_bytes(int32_t nseq, int32_t heads, int32_t max_ne
  * and are not held take pages from its beginning, in the same order.  Pages that this call gives up are not taken before the next one, so that what runs
  * beside it may still read them.  A block that there is no page for, and one that begins before lens and is not held, are not held (-1) or left as they are.  An entry that is negative or
  * num_pages or more is not held; new entries that are not held and not to be held are -1.  A page is held by one entry at most.
- * With new_lens < 0 nothing is held and the sequence counts as 0 new tokens and 0 tokens.  lens, new_lens and query_from are cut to what the table has room for;
- * cu_new counts all of new_lens, positions are lens[b] + i for all of them, and entries of positions beyond the last row are left as they were.
+ * With new_lens < 0 nothing is held and the sequence counts as 0 new tokens and 0 tokens.  With max_len = max_blocks * block_size, lens are cut to [0, max_len] and
+ * query_from to [0, max_len); seq_lens are min(lens + new_lens, max_len).  cu_new counts all of new_lens (up to 2^31 - 1 together), positions are lens[b] + i
+ * for all of them, also from max_len on (s2_kv_append_paged leaves such rows out, and they attend nothing), and entries of positions beyond the last row are left as
+ * they were.  A ring whose free_state is out of range is taken to begin at 0, or to hold none, or num_pages.
  * p->num_heads is heads, p->num_blocks is ignored; with a layout, it covers the cache.
  * workspace: s2_kv_plan_workspace_bytes(nseq, heads) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit.
  * Errors: NULL, BAD_PARAM, SHAPE, ALIGN, WORKSPACE, NO_DEVICE (layout), HIP. */

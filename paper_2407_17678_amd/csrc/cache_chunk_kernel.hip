@@ -5,9 +5,12 @@
 // what they read: a tile of 16 rows makes 64 D flops of a token's K and V, so that a tile of a few rows is bound by the cache's bytes and one of 128 by
 // matrix instructions.
 //
-// The four wavefronts of a workgroup share a unit of 64 tokens: each fetches a piece of 16 of them, brings it to bf16 once and writes its K and V rows into LDS
-// (ChunkTile); then each takes its 16 or 32 queries against the whole unit.  Scores are formed as keys x queries, so that a lane holds one query and the
-// probabilities are the second operand of the product with V as they stand.
+// Three forms, by rows to a sequence.  Up to 32: each wavefront takes tokens of its own against all rows (cache_chunk_few.h; 64 sequences of 1 to 12 rows of
+// 32 heads after 8192 to 32768 tokens, e4m3, 210 us, 5.6 TB/s).  33 to 64, below: the four wavefronts of a workgroup share a unit of 64 tokens: each
+// fetches a piece of 16 of them, brings it to bf16 once and writes its K and V rows into LDS (ChunkTile); then each takes 16 queries against the whole unit (64
+// sequences of 1 to 40 rows, bf16, 283 us, 5.3 TB/s; one of 40 rows after 32768 tokens, 512 workgroups of three units each, 18 us and 4 for the splits' sums).
+// More: tiles of 128 rows (cache_chunk_wide_kernel.hip).  In all of them scores are formed as keys x queries, so that a lane holds one query and the
+// probabilities are the second operand of the product with V as they stand.  Up to 64 rows P goes to V in two bf16 terms, 16 bits together, as in a decode step.
 #include <hip/hip_runtime.h>
 
 #include "cache_chunk.h"
@@ -220,7 +223,7 @@ __global__ __launch_bounds__(256, D == 64 ? 4 : 3) void cache_chunk_kernel(const
   }
 }
 
-// Merges the splits, a wavefront to a row (see cache_attn_kernel.hip).
+// Merges the splits, a wavefront to a row (see cache_attn_kernel.hip; 1280 rows of 16 splits 4.1 us, with a load at a time 5.7).
 template <int D>
 __global__ __launch_bounds__(256) void cache_chunk_merge_kernel(const CacheChunkParams p) {
   constexpr int LPR = D / 4, NG = 64 / LPR;

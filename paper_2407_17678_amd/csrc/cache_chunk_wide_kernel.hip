@@ -1,6 +1,7 @@
 // Attention of a chunk of more than 64 new tokens over a paged cache: tiles of 128 rows, 32 to a wavefront (see cache_chunk_kernel.hip for the mathematics).
 //
-// Matrix instructions bound it, and beside them the vector instructions of the softmax and of bringing rows to bf16.  A SIMD overlaps the two where they alternate finely in
+// Matrix instructions bound it (41 % of a SIMD's cycles), and beside them the vector instructions of the softmax and of bringing rows to bf16 (51 %): 2048 rows of 32 heads
+// after 30720 tokens over e4m3, 512 workgroups of 47 units, 114 us, 858 TFLOP/s; the forward of a whole sequence takes 116 for such rows from contiguous bf16.  A SIMD overlaps the two where they alternate finely in
 // one instruction stream (sched_util.h), so the loop is software pipelined by halves of a unit, 32 tokens: in half step j a wavefront forms the scores of half j, turns those of
 // half j - 1 into probabilities and adds the product of half j - 2's with V, which are independent of each other, in one hand-written sequence of slots, a
 // matrix instruction to each.  V lags behind K by a unit, so that both tiles of a trip are used up in it and one barrier a trip is enough: meanwhile each

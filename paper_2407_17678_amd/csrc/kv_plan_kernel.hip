@@ -10,7 +10,8 @@
 // a workgroup adds up the counts before its own (at most kGroups numbers) and moves the pages.  Pages that are given up lie beyond those that were free before, so that
 // taking and giving never meet in the ring, in place too.
 //
-// It reads and writes 4 bytes an entry; a table of 64 sequences x 32 heads x 512 blocks is 4 MB.
+// It reads and writes 4 bytes an entry, and takes what two dependent launches and their trips to memory take: for 64 sequences x 32 heads x 512 blocks, a table of 4 MB, 5.4 and 8.3 us
+// (0.8 TB/s of 11 MB), for 11 x 7 short lines 3.4 and 5.0.  One launch would have each workgroup count what is before it, or wait for others.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
