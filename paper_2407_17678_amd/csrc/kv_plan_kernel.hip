@@ -260,8 +260,8 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
     group_sums(sums, parts);
     const int64_t before = sums[0];
     const int len = p.ws_seq[4 * (int64_t)item], end = p.ws_seq[4 * (int64_t)item + 1], fresh = p.ws_seq[4 * (int64_t)item + 3];
+    constexpr int64_t kMost = 0x7fffffff;
     if (tid == 0) {
-      constexpr int64_t kMost = 0x7fffffff;
       if (p.cu_new) {
         if (item == 0) p.cu_new[0] = 0;
         p.cu_new[item + 1] = (int)min(before + fresh, kMost);
@@ -270,7 +270,7 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
     }
     if (!p.positions) return;
     const int64_t rows = min((int64_t)fresh, p.num_rows - before);
-    for (int64_t i = tid; i < rows; i += kThreadsPlan) p.positions[before + i] = (int)(len + i);
+    for (int64_t i = tid; i < rows; i += kThreadsPlan) p.positions[before + i] = (int)min(len + i, kMost);
     return;
   }
   item -= p.nseq;  // entries of the ring that no page is written to
