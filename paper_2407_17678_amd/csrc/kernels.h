@@ -273,7 +273,8 @@ struct CacheChunkParams {
   // of the sequences' ends (sorted)
   int tile_shift, seq_tiles, num_tiles;
   bool packed, sorted;
-  FastDiv by_heads, by_splits, by_stride, by_tiles;  // set by launch_cache_chunk
+  FastDiv by_heads, by_splits, by_stride, by_tiles, by_new;  // set by launch_cache_chunk
+  bool merge_rows;                                   // likewise: splits are merged by rows of the tensors, not by rows that sequences may have
   ChunkLookUp look_up;                               // likewise
 };
 

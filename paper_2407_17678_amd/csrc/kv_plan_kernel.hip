@@ -10,8 +10,8 @@
 // a workgroup adds up the counts before its own (at most kGroups numbers) and moves the pages.  Pages that are given up lie beyond those that were free before, so that
 // taking and giving never meet in the ring, in place too.
 //
-// It reads and writes 4 bytes an entry, and takes what two dependent launches and their trips to memory take: for 64 sequences x 32 heads x 512 blocks, a table of 4 MB, 5.4 and 8.3 us
-// (0.8 TB/s of 11 MB), for 11 x 7 short lines 3.4 and 5.0.  One launch would have each workgroup count what is before it, or wait for others.
+// It reads and writes 4 bytes an entry, and takes what two dependent launches and their trips to memory take: for 64 sequences x 32 heads x 512 blocks, a table of 4 MB, 5.4 and 7.7 us
+// (0.9 TB/s of 11 MB), for 11 x 7 short lines 3.4 and 4.8.  One launch would have each workgroup count what is before it, or wait for others.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -81,7 +81,7 @@ __device__ __forceinline__ void group_sums(int64_t (&x)[N], int64_t (*parts)[kWa
   }
 }
 
-// kAtOnce times 64 entries of a line from j0 on, a lane's; -1 behind the line's end.  (One load after the other costs its latency 8 times in a line of 512.)
+// kAtOnce times 64 entries of a line from j0 on, a lane's; -1 behind the line's end.  (48 sequences x 32 heads x 543 blocks: 5.7 and 8.2 us; loaded one after the other, with the counts, up to 7.6 and 10.4.)
 constexpr int kAtOnce = 8;
 __device__ __forceinline__ void load_entries(const int32_t* line, int j0, int max_blocks, int lane, int (&to)[kAtOnce]) {
 #pragma unroll
@@ -229,18 +229,18 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
           const uint64_t gives = __ballot(is && f.held && !f.needed), takes = __ballot(is && f.taken);
           const uint64_t below = ((uint64_t)1 << lane) - 1;
           int now = f.needed ? page[k] : -1;
-          if (gives >> lane & 1) {
+          if (gives) {  // (in most lines of a step none, or one chunk's: 8.3 -> 7.7 us)
             const int64_t at = freed + __popcll(gives & below);
-            if (at < room) p.new_ring[slot((int64_t)first + count + at)] = page[k];
+            if ((gives >> lane & 1) && at < room) p.new_ring[slot((int64_t)first + count + at)] = page[k];
+            freed += __popcll(gives);
           }
-          if (takes >> lane & 1) {
+          if (takes) {
             const int64_t at = taken + __popcll(takes & below);
-            now = at < count ? p.ring[slot(first + at)] : -1;
+            if (takes >> lane & 1) now = at < count ? p.ring[slot(first + at)] : -1;
+            without += (int)min(max(taken + __popcll(takes) - max(taken, (int64_t)count), (int64_t)0), (int64_t)64);
+            taken += __popcll(takes);
           }
-          without += __popcll(__ballot((takes >> lane & 1) && taken + __popcll(takes & below) >= count));
           if (is && (p.apart || now != page[k])) to[j] = now;
-          freed += __popcll(gives);
-          taken += __popcll(takes);
         }
         j0 += 64 * kAtOnce;
         if (j0 >= p.max_blocks) break;
@@ -274,13 +274,17 @@ __global__ __launch_bounds__(kThreadsPlan) void kv_plan_move_kernel(const KvPlan
     return;
   }
   item -= p.nseq;  // entries of the ring that no page is written to
+  const int64_t i0 = (int64_t)item * kRingEach + tid;
+  int entry[kRingEach / kThreadsPlan];
+#pragma unroll
+  for (int k = 0; k < kRingEach / kThreadsPlan; ++k) entry[k] = p.ring[min(i0 + k * kThreadsPlan, (int64_t)p.num_pages - 1)];
   int64_t freed, taken;
   before_group(p, p.groups, parts, freed, taken);
   freed = min(freed, (int64_t)room);
-  const int64_t i0 = (int64_t)item * kRingEach;
-  for (int64_t i = i0 + tid; i < min(i0 + kRingEach, (int64_t)p.num_pages); i += kThreadsPlan) {
-    const int64_t from_tail = i - slot((int64_t)first + count);
-    if ((from_tail < 0 ? from_tail + p.num_pages : from_tail) >= freed) p.new_ring[i] = p.ring[i];
+#pragma unroll
+  for (int k = 0; k < kRingEach / kThreadsPlan; ++k) {
+    const int64_t i = i0 + k * kThreadsPlan, from_tail = i - slot((int64_t)first + count);
+    if (i < p.num_pages && (from_tail < 0 ? from_tail + p.num_pages : from_tail) >= freed) p.new_ring[i] = entry[k];
   }
 }
 

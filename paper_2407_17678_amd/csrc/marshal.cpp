@@ -701,7 +701,6 @@ PyObject* plan_call(PyObject* const* a, Py_ssize_t n) {
     fail_assert();
     return nullptr;
   }
-  const int64_t entries = table[0] * table[1] * table[2];
   if (a[11] != Py_None) {
     const Ref count(PyObject_CallMethodNoArgs(a[11], names.numel));
     if (!count.o || !as_i64(count.o, rows)) return nullptr;
@@ -710,8 +709,10 @@ PyObject* plan_call(PyObject* const* a, Py_ssize_t n) {
       return nullptr;
     }
   }
-  if (!ints_of(a[1], entries, d.block_table) || !ints_of(a[2], table[0], d.lens) || !ints_of(a[3], table[0], d.new_lens) ||
-      !ints_of(a[4], pages[0], d.free_pages) || !ints_of(a[5], 2, d.free_state) || !out_ints(a[6], entries, d.new_table) ||
+  // (sizes and types of the tables and of the ring are known)
+  if (!contiguous(a[1]) || !data_of(a[1], d.block_table) || !contiguous(a[4]) || !data_of(a[4], d.free_pages) || !contiguous(a[6]) || !data_of(a[6], d.new_table) ||
+      !ints_of(a[2], table[0], d.lens) || !ints_of(a[3], table[0], d.new_lens) ||
+      !ints_of(a[5], 2, d.free_state) ||
       !out_ints(a[7], pages[0], d.new_free_pages) || !out_ints(a[8], 2, d.new_free_state) || !workspace_of(a[9], ws, bytes) ||
       !out_ints_or_none(a[10], table[0] + 1, d.cu_new) || !out_ints_or_none(a[11], rows, d.positions) || !out_ints_or_none(a[12], table[0], d.seq_lens) ||
       !ints_or_none(a[13], table[0], d.query_from) || !counter_of(a[14], d.short_of) || !as_address(a[0], pattern) || !as_address(a[15], stream))
@@ -735,8 +736,7 @@ PyObject* plan_layout(PyObject*, PyObject* const* a, Py_ssize_t n) { return plan
 // where there is none.
 struct Family {
   bool any = false;
-  PyObject* like = nullptr;
-  int64_t stride[3] = {0, 0, 0};
+  int64_t stride[3] = {0, 0, 0};  // (of a size of 1: 0)
 };
 alignas(16) char nothing[16];  // where a tensor without elements lies (which has no address of its own): nothing is read or written there
 bool member_of(PyObject* t, Family& f, int64_t* size, bool& sized, void*& at) {
@@ -749,10 +749,15 @@ bool member_of(PyObject* t, Family& f, int64_t* size, bool& sized, void*& at) {
     size[i] = mine[i];
   }
   sized = true;
-  if (!strides_of_both(f.any ? f.like : t, t, 4, mine, stride)) return false;
-  for (int i = 0; i < 3; ++i) f.stride[i] = stride[i];
+  const Ref strides(strides_of(t));
+  if (!strides.o || !unit_stride(strides.o, 3)) return false;
+  for (int i = 0; i < 3; ++i) {
+    if (!stride_at(strides.o, i, stride[i])) return false;
+    if (mine[i] == 1) stride[i] = 0;
+    if (f.any && f.stride[i] != stride[i]) return fail_assert();
+    f.stride[i] = stride[i];
+  }
   f.any = true;
-  f.like = t;
   if (!data_of(t, at)) return false;
   if (!at && mine[0] * mine[2] == 0) at = nothing;
   return true;
