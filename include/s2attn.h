@@ -603,11 +603,12 @@ size_t s2_kv_plan_workspace_bytes(int32_t nseq, int32_t heads);
 /* y = w * x / sqrt(mean(x^2) + eps) over the head_dim features of a row (with a weight; else y = x), then each pair of the first rotary_dim features turned by
  * the angle position * inv_freq[pair]: (a, b) -> (a cos - b sin, b cos + a sin); from the strides of a projection to those of the attention calls (a packed batch,
  * and the rows of s2_kv_append_paged and s2_attn_chunk_paged, are batch = 1).  All in 32 bits, angles in 64, one rounding to bf16.
- * Outputs may be the inputs themselves, with the same strides.  Errors: NULL, BAD_PARAM (eps, interleaved), SHAPE, ALIGN, HIP. */
+ * Outputs may be the inputs themselves, with the same strides, q_out not k or k_out.  Errors: NULL, BAD_PARAM (eps, interleaved), SHAPE, ALIGN, HIP. */
 int s2_qk_norm_rope_fwd(const s2_qk_norm_rope_args* a, void* stream);
 
 /* Its gradient: from q, k (as they went in) and d_q_out, d_k_out to dq, dk (bf16) and, where there is a weight, dq_weight, dk_weight (fp32, summed over
- * batch, heads and rows in an order that the sizes alone decide).  dq may be q or d_q_out itself, with the same strides, and dk likewise.
+ * batch, heads and rows in an order that the sizes alone decide).  dq may be q or d_q_out itself, with the same strides, and dk likewise;
+ * nothing that is written for queries may be of the keys', weights that both share have a gradient of either's.
  * workspace: s2_qk_norm_rope_bwd_workspace_bytes(...) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit; none is needed without weights.
  * Errors as above plus WORKSPACE. */
 int s2_qk_norm_rope_bwd(const s2_qk_norm_rope_args* a, void* workspace, size_t workspace_bytes, void* stream);

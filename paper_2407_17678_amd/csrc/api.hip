@@ -1145,13 +1145,19 @@ int qk_rope(const s2_qk_norm_rope_args* a, bool bwd, s2::QkRopeParams& p) {
   }
   const bool alike = (a->batch == 1 || a->in_stride_b == a->out_stride_b) && (a->heads == 1 || a->in_stride_h == a->out_stride_h) &&
                      (a->seqlen <= 1 || a->in_stride_t == a->out_stride_t);
+  // (queries and keys go through at the same time)
+  if (x[0] && x[1] && rows > 0) {
+    if (out[0] == out[1] || (bwd && weight[0] && weight[1] && d_weight[0] == d_weight[1])) return S2_ERR_SHAPE;
+    for (int i = 0; i < 2; ++i)
+      if (out[i] == x[1 - i] || (bwd && out[i] == g[1 - i])) return S2_ERR_SHAPE;
+  }
   for (int i = 0; i < 2; ++i) {
     if (!x[i]) continue;
     for (const void* y : {x[i], (const void*)out[i], bwd ? g[i] : nullptr, (const void*)weight[i]})
       if (!aligned16(y)) return S2_ERR_ALIGN;
     if (bwd && (reinterpret_cast<uintptr_t>(d_weight[i]) & 3u) != 0) return S2_ERR_ALIGN;
     // (in place a row goes where it came from)
-    if (!alike && out[i] == (bwd ? g[i] : x[i])) return S2_ERR_SHAPE;
+    if (!alike && rows > 0 && out[i] == (bwd ? g[i] : x[i])) return S2_ERR_SHAPE;
     p.x[i] = static_cast<const uint16_t*>(x[i]);
     p.y[i] = static_cast<uint16_t*>(out[i]);
     p.g[i] = static_cast<const uint16_t*>(g[i]);

@@ -37,3 +37,16 @@ def test_rows_are_as_in_a_call_of_their_own():
             B.s2_qk_norm_rope_bwd(*x, *g, *back, *c["w"], torch.empty(128, device="cuda"), None, c["freq"], EPS, ws, positions=at)
             for i in range(2):
                 assert np.array_equal(G.to_f64(out[i])[0], y[i][b, :, lo:hi]) and np.array_equal(G.to_f64(back[i])[0], dx[i][b, :, lo:hi])
+
+
+def test_no_rows_between_different_strides():
+    x = torch.zeros(0, 3, 4, 128, dtype=torch.bfloat16, device="cuda")
+    q, k, dq = (x[:, i].transpose(0, 1)[None] for i in range(3))
+    out = [torch.zeros(1, 4, 0, 128, dtype=torch.bfloat16, device="cuda") for _ in "qk"]
+    w, f = torch.ones(128, device="cuda"), torch.ones(64, device="cuda")
+    B.s2_qk_norm_rope_fwd(q, k, *out, w, w, f, EPS)
+    dw = [torch.full((128,), 9.0, device="cuda") for _ in "qk"]
+    ws = torch.empty(B.s2_qk_norm_rope_bwd_workspace_bytes(1, 4, 0, 128), dtype=torch.uint8, device="cuda")
+    B.s2_qk_norm_rope_bwd(q, k, *out, dq, dq, w, w, *dw, f, EPS, ws)
+    torch.cuda.synchronize()
+    assert all((t == 0).all() for t in dw)

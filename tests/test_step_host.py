@@ -160,6 +160,20 @@ def test_backward_rotations_that_are_refused(bad, status):
     assert _bwd(**bad) == status
 
 
+@pytest.mark.parametrize("bad", [dict(q_out=0x2000), dict(k_out=0x1000), dict(k_out=0x3000)])
+def test_outputs_of_queries_that_are_the_keys_are_refused(bad):
+    same = dict(out_stride_b=1920, out_stride_h=128, out_stride_t=384)
+    assert _fwd(**bad) == _fwd(**bad, **same) == SHAPE
+    assert _fwd(seqlen=0, **bad) == _fwd(seqlen=0, q_out=0x1000) == 0
+
+
+@pytest.mark.parametrize("bad", [dict(dq=0x2000), dict(dk=0x1000), dict(dq=0x9000), dict(dk=0x8000), dict(dk=0xa000), dict(dk_weight=0xc000)])
+def test_gradients_of_queries_that_are_the_keys_are_refused(bad):
+    same = dict(out_stride_b=1920, out_stride_h=128, out_stride_t=384)
+    assert _bwd(**bad) == _bwd(**bad, **same) == SHAPE
+    assert _bwd(seqlen=0, q_weight=None, k_weight=None, ws=None, **bad) == 0
+
+
 def test_workspaces_of_rotations():
     f = B.s2_qk_norm_rope_bwd_workspace_bytes
     assert f(0, 3, 5, 128) == f(2, 0, 5, 128) == f(2, 3, -1, 128) == f(2, 3, 5, 96) == 0
