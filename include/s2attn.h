@@ -608,7 +608,7 @@ int s2_qk_norm_rope_fwd(const s2_qk_norm_rope_args* a, void* stream);
 
 /* Its gradient: from q, k (as they went in) and d_q_out, d_k_out to dq, dk (bf16) and, where there is a weight, dq_weight, dk_weight (fp32, summed over
  * batch, heads and rows in an order that the sizes alone decide).  dq may be q or d_q_out itself, with the same strides, and dk likewise;
- * nothing that is written for queries may be of the keys', weights that both share have a gradient of either's.
+ * nothing that is written for the queries may be the keys', or the other way (of a weight that both share there are two gradients, which the caller adds up).
  * workspace: s2_qk_norm_rope_bwd_workspace_bytes(...) bytes, DEVICE, 256-byte aligned, contents undefined on entry and exit; none is needed without weights.
  * Errors as above plus WORKSPACE. */
 int s2_qk_norm_rope_bwd(const s2_qk_norm_rope_args* a, void* workspace, size_t workspace_bytes, void* stream);
