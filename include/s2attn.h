@@ -566,8 +566,8 @@ size_t s2_attn_tree_workspace_bytes(int32_t nseq, int32_t heads, int32_t nodes, 
  * row (start[b] + i) div S of the mask keeps: a chunk gives what as many decode steps give.  A row whose position is outside [0,
  * max_blocks*block_size) gets o = 0 and lse = -inf, and so does one all of whose kept blocks are not resident; such blocks contribute nothing and are counted.
  * Rows that belong to no sequence are left as they were.  What a row does not attend stays out of its result whatever it holds; of what it attends, a V that
- * is NaN, or infinities of both signs, give NaN in their feature, and an infinity an infinity of its sign, however small its token's probability (or NaN, where
- * that is 0).  With max_new (or num_rows) up to 64 probabilities go to V in 16 bits, as in a decode step, else those of 128 rows at a time that lie in
+ * is NaN, or infinities of both signs, give NaN in their feature, and an infinity an infinity of its sign (or NaN, where its token's
+ * probability is below 2^-100 of the row's largest).  With max_new (or num_rows) up to 64 probabilities go to V in 16 bits, as in a decode step, else those of 128 rows at a time that lie in
  * the same 128 positions rounded to bf16, as in s2_attn_fwd, or in 16 bits if they are 32 or fewer; each relative to a power of two of up to 2^8 (the sum is not).
  * max_new is a limit, not a size: the tokens of a sequence beyond it are rows of nobody.  Offsets of cu_new outside [0, num_rows] are cut to it.
  * q and o may be the same tensor.

@@ -196,7 +196,9 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
       if (__any(mx - m_run > tau)) {  // (-inf minus itself is not a number, and no reason to move)
         const float top = max_halves(mx);
         const bool moves = top - m_run > tau;
-        alpha = moves ? fast_exp2(m_run * cl - top * cl) : 1.f;  // (what another query's maximum does leaves this one's result as it is)
+        // (What another query's maximum does leaves this one's result as it is.  Never 0, but the smallest number there is: by the time that it is applied, a half step later,
+        // infinities of V that belong to the scores that moved it have been added, and 0 times those is none.)
+        alpha = moves ? fmaxf(fast_exp2(m_run * cl - top * cl), 0x1p-149f) : 1.f;
         m_run = moves ? top : m_run;
         mc = m_run == kNegInf ? 0.f : m_run * cl;
         l_run *= alpha;
