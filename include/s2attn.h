@@ -241,7 +241,7 @@ typedef struct {
   int32_t num_rows;       /* rows of q and o                                                  */
   int32_t max_new;        /* no sequence has more new tokens (>= 0; what is beyond is not looked at) */
   int32_t num_splits;     /* KV splits per (sequence, head); 0 = library chooses              */
-  int64_t q_stride_row, q_stride_head; /* elements, multiples of 8                            */
+  int64_t q_stride_row, q_stride_head; /* elements, multiples of 8; no two rows share an element */
 } s2_chunk_args;
 
 /* The block tables of a paged cache before a step, from the lengths of the requests.  Pages that no table holds lie in a ring
@@ -267,7 +267,8 @@ typedef struct {
 } s2_kv_plan_args;
 
 /* Queries and keys on their way from a projection to attention: element (b,h,t,d) of q and k at b*in_stride_b + h*in_stride_h +
- * t*in_stride_t + d, of q_out and k_out at the out_* strides; gradients of either at the strides of what they are the gradient of. */
+ * t*in_stride_t + d, of q_out and k_out at the out_* strides; gradients of either at the strides of what they are the gradient of.  Rows that are
+ * read may be the same ones (strides of 0); of what is written no two share an element, so that the gradient of such a q or k cannot have its strides: SHAPE. */
 typedef struct {
   const void* q;           /* DEVICE bf16, in; NULL: keys only (then k is given)              */
   const void* k;           /* DEVICE bf16, in; NULL: queries only                             */

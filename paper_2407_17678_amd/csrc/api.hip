@@ -6,6 +6,7 @@
 #include <atomic>
 #include <cmath>
 #include <cstring>
+#include <initializer_list>
 #include <limits>
 #include <new>
 
@@ -995,6 +996,44 @@ int tree_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_pag
   return attend_cache(lp, layout, c, p, scale, a->num_splits, workspace, workspace_bytes, stream);
 }
 
+// Rows of a tensor: n of them, `stride` elements apart, for each of its dimensions but the last.
+struct Steps {
+  int64_t n, stride;
+};
+// Whether so many steps of each stride (fewer than n, either way; strides in descending order, none 0) lead to less than `row` elements from -offset.
+bool steps_meet(const Steps* s, int count, int64_t row, __int128 offset) {
+  if (count == 0) return offset > -row && offset < row;
+  __int128 reach = row - 1;
+  for (int i = 1; i < count; ++i) reach += (__int128)(s[i].n - 1) * s[i].stride;
+  // (what is further away the other strides cannot make up for)
+  auto floor_of = [&](__int128 x) { return x < 0 ? -((-x + s[0].stride - 1) / s[0].stride) : x / s[0].stride; };
+  const __int128 lo = std::max<__int128>(-floor_of(reach + offset), 1 - s[0].n), hi = std::min<__int128>(floor_of(reach - offset), s[0].n - 1);
+  for (__int128 k = lo; k <= hi; ++k)
+    if (steps_meet(s + 1, count - 1, row, offset + k * s[0].stride)) return true;
+  return false;
+}
+// Whether two rows of `row` elements share one, as those of a broadcast dimension do: of what is written none may (it would hold what came last).
+bool rows_overlap(int64_t row, std::initializer_list<Steps> dims) {
+  Steps s[3];
+  int count = 0;
+  for (const Steps& d : dims)
+    if (d.n > 1) s[count++] = d;
+  std::sort(s, s + count, [](const Steps& a, const Steps& b) { return a.stride > b.stride; });
+  // each stride beyond all that the smaller ones reach: as nearly all tensors lie
+  __int128 extent = row;
+  int i = count - 1;
+  for (; i >= 0 && s[i].stride >= extent; --i) extent += (__int128)(s[i].n - 1) * s[i].stride;
+  if (i < 0) return false;
+  if (s[count - 1].stride < row) return true;
+  for (; i >= 0; --i) {  // (two rows whose first difference is k steps of stride i)
+    __int128 reach = row - 1;
+    for (int j = i + 1; j < count; ++j) reach += (__int128)(s[j].n - 1) * s[j].stride;
+    for (__int128 k = 1; k < s[i].n && k * s[i].stride <= reach; ++k)
+      if (steps_meet(s + i + 1, count - i - 1, row, k * s[i].stride)) return true;
+  }
+  return false;
+}
+
 // The most splits that the library takes for a chunk: units of 64 tokens go two to a split, and the workgroups of the tiles that sequences fill a workgroup to a
 // compute unit, or two of the kernel for 33 to 64 rows, whose wavefronts wait for each other.  bf16, head_dim 128, 44 units for a query, us by splits:
 //   256 rows, 32 heads (64 tiles)    1: 73  2: 49  4: 36  6: 39  8: 38  16: 52      4 x 256 rows, 32 heads (256)   1: 76  2: 79  4: 89
@@ -1039,6 +1078,7 @@ int chunk_cache(const s2_layout_params* lp, const s2_layout* layout, const s2_pa
     if ((reinterpret_cast<uintptr_t>(x) & 3u) != 0) return S2_ERR_ALIGN;
   s2::CacheChunkParams p = chunk_sizes(c->nseq, c->heads, a->max_new, a->num_rows);
   if (p.max_new == 0) return S2_OK;
+  if (rows_overlap(c->head_dim, {{a->num_rows, a->q_stride_row}, {c->heads, a->q_stride_head}})) return S2_ERR_SHAPE;
   const int64_t groups = s2::chunk_tiles(p) * c->heads;
   if (groups > s2::kMostGroups) return S2_ERR_SHAPE;
   const int64_t blocks = layout ? layout->max_row_blocks : s2::row_blocks(*lp, 0, (max_len - 1) / c->block_size, nullptr, 0);
@@ -1143,6 +1183,9 @@ int qk_rope(const s2_qk_norm_rope_args* a, bool bwd, s2::QkRopeParams& p) {
     if (s < 0 || (s & 7) != 0) return S2_ERR_ALIGN;
     if (s > (int64_t)1 << 40) return S2_ERR_SHAPE;
   }
+  if (rows > 0 && (bwd ? rows_overlap(a->head_dim, {{a->batch, a->in_stride_b}, {a->heads, a->in_stride_h}, {a->seqlen, a->in_stride_t}})
+                       : rows_overlap(a->head_dim, {{a->batch, a->out_stride_b}, {a->heads, a->out_stride_h}, {a->seqlen, a->out_stride_t}})))
+    return S2_ERR_SHAPE;
   const bool alike = (a->batch == 1 || a->in_stride_b == a->out_stride_b) && (a->heads == 1 || a->in_stride_h == a->out_stride_h) &&
                      (a->seqlen <= 1 || a->in_stride_t == a->out_stride_t);
   // (queries and keys go through at the same time)
