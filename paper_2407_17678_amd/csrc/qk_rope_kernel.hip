@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * kRopeWaves) void qk_rope_kernel(const QkRopePa
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
         own[e] *= w[e];
-        other[e] *= turn.swapped ? wo[e ^ 1] : wo[e];
+        other[e] = turn.on ? other[e] * (turn.swapped ? wo[e ^ 1] : wo[e]) : 0.f;  // (0 times an infinite weight is none)
       }
     }
     auto load = [&](int h) __attribute__((always_inline)) { return h < h1 ? load_once(x + h * p.x_sh) : u32x4{}; };
