@@ -35,10 +35,10 @@ __device__ __forceinline__ float feature_of(const u32x4& x, int e) { return e & 
 
 // A row's part that nothing here reads again.  (Of 32 heads, 32768 tokens, forward: 225 us with ordinary loads and stores, 222 with these loads, 208 with such stores as
 // well, 202 with the next heads' loads before these heads' sums, 5.3 TB/s, a large copy's rate; without the arithmetic 200.  Of 4 x 16 heads, 8192 tokens, backward: 169
-// with these loads, 155 with such stores and the next heads' loads first; on another day 152, and with ordinary stores, for 256 MB (kFarBytes), 149, 5.4 TB/s.)
+// with these loads, 158 with such stores, 155 with the next heads' loads first, 5.2 TB/s.)
 __device__ __forceinline__ u32x4 load_once(const uint16_t* at) { return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(at)); }
 
-// A row's part of the results; FAR: of more than the caches hold.
+// A row's part of the results; FAR: of more than kFarBytes.
 template <bool FAR>
 __device__ __forceinline__ void store(uint16_t* at, const u32x4& x) {
   if (FAR)
@@ -295,10 +295,16 @@ void head_groups(QkRopeParams& p, int64_t waves) {
 }
 
 constexpr int64_t kFwdWaves = 8192;
-// Bytes of results beyond which they go past the caches: what the cache behind the L2s holds.  Up to there whatever comes next finds them in it (ordinary stores and such
-// ones, us: 64 MB with the attention that reads them 110 and 114, 256 MB forward 91 and 99, with the attention 489 and 500, backward 157 and 164); beyond, they go out
-// faster (288 MB 117 and 116, 384 MB 158 and 146, 512 MB 216 and 203, backward 338 and 308), though an attention of 32768 tokens after it is slower by more (both 1185 and 1210).
-constexpr int64_t kFarBytes = 256 << 20;
+// Bytes of results beyond which they go past the caches.  The cache behind the L2s holds 256 MB, of everything that passes: four states in turn, each call alone and with what
+// reads its results (forward: the attention; backward: a matrix product), us with ordinary stores and with such ones:
+//   results      forward alone     with the attention    backward alone    with the product
+//    16 MB        15.0   14.4        37.9   40.2            18.9   18.7       86.2   87.2
+//    64 MB        32.8   32.4       114    117              43.8   46.6      153    157
+//    96 MB        41.3   39.4       163    166              69.6   66.5      211    214
+//   128 MB        56.1   54.8       224    230              91.8   84.5      261    260
+//   256 MB       100     96.5       429    433             172    156        452    451
+//   384 MB       160    148         805    820             254    234        701    695
+constexpr int64_t kFarBytes = 64 << 20;
 constexpr int kBwdParts = 1024;
 
 bool is_far(const QkRopeParams& p) { return (int64_t)p.rows * p.heads * p.head_dim * 2 * ((p.x[0] != nullptr) + (p.x[1] != nullptr)) > kFarBytes; }
