@@ -1,7 +1,8 @@
 // Attention of a chunk of more than 64 new tokens over a paged cache: tiles of 128 rows, 32 to a wavefront (see cache_chunk_kernel.hip for the mathematics).
 //
 // Matrix instructions bound it (41 % of a SIMD's cycles), and beside them the vector instructions of the softmax and of bringing rows to bf16 (51 %): 2048 rows of 32 heads
-// after 30720 tokens over e4m3, 512 workgroups of 47 units, 114 us, 858 TFLOP/s; the forward of a whole sequence takes 116 for such rows from contiguous bf16.  A SIMD overlaps the two where they alternate finely in
+// after 30720 tokens over e4m3, 512 workgroups of 47 units, 115 us among many such calls (850 TFLOP/s), 118 in a trace of 300, up to 137 in shorter runs; the forward of the same rows
+// over contiguous bf16, timed in turn, 94 among many, up to 109.  A SIMD overlaps the two where they alternate finely in
 // one instruction stream (sched_util.h), so the loop is software pipelined by halves of a unit, 32 tokens: in half step j a wavefront forms the scores of half j, turns those of
 // half j - 1 into probabilities and adds the product of half j - 2's with V, which are independent of each other, in one hand-written sequence of slots, a
 // matrix instruction to each.  V lags behind K by a unit, so that both tiles of a trip are used up in it and one barrier a trip is enough: meanwhile each
@@ -113,7 +114,8 @@ __global__ __launch_bounds__(256, D == 64 ? 3 : 2) void cache_chunk_wide_kernel(
 
   // scores of two halves, then their probabilities in 32 bits: register r is token 8 * (r / 4) + 4 * half + r % 4 of the half, lane % 32 the query
   f32x16 s0 = f32x16{}, s1 = f32x16{};
-  // the same as operands: rounded to bf16, as in the forward of a whole sequence: off by up to 2^-8 of a probability
+  // the same as operands: rounded to bf16, as in the forward of a whole sequence: off by up to 2^-8 of a probability, 2.3e-3 of a result instead of 1.7e-3 (relative L2).  (In two
+  // terms, 16 bits, as for fewer rows, V is multiplied twice: 2048 rows over e4m3 140 us and 174, 12 ragged chunks over bf16 206 and 235, 7 over e2m1 23.4 and 24.8.)
   u32x4 pb0[2] = {u32x4{}, u32x4{}}, pb1[2] = {u32x4{}, u32x4{}};
 
   // The fragments of a trip, in one ring through both of its half steps: of half f / NS the rows of K, then those of V, transposed.
